@@ -46,6 +46,12 @@ extern "C" {
 #define SD_EPI_NONE 0
 #define SD_EPI_GEGLU 1
 
+#define SD_ACT_NONE 0
+#define SD_ACT_GELU 1      /* z Phi(z), exact (erf) form                              */
+#define SD_ACT_GELU_TANH 2 /* its tanh form                                           */
+#define SD_ACT_SILU 3      /* z / (1 + exp(-z))                                       */
+#define SD_ACT_RELU 4
+
 /* One linear projection with an optional rank-r adapter (Section 2, "Low-Rank
  * Adaptation": the patched weight is the base weight plus a rank-r product).
  * All pointers are device memory; bias, A, B may be NULL (A and B together). */
@@ -287,6 +293,82 @@ int sd_groupnorm_fwd(const uint16_t* x, uint16_t* y, const uint16_t* gamma, cons
 int sd_groupnorm_silu_fwd(const uint16_t* x, uint16_t* y, const uint16_t* gamma, const uint16_t* beta,
                           int32_t Bn, int32_t T, int32_t C, int32_t groups, float eps,
                           void* ws, size_t ws_bytes, void* stream);
+
+/* ---- layernorm_fwd / layernorm_bwd -------------------------------------------------------
+ * Layer norm as an operator of its own, for the blocks of diffusion transformers (the backbones to
+ * which the paper carries its ideas over), with what its backward pass needs.
+ *   mean = sum_c x / C, rstd = 1 / sqrt(sum_c (x - mean)^2 / C + eps), y = (x - mean) rstd gamma + beta
+ *   x            device [M, C] of x_dtype;  y device [M, C] of y_dtype (bf16 or fp32 each); y may alias x
+ *                if the types are the same
+ *   gamma, beta  device [C] bf16; NULL: ones, zeros
+ *   mean, rstd   device [M] fp32 or NULL: kept for the backward pass
+ * Backward: n = (x - mean) rstd, g = dy gamma;  dx = rstd (g - sum_c g / C - n sum_c (g n) / C),
+ *   dgamma = sum_m dy n, dbeta = sum_m dy, added up in a fixed order.
+ *   dy           device [M, C] of y_dtype;  dx device [M, C] of x_dtype; may alias x, or dy if the types
+ *                are the same
+ *   dgamma, dbeta device [C] fp32, overwritten (zeros for M = 0); NULL: not wanted.  With neither of
+ *                them ws may be NULL.
+ * 4 <= C <= 16384, any C (SD_EUNSUPPORTED outside).  A row that holds an infinity or NaN gives NaN in that row. */
+int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* gamma, const uint16_t* beta, float eps, void* y, int32_t y_dtype,
+                     float* mean, float* rstd, int32_t M, int32_t C, void* stream);
+size_t sd_layernorm_bwd_workspace_bytes(int32_t M, int32_t C);
+int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_dtype, const float* mean, const float* rstd, const uint16_t* gamma,
+                     void* dx, float* dgamma, float* dbeta, int32_t M, int32_t C, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- rope_fwd / rope_bwd -------------------------------------------------------------------
+ * Rotary positions with several axes, height and width of an image's latent or time, height and
+ * width of a video's, on the queries and keys that sd_attention_fwd reads.  A head's first 2 R elements are R pairs
+ * (R = pairs[0] + ... + pairs[n_axes - 1]); axis a owns pairs[a] of them, in order.  The i-th pair of an axis turns by
+ *   pos[t, a] theta^(-i / pairs[a]), or, with `whole`, pair p of the head by pos[t, a] theta^(-p / R):
+ *   y_lo = x_lo cos - x_hi sin,  y_hi = x_lo sin + x_hi cos.  Elements from 2 R on are copied.
+ * Backward (gradients of the results in, of the arguments out) turns by the opposite angle.
+ *   layout     which elements pair p has: SD_ROPE_INTERLEAVED 2p and 2p + 1; SD_ROPE_HALVES p and p + R;
+ *              SD_ROPE_AXIS_HALVES each axis has 2 pairs[a] elements of its own, in order, of which the i-th
+ *              and the (i + pairs[a])-th are a pair
+ *   pos        device fp32 [Bn, T, n_axes], samples pos_stride elements apart (0: all samples have the same);
+ *              4-byte aligned; fractions are fine, whole numbers are exact up to 2^24
+ *   q, k       device [Bn * T] rows of heads x head_dim elements, ld elements apart (the queries and keys of packed
+ *              rows, for instance); heads_k = 0: queries alone (k, yk NULL)
+ *   yq, yk     rows like those; may be the same rows as q and k (in place), else they do not overlap them
+ * head_dim is a multiple of 8, at most 256 (SD_EUNSUPPORTED otherwise); ld are multiples of 8. */
+#define SD_ROPE_INTERLEAVED 0
+#define SD_ROPE_HALVES 1
+#define SD_ROPE_AXIS_HALVES 2
+#define SD_ROPE_MAX_AXES 4
+#define SD_ROPE_MAX_HEADS 256
+typedef struct sd_rope {
+    int32_t head_dim, n_axes;
+    int32_t pairs[SD_ROPE_MAX_AXES];
+    int32_t layout, whole;
+    double theta;
+} sd_rope;
+int sd_rope_fwd(const sd_rope* r, const float* pos, int64_t pos_stride, const void* q, int64_t ldq, int32_t heads_q, void* yq, int64_t ldyq,
+                const void* k, int64_t ldk, int32_t heads_k, void* yk, int64_t ldyk, int32_t dtype, int32_t Bn, int32_t T, void* stream);
+int sd_rope_bwd(const sd_rope* r, const float* pos, int64_t pos_stride, const void* dq, int64_t ldq, int32_t heads_q, void* dxq, int64_t ldyq,
+                const void* dk, int64_t ldk, int32_t heads_k, void* dxk, int64_t ldyk, int32_t dtype, int32_t Bn, int32_t T, void* stream);
+
+/* ---- linear_fwd / linear_bwd ---------------------------------------------------------------
+ * A linear layer without adapter with what follows it in the feed-forward and behind the attention of a diffusion
+ * transformer's block (sd_lora_linear_fwd has the adapter and the GEGLU), and its backward pass:
+ *   z = x W^T + bias,  y = act(z) + residual
+ *   x         device [M, K] bf16;  W device [N, K] bf16;  bias device [N] bf16 or NULL
+ *   act       SD_ACT_*
+ *   residual  device [M, N] of y_dtype or NULL; may alias y
+ *   y         device [M, N] of y_dtype, bf16 or fp32
+ *   z         device [M, N] bf16 or NULL: what the backward pass of an activation needs
+ * Backward: dz = dy act'(z);  dx = dz W,  dW = dz^T x,  dbias = sum_m dz.  (The residual's gradient is dy.)
+ *   dy        device [M, N] of y_dtype;  z as kept by the forward call (not read for SD_ACT_NONE)
+ *   dx        device [M, K] bf16, dW device [N, K] bf16 or fp32 (dw_dtype), dbias device [N] fp32; each
+ *             overwritten, or NULL: not wanted (x and W may be NULL where nothing needs them).  None of them
+ *             aliases an input.
+ *   The products multiply dz in bf16 (rounded once) and sum in fp32; dbias sums dz as it was before.  All sums
+ *   are in a fixed order.
+ * K is a multiple of 8 (SD_EUNSUPPORTED otherwise); M and N are any. */
+int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int32_t act, const void* residual, void* y, int32_t y_dtype, uint16_t* z,
+                  int32_t M, int32_t N, int32_t K, void* stream);
+size_t sd_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, const uint16_t* W, const uint16_t* z, int32_t act, uint16_t* dx, void* dW, int32_t dw_dtype,
+                  float* dbias, int32_t M, int32_t N, int32_t K, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- spatial_transformer_fwd ----------------------------------------------------------
  * The whole hot path on the guidance pair (Section 3.3: both latents in one batch):

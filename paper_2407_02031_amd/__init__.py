@@ -9,6 +9,9 @@ import importlib
 
 _BINDING_NAMES = {
     "lora_linear_fwd", "attention_fwd", "attn_block_fwd", "ff_block_fwd", "groupnorm_fwd",
+    "layernorm_fwd", "layernorm_bwd", "Rope", "rope_fwd", "rope_bwd", "linear_fwd", "linear_bwd",
+    "SD_ACT_NONE", "SD_ACT_GELU", "SD_ACT_GELU_TANH", "SD_ACT_SILU", "SD_ACT_RELU",
+    "SD_ROPE_INTERLEAVED", "SD_ROPE_HALVES", "SD_ROPE_AXIS_HALVES",
     "spatial_transformer_fwd", "spatial_transformer_workspace_bytes", "multi_lora_linear_fwd",
     "lora_patch", "lora_unpatch", "timing_enable", "timing_collect", "timing_disable", "TIMING_TAGS", "PatchPlan", "Proj", "StackParams", "to_bf16", "SwiftDiffError",
     "SD_BF16", "SD_F32", "SD_EPI_NONE", "SD_EPI_GEGLU", "LIB_PATH", "EXPORTS", "lib",

@@ -21,6 +21,9 @@ LIB_PATH = os.environ.get("SWIFTDIFF_LIB") or os.path.join(_HERE, "libswiftdiff.
 
 SD_BF16, SD_F32 = 0, 1
 SD_EPI_NONE, SD_EPI_GEGLU = 0, 1
+SD_ACT_NONE, SD_ACT_GELU, SD_ACT_GELU_TANH, SD_ACT_SILU, SD_ACT_RELU = range(5)
+SD_ROPE_INTERLEAVED, SD_ROPE_HALVES, SD_ROPE_AXIS_HALVES = range(3)
+SD_ROPE_MAX_AXES = 4
 _ERR = {-1: "SD_EINVAL", -2: "SD_EUNSUPPORTED", -3: "SD_EWORKSPACE", -4: "SD_EHIP"}
 
 
@@ -64,6 +67,11 @@ class sd_patch_multi_desc(C.Structure):
                 ("r", C.c_int32 * SD_PATCH_MAX_ADAPTERS), ("scale", C.c_float * SD_PATCH_MAX_ADAPTERS)]
 
 
+class sd_rope(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("n_axes", C.c_int32), ("pairs", C.c_int32 * SD_ROPE_MAX_AXES),
+                ("layout", C.c_int32), ("whole", C.c_int32), ("theta", C.c_double)]
+
+
 BAL_LOAD_FN = C.CFUNCTYPE(C.c_int32, C.c_void_p, C.c_int32)
 
 
@@ -101,6 +109,14 @@ def _load() -> C.CDLL:
         "sd_groupnorm_workspace_bytes": (sz, [i32, i32, i32, i32]),
         "sd_groupnorm_fwd": (C.c_int, [vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, sz, vp]),
         "sd_groupnorm_silu_fwd": (C.c_int, [vp, vp, vp, vp, i32, i32, i32, i32, f32, vp, sz, vp]),
+        "sd_layernorm_fwd": (C.c_int, [vp, i32, vp, vp, f32, vp, i32, vp, vp, i32, i32, vp]),
+        "sd_layernorm_bwd_workspace_bytes": (sz, [i32, i32]),
+        "sd_layernorm_bwd": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, vp, sz, vp]),
+        "sd_rope_fwd": (C.c_int, [P(sd_rope), vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, i32, i32, i32, vp]),
+        "sd_rope_bwd": (C.c_int, [P(sd_rope), vp, i64, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, i32, i32, i32, vp]),
+        "sd_linear_fwd": (C.c_int, [vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp]),
+        "sd_linear_bwd_workspace_bytes": (sz, [i32, i32, i32]),
+        "sd_linear_bwd": (C.c_int, [vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, sz, vp]),
         "sd_spatial_transformer_workspace_bytes": (sz, [i32, i32, i32, i32, i32, i32]),
         "sd_spatial_transformer_fwd": (C.c_int, [vp, vp, P(sd_stack_params), vp, i32, i32, i32, i32, i32, i32, vp, sz, vp]),
         "sd_multi_lora_linear_workspace_bytes": (sz, [i32, i32]),
@@ -136,6 +152,8 @@ EXPORTS = ["sd_last_error", "sd_version", "sd_dry_run", "sd_dry_run_text", "sd_g
            "sd_lora_linear_workspace_bytes", "sd_lora_linear_fwd", "sd_lora_linear_fwd_static",
            "sd_attn_block_workspace_bytes", "sd_attn_block_fwd", "sd_attention_workspace_bytes", "sd_attention_fwd", "sd_ff_block_workspace_bytes",
            "sd_ff_block_fwd", "sd_groupnorm_workspace_bytes", "sd_groupnorm_fwd", "sd_groupnorm_silu_fwd",
+           "sd_layernorm_fwd", "sd_layernorm_bwd_workspace_bytes", "sd_layernorm_bwd", "sd_rope_fwd", "sd_rope_bwd",
+           "sd_linear_fwd", "sd_linear_bwd_workspace_bytes", "sd_linear_bwd",
            "sd_spatial_transformer_workspace_bytes", "sd_spatial_transformer_fwd",
            "sd_multi_lora_linear_workspace_bytes", "sd_multi_lora_linear_fwd", "sd_patch_plan_bytes",
            "sd_patch_plan_build", "sd_lora_patch", "sd_lora_unpatch", "sd_patch_multi_plan_bytes",
@@ -328,6 +346,143 @@ def groupnorm_silu_fwd(x: torch.Tensor, gamma, beta, groups: int = 32, eps: floa
     w = _ws(_lib.sd_groupnorm_workspace_bytes(Bn, T, Cc, groups), ws)
     _check(_lib.sd_groupnorm_silu_fwd(_ptr(x), _ptr(y), _ptr(gamma), _ptr(beta), Bn, T, Cc, groups, eps, _ptr(w), w.numel(), _stream()))
     return y
+
+
+def _expect(name: str, t: Optional[torch.Tensor], shape, *dtypes, dense: bool = True) -> None:
+    """What the C call cannot see of a tensor: its shape, type, order and device."""
+    if t is None:
+        return
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: not on a GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, the current device is {torch.cuda.current_device()}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+
+
+_FLOATS = (torch.bfloat16, torch.float32)
+
+
+def layernorm_fwd(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, out_dtype=torch.bfloat16, stats: bool = False, out=None):
+    """Layer norm over the last axis of x [..., C], bf16 or fp32; y, or with `stats` (y, mean, rstd) for layernorm_bwd."""
+    Cc = x.shape[-1]
+    M = x.numel() // Cc if Cc else 0
+    _expect("x", x, x.shape, *_FLOATS)
+    _expect("gamma", gamma, (Cc,), torch.bfloat16)
+    _expect("beta", beta, (Cc,), torch.bfloat16)
+    _expect("out", out, x.shape, *_FLOATS)
+    y = out if out is not None else torch.empty(x.shape, dtype=out_dtype, device=x.device)
+    mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2)) if stats else (None, None)
+    _check(_lib.sd_layernorm_fwd(_ptr(x), _dt(x), _ptr(gamma), _ptr(beta), eps, _ptr(y), _dt(y), _ptr(mean), _ptr(rstd), M, Cc, _stream()))
+    return (y, mean, rstd) if stats else y
+
+
+def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma=None, weight_grads: bool = True, out=None, ws=None):
+    """(dx, dgamma, dbeta) of layernorm_fwd, the latter two fp32, or None without `weight_grads`."""
+    Cc = x.shape[-1]
+    M = x.numel() // Cc if Cc else 0
+    _expect("x", x, x.shape, *_FLOATS)
+    _expect("dy", dy, x.shape, *_FLOATS)
+    _expect("mean", mean, x.shape[:-1], torch.float32)
+    _expect("rstd", rstd, x.shape[:-1], torch.float32)
+    _expect("gamma", gamma, (Cc,), torch.bfloat16)
+    _expect("out", out, x.shape, x.dtype)
+    dx = out if out is not None else torch.empty_like(x)
+    dg, db = (torch.empty(Cc, dtype=torch.float32, device=x.device) for _ in range(2)) if weight_grads else (None, None)
+    w = _ws(_lib.sd_layernorm_bwd_workspace_bytes(M, Cc), ws) if weight_grads else None
+    _check(_lib.sd_layernorm_bwd(_ptr(dy), _dt(dy), _ptr(x), _dt(x), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(dx), _ptr(dg), _ptr(db), M, Cc,
+                                 _ptr(w), w.numel() if w is not None else 0, _stream()))
+    return dx, dg, db
+
+
+class Rope:
+    """Rotary positions with one or several axes: which pairs of a head's elements belong to which axis, and how fast they turn."""
+
+    def __init__(self, head_dim: int, axis_pairs: Sequence[int], theta: float = 10000.0, layout: int = SD_ROPE_INTERLEAVED, whole: bool = False):
+        if not 1 <= len(axis_pairs) <= SD_ROPE_MAX_AXES:
+            raise ValueError(f"{len(axis_pairs)} axes (1 to {SD_ROPE_MAX_AXES})")
+        self.head_dim, self.axis_pairs = int(head_dim), [int(n) for n in axis_pairs]
+        self.c = sd_rope(self.head_dim, len(axis_pairs), (C.c_int32 * SD_ROPE_MAX_AXES)(*self.axis_pairs), layout, int(whole), float(theta))
+
+
+def _token_rows(name: str, t: torch.Tensor, head_dim: int) -> int:
+    """Elements between the tokens of t [Bn, T, heads, head_dim], whose heads are dense and whose samples follow each other."""
+    Bn, T, H, D = t.shape
+    if D != head_dim:
+        raise ValueError(f"{name}: head dim {D}, expected {head_dim}")
+    sb, st, sh, sd = t.stride()
+    ld = st if T > 1 else sb if Bn > 1 else H * D
+    if t.numel() and (sd != 1 or (H > 1 and sh != D) or (Bn > 1 and sb != T * ld)):
+        raise ValueError(f"{name}: strides {t.stride()}: rows of heads x head dim that are one distance apart, please")
+    return ld
+
+
+def _rope(fn, rope: Rope, pos: torch.Tensor, q: torch.Tensor, k, q_out, k_out):
+    Bn, T = q.shape[:2]
+    n = len(rope.axis_pairs)
+    shared = pos.dim() == 2 or (pos.dim() == 3 and pos.shape[0] == 1)
+    _expect("pos", pos, (T, n) if pos.dim() == 2 else (1 if shared else Bn, T, n), torch.float32)
+    rows = []
+    for name, t, o in (("q", q, q_out), ("k", k, k_out)):
+        if t is None:
+            rows.append((None, None, 0, 0, 0))
+            continue
+        _expect(name, t, (Bn, T, *t.shape[2:]), q.dtype, dense=False)
+        y = o if o is not None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        _expect(name + "_out", y, t.shape, q.dtype, dense=False)
+        rows.append((t, y, t.shape[2], _token_rows(name, t, rope.head_dim), _token_rows(name + "_out", y, rope.head_dim)))
+    (q, yq, hq, ldq, ldyq), (k, yk, hk, ldk, ldyk) = rows
+    at = lambda t: t.data_ptr() if t is not None else None
+    _check(fn(C.byref(rope.c), _ptr(pos), 0 if shared else T * n, at(q), ldq, hq, at(yq), ldyq, at(k), ldk, hk, at(yk), ldyk, _dt(q), Bn, T, _stream()))
+    return yq, yk
+
+
+def rope_fwd(rope: Rope, pos: torch.Tensor, q: torch.Tensor, k=None, q_out=None, k_out=None):
+    """Queries and keys [Bn, T, heads, head_dim] turned by their positions [T, axes], [1, T, axes] or [Bn, T, axes].  They may be
+    views into the rows of a packed projection; the results may be given, the arguments themselves among them."""
+    return _rope(_lib.sd_rope_fwd, rope, pos, q, k, q_out, k_out)
+
+
+def rope_bwd(rope: Rope, pos: torch.Tensor, dq: torch.Tensor, dk=None, q_out=None, k_out=None):
+    """Gradients of rope_fwd's arguments from those of its results."""
+    return _rope(_lib.sd_rope_bwd, rope, pos, dq, dk, q_out, k_out)
+
+
+def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_NONE, residual=None, out_dtype=torch.bfloat16, save_z: bool = False, out=None):
+    """act(x W^T + bias) + residual for x [M, K]; with `save_z` (y, z), z for linear_bwd."""
+    M, K = x.shape
+    N = W.shape[0]
+    _expect("x", x, (M, K), torch.bfloat16)
+    _expect("W", W, (N, K), torch.bfloat16)
+    _expect("bias", bias, (N,), torch.bfloat16)
+    y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=x.device)
+    _expect("out", y, (M, N), *_FLOATS)
+    _expect("residual", residual, (M, N), y.dtype)
+    z = torch.empty((M, N), dtype=torch.bfloat16, device=x.device) if save_z else None
+    _check(_lib.sd_linear_fwd(_ptr(x), _ptr(W), _ptr(bias), act, _ptr(residual), _ptr(y), _dt(y), _ptr(z), M, N, K, _stream()))
+    return (y, z) if save_z else y
+
+
+def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: int = SD_ACT_NONE, grads: Sequence[bool] = (True, True, True),
+               dw_dtype=torch.bfloat16, ws=None):
+    """(dx, dW, dbias) of linear_fwd, each None where `grads` does not ask for it."""
+    M, K = x.shape
+    N = W.shape[0]
+    _expect("x", x, (M, K), torch.bfloat16)
+    _expect("W", W, (N, K), torch.bfloat16)
+    _expect("dy", dy, (M, N), *_FLOATS)
+    _expect("z", z, (M, N), torch.bfloat16)
+    dx = torch.empty((M, K), dtype=torch.bfloat16, device=x.device) if grads[0] else None
+    dW = torch.empty((N, K), dtype=dw_dtype, device=x.device) if grads[1] else None
+    db = torch.empty(N, dtype=torch.float32, device=x.device) if grads[2] else None
+    w = _ws(_lib.sd_linear_bwd_workspace_bytes(M, N, K), ws)
+    _check(_lib.sd_linear_bwd(_ptr(dy), _dt(dy), _ptr(x), _ptr(W), _ptr(z), act, _ptr(dx), _ptr(dW), _dt(dW) if dW is not None else SD_BF16, _ptr(db),
+                              M, N, K, _ptr(w), w.numel(), _stream()))
+    return dx, dW, db
 
 
 def spatial_transformer_workspace_bytes(Bn, T, Cc, Tc, Dc, r_max) -> int:

@@ -31,6 +31,51 @@ __device__ __forceinline__ float gelu_erf(float z) {
     return fmaf(fabsf(h), r, h);
 }
 
+// The tanh form: gelu(z) = z / (1 + exp(-2u)), u = sqrt(2 / pi) (z + 0.044715 z^3).
+__device__ __forceinline__ float gelu_tanh_gate(float z) {      // 1 / (1 + exp(-2u))
+    const float w = -2.f * 0.79788456080286535588f * 1.44269504088896340736f;
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(fmaf(z * z, 0.044715f * w, w) * z));
+}
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * z)); }
+// v <- act(v); the kind is the same for all lanes.  (relu keeps NaN)
+template <int N>
+__device__ __forceinline__ void apply_act(int kind, f32x4 (&v)[N]) {
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][e] = f(v[i][e]);
+    };
+    if (kind == SD_ACT_GELU) each([](float z) { return gelu_erf(z); });
+    else if (kind == SD_ACT_GELU_TANH) each([](float z) { return z * gelu_tanh_gate(z); });
+    else if (kind == SD_ACT_SILU) each([](float z) { return z * sigmoid(z); });
+    else if (kind == SD_ACT_RELU) each([](float z) { return z < 0.f ? 0.f : z; });
+}
+// act'(z)
+__device__ __forceinline__ float act_slope(int kind, float z) {
+    if (kind == SD_ACT_GELU) {
+        // Phi(z) + z phi(z), Phi from gelu_erf's polynomial
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, fabsf(z), 1.0f));
+        float p = fmaf(1.061405429f, t, -1.453152027f);
+        p = fmaf(p, t, 1.421413741f);
+        p = fmaf(p, t, -0.284496736f);
+        p = fmaf(p, t, 0.254829592f) * t;
+        const float e = __builtin_amdgcn_exp2f((-0.5f * 1.44269504088896340736f * z) * z);
+        const float half = 0.5f * p * e;                  // Phi(-|z|)
+        return (z < 0.f ? half : 1.f - half) + z * e * 0.39894228040143267794f;
+    }
+    if (kind == SD_ACT_GELU_TANH) {
+        const float s = gelu_tanh_gate(z);
+        return s + z * s * (1.f - s) * (2.f * 0.79788456080286535588f) * fmaf(3.f * 0.044715f * z, z, 1.f);
+    }
+    if (kind == SD_ACT_SILU) {
+        const float s = sigmoid(z);
+        return s * fmaf(z, 1.f - s, 1.f);
+    }
+    if (kind == SD_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;   // (NaN stays)
+    return 1.f;
+}
+
 // 256 bytes of zeros: where the lanes of a direct-to-LDS load point when their chunk lies
 // past the end of a K segment (the load itself cannot zero-fill)
 static __device__ __attribute__((aligned(256))) uint32_t g_gemm_zeros[64];

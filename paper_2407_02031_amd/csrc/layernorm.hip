@@ -1,0 +1,326 @@
+// Layer norm as an operator of its own, forward and backward, for rows of 4 to 16384 elements in fp32 or bf16.
+// (The one in norm.hip feeds a projection of the transformer block: bf16 out, and it clears flags and reads weights ahead.)
+//
+//   mean = sum_c x / C,  rstd = 1 / sqrt(sum_c (x - mean)^2 / C + eps),  y = (x - mean) rstd gamma + beta
+//   n = (x - mean) rstd, g = dy gamma:  dx = rstd (g - sum_c g / C - n sum_c (g n) / C),
+//   dgamma = sum_m dy n,  dbeta = sum_m dy
+//
+// Bound by HBM: every element is read once and written once.  A row lives in the registers of TPR threads, four elements a
+// chunk, and all of its loads are issued before the first is used.  Statistics are fp32 and taken in two steps over the
+// registers: a mean, then the sums of the deviations and of their squares, of which the first corrects the mean's own
+// rounding.  (One pass over sums and squares loses the variance's digits where a row has a large offset, or one
+// element far from all others.)
+#include "rows.hpp"
+
+namespace sd {
+
+// sums over the TPR threads of a row, in every one of them
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* sh) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        const int wave = threadIdx.x >> 6;
+        __syncthreads();                   // the last sums have been read
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sh[i * W + wave] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) v[i] += sh[i * W + w];
+        }
+    }
+}
+
+// Chunk j of thread t holds elements [at, at + 4), at = 4 (t + j TPR); the last chunk of a row whose length is no multiple
+// of four begins earlier, at C - 4, and the elements that its neighbour has too are off there, as are all of those
+// behind the row's end.  WHOLE: a chunk that every row of this kernel has whole.
+template <bool WHOLE>
+struct Chunk {
+    int at, first;      // where it begins; its first element that counts (C: none does)
+    __device__ __forceinline__ Chunk(int ch, int C) {
+        first = WHOLE ? 4 * ch : min(4 * ch, C);
+        at = WHOLE ? 4 * ch : min(4 * ch, C - 4);
+    }
+    __device__ __forceinline__ bool on(int e) const { return WHOLE || at + e >= first; }
+    template <class T>
+    __device__ __forceinline__ void store(T* p, int C, f32x4 v) const {
+        if (WHOLE || at == first) store4(p + at, v);
+        else if (first < C)
+#pragma unroll
+            for (int e = 1; e < 4; ++e)
+                if (on(e)) p[at + e] = (T)v[e];
+    }
+};
+// f(j, chunk) for the J chunks of thread t, of which the first JW are whole
+template <int TPR, int J, int JW, class F>
+__device__ __forceinline__ void each_chunk(int t, int C, F f) {
+#pragma unroll
+    for (int j = 0; j < JW; ++j) f(j, Chunk<true>(t + j * TPR, C));
+#pragma unroll
+    for (int j = JW; j < J; ++j) f(j, Chunk<false>(t + j * TPR, C));
+}
+
+constexpr int LN_THREADS = 256;
+template <int TPR>
+constexpr int ln_block() { return TPR > LN_THREADS ? TPR : LN_THREADS; }
+
+template <class X, class Y, int TPR, int J, int JW>
+__global__ __launch_bounds__(ln_block<TPR>()) void ln_fwd_kernel(const X* x, const uint16_t* __restrict__ gamma, const uint16_t* __restrict__ beta,
+                                                                 float eps, Y* y, float* __restrict__ mean, float* __restrict__ rstd, int M, int C) {
+    constexpr int RPB = ln_block<TPR>() / TPR;
+    __shared__ float sh[TPR > 64 ? 2 * TPR / 64 : 1];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    if (row >= M) return;      // (whole wavefronts; a block of one row is never past the end)
+    const X* const xr = x + row * C;
+    const __bf16* const gb = reinterpret_cast<const __bf16*>(gamma);
+    const __bf16* const bb = reinterpret_cast<const __bf16*>(beta);
+    f32x4 v[J], g[J], b[J];
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) { v[j] = load4(xr + c.at); });
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+        g[j] = gamma ? load4(gb + c.at) : f32x4{1.f, 1.f, 1.f, 1.f};
+        b[j] = beta ? load4(bb + c.at) : f32x4{0.f, 0.f, 0.f, 0.f};
+    });
+    const float inv = 1.0f / (float)C;
+    float s[2] = {0.f, 0.f}, one[1] = {0.f};
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) one[0] += c.on(e) ? v[j][e] : 0.f;
+    });
+    row_sums<TPR>(one, sh);
+    const float m0 = one[0] * inv;
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[j][e] -= m0;
+            const float d = c.on(e) ? v[j][e] : 0.f;
+            s[0] += d;
+            s[1] += d * d;
+        }
+    });
+    row_sums<TPR>(s, sh);
+    const float dm = s[0] * inv;
+    float var = s[1] * inv - dm * dm;
+    var = var < 0.f ? 0.f : var;       // (NaN stays)
+    const float r = 1.0f / sqrtf(var + eps);
+    if (mean && t == 0) mean[row] = m0 + dm;
+    if (rstd && t == 0) rstd[row] = r;
+    Y* const yr = y + row * C;
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+        f32x4 o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = (v[j][e] - dm) * r * g[j][e] + b[j][e];
+        c.store(yr, C, o);
+    });
+}
+
+// A workgroup takes every `gridDim.x`-th group of rows, keeps the sums of its columns in registers, and leaves them in
+// partials[blockIdx.x], gradient of gamma first; sum_partials adds those up.
+template <class X, class D, int TPR, int J, int JW, bool GRADS>
+__global__ __launch_bounds__(ln_block<TPR>()) void ln_bwd_kernel(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                 const uint16_t* __restrict__ gamma, X* dx, float* __restrict__ partials, int M, int C) {
+    constexpr int RPB = ln_block<TPR>() / TPR;
+    __shared__ float sh[TPR > 64 ? 2 * TPR / 64 : 1];
+    __shared__ f32x4 comb[GRADS && RPB > 1 ? (RPB - 1) * 64 * 2 : 1];
+    const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const __bf16* const gb = reinterpret_cast<const __bf16*>(gamma);
+    f32x4 g[J], ag[GRADS ? J : 1], ab[GRADS ? J : 1];
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+        g[j] = gamma ? load4(gb + c.at) : f32x4{1.f, 1.f, 1.f, 1.f};
+        if (GRADS) ag[GRADS ? j : 0] = ab[GRADS ? j : 0] = f32x4{0.f, 0.f, 0.f, 0.f};
+    });
+    const float inv = 1.0f / (float)C;
+    for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < M; row += (int64_t)gridDim.x * RPB) {
+        f32x4 v[J], d[J];
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+            v[j] = load4(x + row * C + c.at);
+            d[j] = load4(dy + row * C + c.at);
+        });
+        const float m = mean[row], r = rstd[row];
+        float s[2] = {0.f, 0.f};
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float dd = c.on(e) ? d[j][e] : 0.f;
+                v[j][e] = c.on(e) ? (v[j][e] - m) * r : 0.f;
+                if (GRADS) {
+                    ag[GRADS ? j : 0][e] += dd * v[j][e];
+                    ab[GRADS ? j : 0][e] += dd;
+                }
+                d[j][e] = dd * g[j][e];
+                s[0] += d[j][e];
+                s[1] += d[j][e] * v[j][e];
+            }
+        });
+        row_sums<TPR>(s, sh);
+        const float c1 = s[0] * inv, c2 = s[1] * inv;
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+            f32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = r * (d[j][e] - c1 - v[j][e] * c2);
+            c.store(dx + row * C, C, o);
+        });
+    }
+    if constexpr (GRADS) {
+        float* const out = partials + (int64_t)blockIdx.x * 2 * C;
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+            if constexpr (RPB > 1) {      // the wavefronts' sums, in their order
+                __syncthreads();
+                if (sub > 0) {
+                    comb[((sub - 1) * 2) * 64 + t] = ag[j];
+                    comb[((sub - 1) * 2 + 1) * 64 + t] = ab[j];
+                }
+                __syncthreads();
+                if (sub > 0) return;
+#pragma unroll
+                for (int w = 0; w < RPB - 1; ++w) {
+                    ag[j] += comb[w * 2 * 64 + t];
+                    ab[j] += comb[(w * 2 + 1) * 64 + t];
+                }
+            }
+            c.store(out, C, ag[j]);
+            c.store(out + C, C, ab[j]);
+        });
+    }
+}
+
+// 64 columns a workgroup; 16 wavefronts take every 16th row each, and their sums are added in order.
+__global__ __launch_bounds__(1024) void sum_partials_kernel(const float* __restrict__ partials, int G, float* __restrict__ out0, int n0, float* __restrict__ out1, int n1) {
+    __shared__ float sh[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, n = n0 + n1;
+    float a = 0.f;
+    if (c < n)
+#pragma unroll 8
+        for (int g = wave; g < G; g += 16) a += partials[(int64_t)g * n + c];
+    sh[wave][lane] = a;
+    __syncthreads();
+    if (wave == 0 && c < n) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) a += sh[w][lane];
+        float* const out = c < n0 ? out0 : out1;
+        if (out) out[c < n0 ? c : c - n0] = a;
+    }
+}
+int launch_sum_partials(const float* partials, int G, float* out0, int n0, float* out1, int n1, hipStream_t stream) {
+    if (SD_DRY_RUN("sum partials; ")) return SD_OK;
+    hipLaunchKernelGGL(sum_partials_kernel, dim3((n0 + n1 + 63) / 64), dim3(1024), 0, stream, partials, G, out0, n0, out1, n1);
+    SD_HIP_CHECK(hipGetLastError());
+    return SD_OK;
+}
+
+// Threads a row and chunks a thread, from the row's length: a wavefront up to 2048 elements, then 256 threads up to 8192.
+template <int TPR_, int J_, int JW_>
+struct LnShape { static constexpr int TPR = TPR_, J = J_, JW = JW_; };
+template <class F>
+static int ln_by_length(int C, F f) {
+    if (C <= 64 * 4) return f(LnShape<64, 1, 0>());
+    if (C <= 64 * 4 * 3) return f(LnShape<64, 3, 1>());
+    if (C <= 64 * 4 * 5) return f(LnShape<64, 5, 3>());
+    if (C <= 64 * 4 * 8) return f(LnShape<64, 8, 5>());
+    if (C <= 256 * 4 * 4) return f(LnShape<256, 4, 2>());
+    if (C <= 256 * 4 * 8) return f(LnShape<256, 8, 4>());
+    return f(LnShape<1024, 4, 2>());
+}
+template <class F>
+static int by_type(int dtype, F f) {
+    if (dtype == SD_F32) return f(static_cast<float*>(nullptr));
+    return f(static_cast<__bf16*>(nullptr));
+}
+
+constexpr int LN_MIN_C = 4, LN_MAX_C = 16384;
+static int ln_check(const char* who, int x_dtype, int y_dtype, int M, int C) {
+    SD_REQUIRE(M >= 0 && C > 0, SD_EINVAL, "%s: M=%d C=%d", who, M, C);
+    SD_REQUIRE(C >= LN_MIN_C && C <= LN_MAX_C, SD_EUNSUPPORTED, "%s: rows of %d elements (%d to %d)", who, C, LN_MIN_C, LN_MAX_C);
+    SD_REQUIRE((x_dtype == SD_BF16 || x_dtype == SD_F32) && (y_dtype == SD_BF16 || y_dtype == SD_F32), SD_EINVAL, "%s: types %d, %d", who, x_dtype, y_dtype);
+    return SD_OK;
+}
+
+// workgroups of the backward pass: two a CU, or one for every group of rows
+static int ln_bwd_groups(int M, int C) {
+    const int rpb = C > 2048 ? 1 : LN_THREADS / 64;
+    const int most = 512;
+    const int groups = M > 0 ? (M - 1) / rpb + 1 : 0;
+    return groups < most ? groups : most;
+}
+
+}  // namespace sd
+
+using namespace sd;
+
+extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* gamma, const uint16_t* beta, float eps, void* y, int32_t y_dtype,
+                                float* mean, float* rstd, int32_t M, int32_t C, void* stream) {
+    int rc = ln_check("layernorm_fwd", x_dtype, y_dtype, M, C);
+    if (rc) return rc;
+    if (M == 0) return SD_OK;
+    SD_REQUIRE(x && y, SD_EINVAL, "layernorm_fwd: x or y is null");
+    SD_REQUIRE(aligned16(x) && aligned16(y) && aligned16(gamma) && aligned16(beta) && aligned16(mean) && aligned16(rstd), SD_EINVAL,
+               "layernorm_fwd: pointers must be 16-byte aligned");
+    if (SD_DRY_RUN("layernorm fwd; ")) return SD_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return by_type(x_dtype, [&](auto* xt) {
+        return by_type(y_dtype, [&](auto* yt) {
+            return ln_by_length(C, [&](auto shape) {
+                using X = std::remove_pointer_t<decltype(xt)>;
+                using Y = std::remove_pointer_t<decltype(yt)>;
+                using S = decltype(shape);
+                    constexpr int B = ln_block<S::TPR>(), RPB = B / S::TPR;
+                hipLaunchKernelGGL((ln_fwd_kernel<X, Y, S::TPR, S::J, S::JW>), dim3((M - 1) / RPB + 1), dim3(B), 0, s, static_cast<const X*>(x), gamma, beta, eps,
+                                   static_cast<Y*>(y), mean, rstd, M, C);
+                SD_HIP_CHECK(hipGetLastError());
+                return (int)SD_OK;
+            });
+        });
+    });
+}
+
+extern "C" size_t sd_layernorm_bwd_workspace_bytes(int32_t M, int32_t C) {
+    if (M <= 0 || C <= 0) return 256;
+    return round_up((size_t)ln_bwd_groups(M, C) * 2 * C * 4, 256);
+}
+
+extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_dtype, const float* mean, const float* rstd, const uint16_t* gamma,
+                                void* dx, float* dgamma, float* dbeta, int32_t M, int32_t C, void* ws, size_t ws_bytes, void* stream) {
+    int rc = ln_check("layernorm_bwd", x_dtype, y_dtype, M, C);
+    if (rc) return rc;
+    const bool grads = dgamma || dbeta;
+    SD_REQUIRE(M == 0 || (dy && x && mean && rstd && dx), SD_EINVAL, "layernorm_bwd: dy, x, mean, rstd or dx is null");
+    SD_REQUIRE(aligned16(dy) && aligned16(x) && aligned16(mean) && aligned16(rstd) && aligned16(gamma) && aligned16(dx) && aligned16(dgamma) && aligned16(dbeta), SD_EINVAL,
+               "layernorm_bwd: pointers must be 16-byte aligned");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (M == 0) return grads ? launch_sum_partials(nullptr, 0, dgamma, C, dbeta, C, s) : SD_OK;    // sums over no rows
+    float* partials = nullptr;
+    if (grads) {
+        Workspace w(ws, ws_bytes);
+        const size_t need = sd_layernorm_bwd_workspace_bytes(M, C);
+        partials = static_cast<float*>(w.take(need));
+        SD_REQUIRE(partials && w.ok() && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SD_EWORKSPACE, "layernorm_bwd: workspace of %zu bytes, need %zu, 256-byte aligned", ws_bytes, need);
+    }
+    const int groups = ln_bwd_groups(M, C);
+    if (!SD_DRY_RUN("layernorm bwd; ")) {
+        rc = by_type(x_dtype, [&](auto* xt) {
+            return by_type(y_dtype, [&](auto* yt) {
+                return ln_by_length(C, [&](auto shape) {
+                    using X = std::remove_pointer_t<decltype(xt)>;
+                    using D = std::remove_pointer_t<decltype(yt)>;
+                    using S = decltype(shape);
+                    constexpr int B = ln_block<S::TPR>();
+                    if (grads)
+                        hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, true>), dim3(groups), dim3(B), 0, s, static_cast<const D*>(dy), static_cast<const X*>(x), mean, rstd, gamma,
+                                           static_cast<X*>(dx), partials, M, C);
+                    else
+                        hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, false>), dim3(groups), dim3(B), 0, s, static_cast<const D*>(dy), static_cast<const X*>(x), mean, rstd, gamma,
+                                           static_cast<X*>(dx), partials, M, C);
+                    SD_HIP_CHECK(hipGetLastError());
+                    return (int)SD_OK;
+                });
+            });
+        });
+        if (rc) return rc;
+    }
+    return grads ? launch_sum_partials(partials, groups, dgamma, C, dbeta, C, s) : SD_OK;
+}

@@ -1,0 +1,217 @@
+// Rotary positions with several axes (height and width of an image; time, height and width of a video) on queries and keys.
+//
+// A head's 2R leading elements are R pairs.  Pair p belongs to one axis a and turns by angle pos[t, a] w_p, w_p = theta^(-i / n_a)
+// for the i-th of the axis' n_a pairs (or theta^(-p / R)):
+//   y_lo = x_lo cos - x_hi sin,  y_hi = x_lo sin + x_hi cos;  backward is the same by the opposite angle.
+//
+// Bound by HBM: queries and keys are read once and written once, wherever the rows of a packed projection hold them.  A
+// workgroup takes a few tokens, forms the tokens' R cosines and sines once, in LDS, and turns all their heads with
+// them.  Angles are reduced in 64 bits, as turns, whose whole part falls away exactly: in fp32 position 10^5 would be off by
+// 2^-24 10^5 = 6e-3 turns' radians and more.
+#include "common.hpp"
+
+#include <math.h>
+#include <string.h>
+
+namespace sd {
+
+constexpr int ROPE_AXES = SD_ROPE_MAX_AXES, ROPE_MAX_D = 256, ROPE_THREADS = 256;
+constexpr int ROPE_MAX_TOKENS = 32;        // of a workgroup
+constexpr int ROPE_TABLE = 4096;           // cosine-sine pairs in LDS
+
+struct RopeArgs {
+    const float* pos;
+    int64_t pos_stride, rows;
+    const void *q, *k;
+    void *yq, *yk;
+    int64_t ldq, ldk, ldyq, ldyk;          // elements between tokens
+    int32_t T, n_axes, tokens;             // tokens of a workgroup
+    int32_t heads_q, heads, D, R;
+    int32_t units, rot_units;              // of a head; the first of them turn
+    int32_t axis_halves;
+    int32_t first[ROPE_AXES + 1];          // first pair of each axis, then R
+    float sign;
+    double log2_step[ROPE_AXES];           // log2 of the ratio of two neighbouring frequencies
+    int32_t whole;
+};
+
+template <class T, int V>
+struct RopeVec { typedef T type __attribute__((ext_vector_type(V))); };
+template <class T>
+struct RopeVec<T, 1> { typedef T type; };
+template <class T, int V>
+__device__ __forceinline__ T& elem(typename RopeVec<T, V>::type& v, int i) { return reinterpret_cast<T*>(&v)[i]; }
+
+// A unit is what a thread moves at a time: V neighbouring elements (INTER: pairs are neighbours), or V of them and the V
+// that they are paired with.
+template <class T, int V, bool INTER>
+__global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(const RopeArgs a) {
+    typedef typename RopeVec<T, V>::type vec;
+    __shared__ float2 table[ROPE_TABLE];
+    const int64_t row0 = (int64_t)blockIdx.x * a.tokens;
+    const int tokens = (int)min((int64_t)a.tokens, a.rows - row0);
+    // ---- cosines and sines of the tokens' angles
+    const int64_t b0 = row0 / a.T;
+    const int t0 = (int)(row0 - b0 * a.T);
+    for (int i = threadIdx.x; i < tokens * a.R; i += ROPE_THREADS) {
+        const int tok = i / a.R, p = i - tok * a.R;
+        int ax = 0;
+#pragma unroll
+        for (int j = 1; j < ROPE_AXES; ++j) ax += p >= a.first[j] ? 1 : 0;
+        int64_t b = b0;
+        int t = t0 + tok;
+        while (t >= a.T) {
+            t -= a.T;
+            ++b;
+        }
+        const double w = exp2(-(double)(a.whole ? p : p - a.first[ax]) * a.log2_step[ax]) * 0.15915494309189533577;   // turns per unit of position
+        const double turns = (double)a.pos[b * a.pos_stride + (int64_t)t * a.n_axes + ax] * w;
+        float s, c;
+        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        table[i] = make_float2(c, a.sign * s);
+    }
+    __syncthreads();
+    // ---- the heads
+    const int per = a.heads * a.units, n = tokens * per;
+    for (int i = threadIdx.x; i < n; i += ROPE_THREADS) {
+        const int tok = i / per, rem = i - tok * per;
+        const int head = rem / a.units, u = rem - head * a.units;
+        const bool isq = head < a.heads_q;
+        const int64_t row = row0 + tok;
+        const int h = (isq ? head : head - a.heads_q) * a.D;
+        const T* const x = static_cast<const T*>(isq ? a.q : a.k) + row * (isq ? a.ldq : a.ldk) + h;
+        T* const y = static_cast<T*>(isq ? a.yq : a.yk) + row * (isq ? a.ldyq : a.ldyk) + h;
+        const float2* const cs = table + tok * a.R;
+        if constexpr (INTER) {
+            vec v = *reinterpret_cast<const vec*>(x + u * V);
+            if (u < a.rot_units)
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    const float2 f = cs[u * (V / 2) + e / 2];
+                    const float lo = (float)elem<T, V>(v, e), hi = (float)elem<T, V>(v, e + 1);
+                    elem<T, V>(v, e) = (T)(lo * f.x - hi * f.y);
+                    elem<T, V>(v, e + 1) = (T)(lo * f.y + hi * f.x);
+                }
+            *reinterpret_cast<vec*>(y + u * V) = v;
+        } else {
+            const bool turn = u < a.rot_units;
+            const int p = u * V;
+            int lo = p, hi = p + a.R;
+            if (!turn) {
+                lo = 2 * a.R + (u - a.rot_units) * 2 * V;
+                hi = lo + V;
+            } else if (a.axis_halves) {
+                int ax = 0;
+#pragma unroll
+                for (int j = 1; j < ROPE_AXES; ++j) ax += p >= a.first[j] ? 1 : 0;
+                lo = a.first[ax] + p;
+                hi = lo + a.first[ax + 1] - a.first[ax];
+            }
+            vec l = *reinterpret_cast<const vec*>(x + lo), r = *reinterpret_cast<const vec*>(x + hi);
+            if (turn)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float2 f = cs[p + e];
+                    const float c = (float)elem<T, V>(l, e), d = (float)elem<T, V>(r, e);
+                    elem<T, V>(l, e) = (T)(c * f.x - d * f.y);
+                    elem<T, V>(r, e) = (T)(c * f.y + d * f.x);
+                }
+            *reinterpret_cast<vec*>(y + lo) = l;
+            *reinterpret_cast<vec*>(y + hi) = r;
+        }
+    }
+}
+
+template <class T, int V, bool INTER>
+static int launch_rope(RopeArgs& a, hipStream_t stream) {
+    a.units = INTER ? a.D / V : a.D / (2 * V);
+    a.rot_units = INTER ? 2 * a.R / V : a.R / V;
+    if (SD_DRY_RUN("rope %s%d; ", INTER ? "neighbours " : "halves ", V)) return SD_OK;
+    const int per = a.heads * a.units;
+    int tokens = 8 * ROPE_THREADS / per;
+    tokens = tokens < 1 ? 1 : tokens > ROPE_MAX_TOKENS ? ROPE_MAX_TOKENS : tokens;
+    while (tokens * a.R > ROPE_TABLE) --tokens;
+    a.tokens = tokens;
+    hipLaunchKernelGGL((rope_kernel<T, V, INTER>), dim3((unsigned)((a.rows - 1) / tokens + 1)), dim3(ROPE_THREADS), 0, stream, a);
+    SD_HIP_CHECK(hipGetLastError());
+    return SD_OK;
+}
+
+// Elements of an access: as many as 16 bytes hold, fewer where an axis or what a head keeps unturned ends inside.
+template <class T>
+static int launch_rope_as(RopeArgs& a, bool inter, hipStream_t stream) {
+    constexpr int MAXV = 16 / (int)sizeof(T);
+    int v = MAXV;
+    for (; v > 1; v /= 2) {
+        if (inter) {
+            if (2 * a.R % v == 0) break;
+            continue;
+        }
+        bool ok = a.R % v == 0 && (a.D - 2 * a.R) % (2 * v) == 0;
+        for (int j = 1; ok && a.axis_halves && j < a.n_axes; ++j) ok = a.first[j] % v == 0;
+        if (ok) break;
+    }
+    if (inter) {
+        if constexpr (MAXV == 8)
+            if (v == 8) return launch_rope<T, 8, true>(a, stream);
+        if (v == 4) return launch_rope<T, 4, true>(a, stream);
+        return launch_rope<T, 2, true>(a, stream);
+    }
+    if constexpr (MAXV == 8)
+        if (v == 8) return launch_rope<T, 8, false>(a, stream);
+    if (v == 4) return launch_rope<T, 4, false>(a, stream);
+    if (v == 2) return launch_rope<T, 2, false>(a, stream);
+    return launch_rope<T, 1, false>(a, stream);
+}
+
+static int rope(const char* who, float sign, const sd_rope* r, const float* pos, int64_t pos_stride, const void* q, int64_t ldq, int heads_q, void* yq, int64_t ldyq,
+                const void* k, int64_t ldk, int heads_k, void* yk, int64_t ldyk, int dtype, int Bn, int T, hipStream_t stream) {
+    SD_REQUIRE(r, SD_EINVAL, "%s: no description", who);
+    SD_REQUIRE(r->head_dim > 0 && r->head_dim <= ROPE_MAX_D && r->head_dim % 8 == 0, SD_EUNSUPPORTED, "%s: head dim %d (a multiple of 8, at most %d)", who, r->head_dim, ROPE_MAX_D);
+    SD_REQUIRE(r->n_axes >= 1 && r->n_axes <= ROPE_AXES, SD_EINVAL, "%s: %d axes (1 to %d)", who, r->n_axes, ROPE_AXES);
+    SD_REQUIRE(r->layout == SD_ROPE_INTERLEAVED || r->layout == SD_ROPE_HALVES || r->layout == SD_ROPE_AXIS_HALVES, SD_EINVAL, "%s: layout %d", who, r->layout);
+    SD_REQUIRE(r->theta > 0 && r->theta < 1e300, SD_EINVAL, "%s: theta %g", who, r->theta);
+    SD_REQUIRE(dtype == SD_BF16 || dtype == SD_F32, SD_EINVAL, "%s: type %d", who, dtype);
+    RopeArgs a;
+    memset(&a, 0, sizeof(a));
+    int64_t R = 0;
+    for (int j = 0; j < r->n_axes; ++j) {
+        SD_REQUIRE(r->pairs[j] >= 1, SD_EINVAL, "%s: axis %d has %d pairs", who, j, r->pairs[j]);
+        a.first[j] = (int32_t)R;
+        R += r->pairs[j];
+        SD_REQUIRE(2 * R <= r->head_dim, SD_EINVAL, "%s: more pairs than half of the head dim %d", who, r->head_dim);
+    }
+    for (int j = r->n_axes; j <= ROPE_AXES; ++j) a.first[j] = (int32_t)R;
+    for (int j = 0; j < r->n_axes; ++j) a.log2_step[j] = log2(r->theta) / (double)(r->whole ? R : r->pairs[j]);
+    SD_REQUIRE(Bn >= 0 && T >= 0 && heads_q >= 0 && heads_k >= 0 && heads_q <= SD_ROPE_MAX_HEADS && heads_k <= SD_ROPE_MAX_HEADS, SD_EINVAL,
+               "%s: Bn=%d T=%d heads %d, %d (at most %d)", who, Bn, T, heads_q, heads_k, SD_ROPE_MAX_HEADS);
+    if (Bn == 0 || T == 0 || heads_q + heads_k == 0) return SD_OK;
+    SD_REQUIRE(pos && (reinterpret_cast<uintptr_t>(pos) & 3u) == 0 && (pos_stride == 0 || pos_stride >= (int64_t)T * r->n_axes), SD_EINVAL, "%s: positions %p, %lld apart", who, (const void*)pos,
+               (long long)pos_stride);
+    const int64_t wq = (int64_t)heads_q * r->head_dim, wk = (int64_t)heads_k * r->head_dim;
+    SD_REQUIRE(heads_q == 0 || (q && yq && aligned16(q) && aligned16(yq) && ldq >= wq && ldyq >= wq && ldq % 8 == 0 && ldyq % 8 == 0), SD_EINVAL,
+               "%s: queries need 16-byte aligned pointers and rows of a multiple of 8 elements, %lld at least", who, (long long)wq);
+    SD_REQUIRE(heads_k == 0 || (k && yk && aligned16(k) && aligned16(yk) && ldk >= wk && ldyk >= wk && ldk % 8 == 0 && ldyk % 8 == 0), SD_EINVAL,
+               "%s: keys need 16-byte aligned pointers and rows of a multiple of 8 elements, %lld at least", who, (long long)wk);
+    a.rows = (int64_t)Bn * T;
+    SD_REQUIRE(a.rows <= 0x7fffffff, SD_EUNSUPPORTED, "%s: %lld tokens", who, (long long)a.rows);
+    a.pos = pos; a.pos_stride = pos_stride; a.q = q; a.k = k; a.yq = yq; a.yk = yk;
+    a.ldq = ldq; a.ldk = ldk; a.ldyq = ldyq; a.ldyk = ldyk;
+    a.T = T; a.n_axes = r->n_axes; a.heads_q = heads_q; a.heads = heads_q + heads_k; a.D = r->head_dim; a.R = (int32_t)R;
+    a.axis_halves = r->layout == SD_ROPE_AXIS_HALVES;
+    a.sign = sign;
+    a.whole = r->whole != 0;
+    const bool inter = r->layout == SD_ROPE_INTERLEAVED;
+    return dtype == SD_F32 ? launch_rope_as<float>(a, inter, stream) : launch_rope_as<__bf16>(a, inter, stream);
+}
+
+}  // namespace sd
+
+extern "C" int sd_rope_fwd(const sd_rope* r, const float* pos, int64_t pos_stride, const void* q, int64_t ldq, int32_t heads_q, void* yq, int64_t ldyq,
+                           const void* k, int64_t ldk, int32_t heads_k, void* yk, int64_t ldyk, int32_t dtype, int32_t Bn, int32_t T, void* stream) {
+    return sd::rope("rope_fwd", 1.f, r, pos, pos_stride, q, ldq, heads_q, yq, ldyq, k, ldk, heads_k, yk, ldyk, dtype, Bn, T, static_cast<hipStream_t>(stream));
+}
+extern "C" int sd_rope_bwd(const sd_rope* r, const float* pos, int64_t pos_stride, const void* dq, int64_t ldq, int32_t heads_q, void* dxq, int64_t ldyq,
+                           const void* dk, int64_t ldk, int32_t heads_k, void* dxk, int64_t ldyk, int32_t dtype, int32_t Bn, int32_t T, void* stream) {
+    return sd::rope("rope_bwd", -1.f, r, pos, pos_stride, dq, ldq, heads_q, dxq, ldyq, dk, ldk, heads_k, dxk, ldyk, dtype, Bn, T, static_cast<hipStream_t>(stream));
+}

@@ -1,0 +1,111 @@
+"""Layer norm, rotary positions and the linear layer with its gradients: what the calls refuse, and what they would launch, without a GPU."""
+import ctypes as C
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2407_02031_amd", "libswiftdiff.so")
+EINVAL, EUNSUPPORTED, EWORKSPACE = -1, -2, -3
+PX, PY, PZ, PW, PA, PB, PC = (i << 12 for i in range(1, 8))      # aligned addresses that nothing reads
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not os.path.exists(LIB):
+        from paper_2407_02031_amd import build
+        build.build(verbose=False)
+    from paper_2407_02031_amd import binding
+    return binding
+
+
+def ln_fwd(L, x=PX, xt=0, g=PA, b=PB, y=PY, yt=0, mean=None, rstd=None, M=4, Cc=64):
+    return L.sd_layernorm_fwd(x, xt, g, b, 1e-5, y, yt, mean, rstd, M, Cc, None)
+
+
+def test_layernorm_refusals(B):
+    L = B.lib()
+    assert ln_fwd(L, x=None) == EINVAL and ln_fwd(L, y=None) == EINVAL
+    assert ln_fwd(L, x=PX + 8) == EINVAL and ln_fwd(L, g=PA + 2) == EINVAL and b"aligned" in L.sd_last_error()
+    assert ln_fwd(L, xt=2) == EINVAL and ln_fwd(L, yt=-1) == EINVAL
+    assert ln_fwd(L, M=-1) == EINVAL and ln_fwd(L, Cc=0) == EINVAL
+    assert ln_fwd(L, Cc=3) == EUNSUPPORTED and ln_fwd(L, Cc=16385) == EUNSUPPORTED
+    assert ln_fwd(L, x=None, y=None, M=0) == 0
+    bwd = lambda dy=PY, yt=0, x=PX, xt=0, mean=PA, rstd=PB, g=None, dx=PZ, dg=PC, db=PW, M=4, Cc=64, ws=1 << 20, n=1 << 20: L.sd_layernorm_bwd(
+        dy, yt, x, xt, mean, rstd, g, dx, dg, db, M, Cc, ws, n, None)
+    for k in ("dy", "x", "mean", "rstd", "dx"):
+        assert bwd(**{k: None}) == EINVAL, k
+    assert bwd(ws=None) == EWORKSPACE and bwd(n=16) == EWORKSPACE and bwd(ws=(1 << 20) + 16) == EWORKSPACE
+    assert bwd(Cc=2) == EUNSUPPORTED and bwd(xt=7) == EINVAL and bwd(dg=PC + 4) == EINVAL
+    assert L.sd_layernorm_bwd(None, 0, None, 0, None, None, None, None, None, None, 0, 64, None, 0, None) == 0
+
+
+def rope(B, **kw):
+    d = dict(D=64, pairs=(16, 16), layout=0, theta=1e4, n=None, pos=PA, stride=0, q=PX, ldq=640, hq=10, yq=PY, ldyq=640, k=PZ, ldk=640, hk=10, yk=PW, ldyk=640, t=0, Bn=2, T=5, bwd=False)
+    d.update(kw)
+    r = B.sd_rope(d["D"], len(d["pairs"]) if d["n"] is None else d["n"], (C.c_int32 * 4)(*d["pairs"][:4]), d["layout"], 0, d["theta"])
+    fn = B.lib().sd_rope_bwd if d["bwd"] else B.lib().sd_rope_fwd
+    return fn(C.byref(r), d["pos"], d["stride"], d["q"], d["ldq"], d["hq"], d["yq"], d["ldyq"], d["k"], d["ldk"], d["hk"], d["yk"], d["ldyk"], d["t"], d["Bn"], d["T"], None)
+
+
+@pytest.mark.parametrize("bwd", [False, True])
+def test_rope_refusals(B, bwd):
+    f = lambda **kw: rope(B, bwd=bwd, **kw)
+    assert f(D=63) == EUNSUPPORTED and f(D=264) == EUNSUPPORTED and f(D=0) == EUNSUPPORTED
+    assert f(n=0) == EINVAL and f(n=5) == EINVAL and f(pairs=(16, 17)) == EINVAL and f(pairs=(0, 16)) == EINVAL and f(pairs=(2 ** 31 - 1, 2 ** 31 - 1)) == EINVAL
+    assert f(layout=3) == EINVAL and f(theta=0.0) == EINVAL and f(theta=float("nan")) == EINVAL and f(t=3) == EINVAL
+    assert f(q=None) == EINVAL and f(yk=None) == EINVAL and f(pos=None) == EINVAL and f(pos=PA + 2) == EINVAL
+    assert f(q=PX + 8) == EINVAL and f(ldq=632) == EINVAL and f(ldyk=644) == EINVAL and f(stride=9) == EINVAL
+    assert f(hq=-1) == EINVAL and f(hk=257) == EINVAL and f(Bn=-1) == EINVAL and f(T=-1) == EINVAL
+    assert f(Bn=65536, T=65536) == EUNSUPPORTED
+    assert f(T=0, q=None, pos=None) == 0 and f(Bn=0) == 0 and f(hq=0, hk=0, q=None) == 0
+
+
+def test_rope_access_width(B):
+    """16 bytes where every axis and the rest of the head end at such a border."""
+    from paper_2407_02031_amd import binding
+    for kw, name in ((dict(), "rope neighbours 8"), (dict(layout=2), "rope halves 8"), (dict(layout=2, pairs=(12, 20)), "rope halves 4"), (dict(layout=1, pairs=(13, 19)), "rope halves 8"),
+                     (dict(layout=1, pairs=(13, 18)), "rope halves 1"), (dict(pairs=(13, 18)), "rope neighbours 2"), (dict(pairs=(13, 18), t=1), "rope neighbours 2"), (dict(layout=2, t=1), "rope halves 4"),
+                     (dict(layout=1, pairs=(8, 8)), "rope halves 8"), (dict(layout=1, pairs=(4, 8)), "rope halves 4")):
+        with binding.dry_run() as names:
+            assert rope(B, **kw) == 0
+        assert names == [name], kw
+
+
+def lin_fwd(L, x=PX, W=PW, bias=PB, act=1, res=None, y=PY, yt=0, z=None, M=4, N=8, K=64):
+    return L.sd_linear_fwd(x, W, bias, act, res, y, yt, z, M, N, K, None)
+
+
+def test_linear_refusals(B):
+    L = B.lib()
+    assert lin_fwd(L, x=None) == EINVAL and lin_fwd(L, W=None) == EINVAL and lin_fwd(L, y=None) == EINVAL
+    assert lin_fwd(L, y=PY + 4) == EINVAL and lin_fwd(L, z=PZ + 2) == EINVAL
+    assert lin_fwd(L, K=12) == EUNSUPPORTED and lin_fwd(L, K=0) == EUNSUPPORTED and lin_fwd(L, K=1 << 22) == EUNSUPPORTED
+    assert lin_fwd(L, act=5) == EINVAL and lin_fwd(L, act=-1) == EINVAL and lin_fwd(L, yt=2) == EINVAL and lin_fwd(L, M=-1) == EINVAL
+    assert lin_fwd(L, x=None, M=0) == 0 and lin_fwd(L, W=None, N=0) == 0
+    bwd = lambda dy=PY, yt=0, x=PX, W=PW, z=PZ, act=1, dx=PA, dW=PB, wt=0, db=PC, M=4, N=8, K=64, ws=1 << 20, n=1 << 20: L.sd_linear_bwd(
+        dy, yt, x, W, z, act, dx, dW, wt, db, M, N, K, ws, n, None)
+    assert bwd(dy=None) == EINVAL and bwd(x=None) == EINVAL and bwd(W=None) == EINVAL and bwd(z=None) == EINVAL
+    assert bwd(K=4) == EUNSUPPORTED and bwd(wt=2) == EINVAL and bwd(act=9) == EINVAL and bwd(dx=PA + 8) == EINVAL
+    assert bwd(ws=None) == EWORKSPACE and bwd(n=64) == EWORKSPACE and bwd(ws=(1 << 20) + 64) == EWORKSPACE
+    assert L.sd_linear_bwd(PY, 0, None, None, None, 0, None, None, 0, None, 4, 8, 64, None, 0, None) == 0     # nothing asked for
+    assert L.sd_linear_bwd_workspace_bytes(0, 8, 8) == 256 and L.sd_linear_bwd_workspace_bytes(100, 13, 8) >= 100 * 16 * 2 + 2 * 13 * 4
+
+
+def test_binding_refuses_what_the_c_call_cannot_see(B):
+    import torch
+    x = torch.zeros(4, 64)
+    with pytest.raises(ValueError, match="not on a GPU"):
+        B.layernorm_fwd(x)
+    with pytest.raises(TypeError):
+        B.layernorm_fwd(x.half())
+    with pytest.raises(ValueError, match="axes"):
+        B.Rope(64, [])
+    with pytest.raises(ValueError, match="shape"):
+        B._expect("x", x, (4, 65), torch.float32)
+    q = torch.zeros(2, 5, 3, 8)
+    assert B._token_rows("q", q, 8) == 24 and B._token_rows("q", q[:, :, :2], 8) == 24
+    assert B._token_rows("q", q[:1, :1], 8) == 24 and B._token_rows("q", torch.zeros(2, 1, 3, 8), 8) == 24
+    for bad in (q.transpose(1, 2), q[:, :4], q[:, ::2][:, :2], q[..., ::2]):
+        with pytest.raises(ValueError):
+            B._token_rows("q", bad, bad.shape[-1])
