@@ -348,54 +348,76 @@ def groupnorm_silu_fwd(x: torch.Tensor, gamma, beta, groups: int = 32, eps: floa
     return y
 
 
-def _expect(name: str, t: Optional[torch.Tensor], shape, *dtypes, dense: bool = True) -> None:
-    """What the C call cannot see of a tensor: its shape, type, order and device."""
+_FLOATS = (torch.bfloat16, torch.float32)
+_BF16, _F32 = (torch.bfloat16,), (torch.float32,)
+
+
+def _on(x: torch.Tensor) -> int:
+    """The GPU that x is on, which has to be the current one: kernels go to its current stream."""
+    dev = x.get_device()
+    if dev < 0:
+        raise ValueError(f"a tensor on {x.device}: not on a GPU")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"a tensor on {x.device}, the current device is {torch.cuda.current_device()}")
+    return dev
+
+
+def _raw_stream(dev: int) -> int:
+    # (torch.cuda.current_stream builds an object around this number: 2.9 us)
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _expect(name: str, t: Optional[torch.Tensor], shape, dtypes, dev: int, dense: bool = True) -> Optional[int]:
+    """The address of a tensor of which everything is as expected that the C call cannot see: shape, type, device, order."""
     if t is None:
-        return
-    if tuple(t.shape) != tuple(shape):
+        return None
+    if t.shape == shape and t.dtype in dtypes and t.get_device() == dev and (not dense or t.is_contiguous()):
+        return t.data_ptr()
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype not in dtypes:
         raise TypeError(f"{name}: {t.dtype}, expected {' or '.join(str(d) for d in dtypes)}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: not on a GPU")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name}: on {t.device}, the current device is {torch.cuda.current_device()}")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
-
-
-_FLOATS = (torch.bfloat16, torch.float32)
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on {t.device}, the others are on cuda:{dev}")
+    raise ValueError(f"{name}: not contiguous")
 
 
 def layernorm_fwd(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, out_dtype=torch.bfloat16, stats: bool = False, out=None):
     """Layer norm over the last axis of x [..., C], bf16 or fp32; y, or with `stats` (y, mean, rstd) for layernorm_bwd."""
-    Cc = x.shape[-1]
+    dev, shape = _on(x), x.shape
+    Cc = shape[-1]
     M = x.numel() // Cc if Cc else 0
-    _expect("x", x, x.shape, *_FLOATS)
-    _expect("gamma", gamma, (Cc,), torch.bfloat16)
-    _expect("beta", beta, (Cc,), torch.bfloat16)
-    _expect("out", out, x.shape, *_FLOATS)
-    y = out if out is not None else torch.empty(x.shape, dtype=out_dtype, device=x.device)
-    mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2)) if stats else (None, None)
-    _check(_lib.sd_layernorm_fwd(_ptr(x), _dt(x), _ptr(gamma), _ptr(beta), eps, _ptr(y), _dt(y), _ptr(mean), _ptr(rstd), M, Cc, _stream()))
+    px = _expect("x", x, shape, _FLOATS, dev)
+    pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
+    pb = _expect("beta", beta, (Cc,), _BF16, dev)
+    y = out if out is not None else torch.empty_like(x, dtype=out_dtype)
+    py = _expect("out", y, shape, _FLOATS, dev)
+    mean = rstd = None
+    if stats:
+        mean, rstd = x.new_empty(shape[:-1], dtype=torch.float32), x.new_empty(shape[:-1], dtype=torch.float32)
+    _check(_lib.sd_layernorm_fwd(px, _dt(x), pg, pb, eps, py, _dt(y), mean.data_ptr() if stats else None, rstd.data_ptr() if stats else None, M, Cc,
+                                 _raw_stream(dev)))
     return (y, mean, rstd) if stats else y
 
 
 def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma=None, weight_grads: bool = True, out=None, ws=None):
     """(dx, dgamma, dbeta) of layernorm_fwd, the latter two fp32, or None without `weight_grads`."""
-    Cc = x.shape[-1]
+    dev, shape = _on(x), x.shape
+    Cc = shape[-1]
     M = x.numel() // Cc if Cc else 0
-    _expect("x", x, x.shape, *_FLOATS)
-    _expect("dy", dy, x.shape, *_FLOATS)
-    _expect("mean", mean, x.shape[:-1], torch.float32)
-    _expect("rstd", rstd, x.shape[:-1], torch.float32)
-    _expect("gamma", gamma, (Cc,), torch.bfloat16)
-    _expect("out", out, x.shape, x.dtype)
+    px = _expect("x", x, shape, _FLOATS, dev)
+    pd = _expect("dy", dy, shape, _FLOATS, dev)
+    pm = _expect("mean", mean, shape[:-1], _F32, dev)
+    pr = _expect("rstd", rstd, shape[:-1], _F32, dev)
+    pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
     dx = out if out is not None else torch.empty_like(x)
-    dg, db = (torch.empty(Cc, dtype=torch.float32, device=x.device) for _ in range(2)) if weight_grads else (None, None)
-    w = _ws(_lib.sd_layernorm_bwd_workspace_bytes(M, Cc), ws) if weight_grads else None
-    _check(_lib.sd_layernorm_bwd(_ptr(dy), _dt(dy), _ptr(x), _dt(x), _ptr(mean), _ptr(rstd), _ptr(gamma), _ptr(dx), _ptr(dg), _ptr(db), M, Cc,
-                                 _ptr(w), w.numel() if w is not None else 0, _stream()))
+    po = _expect("out", dx, shape, (x.dtype,), dev)
+    dg = db = w = None
+    if weight_grads:
+        dg, db = x.new_empty((Cc,), dtype=torch.float32), x.new_empty((Cc,), dtype=torch.float32)
+        w = _ws(_lib.sd_layernorm_bwd_workspace_bytes(M, Cc), ws)
+    _check(_lib.sd_layernorm_bwd(pd, _dt(dy), px, _dt(x), pm, pr, pg, po, _ptr(dg), _ptr(db), M, Cc, _ptr(w), w.numel() if weight_grads else 0,
+                                 _raw_stream(dev)))
     return dx, dg, db
 
 
@@ -407,6 +429,7 @@ class Rope:
             raise ValueError(f"{len(axis_pairs)} axes (1 to {SD_ROPE_MAX_AXES})")
         self.head_dim, self.axis_pairs = int(head_dim), [int(n) for n in axis_pairs]
         self.c = sd_rope(self.head_dim, len(axis_pairs), (C.c_int32 * SD_ROPE_MAX_AXES)(*self.axis_pairs), layout, int(whole), float(theta))
+        self._ref = C.byref(self.c)
 
 
 def _token_rows(name: str, t: torch.Tensor, head_dim: int) -> int:
@@ -416,28 +439,36 @@ def _token_rows(name: str, t: torch.Tensor, head_dim: int) -> int:
         raise ValueError(f"{name}: head dim {D}, expected {head_dim}")
     sb, st, sh, sd = t.stride()
     ld = st if T > 1 else sb if Bn > 1 else H * D
-    if t.numel() and (sd != 1 or (H > 1 and sh != D) or (Bn > 1 and sb != T * ld)):
+    if (sd != 1 or (H > 1 and sh != D) or (Bn > 1 and sb != T * ld)) and t.numel():
         raise ValueError(f"{name}: strides {t.stride()}: rows of heads x head dim that are one distance apart, please")
     return ld
 
 
 def _rope(fn, rope: Rope, pos: torch.Tensor, q: torch.Tensor, k, q_out, k_out):
-    Bn, T = q.shape[:2]
+    dev, shape = _on(q), q.shape
+    Bn, T, hq, D = shape
     n = len(rope.axis_pairs)
-    shared = pos.dim() == 2 or (pos.dim() == 3 and pos.shape[0] == 1)
-    _expect("pos", pos, (T, n) if pos.dim() == 2 else (1 if shared else Bn, T, n), torch.float32)
-    rows = []
-    for name, t, o in (("q", q, q_out), ("k", k, k_out)):
-        if t is None:
-            rows.append((None, None, 0, 0, 0))
-            continue
-        _expect(name, t, (Bn, T, *t.shape[2:]), q.dtype, dense=False)
-        y = o if o is not None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
-        _expect(name + "_out", y, t.shape, q.dtype, dense=False)
-        rows.append((t, y, t.shape[2], _token_rows(name, t, rope.head_dim), _token_rows(name + "_out", y, rope.head_dim)))
-    (q, yq, hq, ldq, ldyq), (k, yk, hk, ldk, ldyk) = rows
-    at = lambda t: t.data_ptr() if t is not None else None
-    _check(fn(C.byref(rope.c), _ptr(pos), 0 if shared else T * n, at(q), ldq, hq, at(yq), ldyq, at(k), ldk, hk, at(yk), ldyk, _dt(q), Bn, T, _stream()))
+    if pos.dim() == 2:
+        apart, ppos = 0, _expect("pos", pos, (T, n), _F32, dev)
+    else:
+        apart = 0 if pos.shape[0] == 1 else T * n
+        ppos = _expect("pos", pos, (Bn if apart else 1, T, n), _F32, dev)
+    types = (q.dtype,)
+    pq, ldq = _expect("q", q, shape, types, dev, dense=False), _token_rows("q", q, rope.head_dim)
+    yq = q_out if q_out is not None else torch.empty(shape, dtype=q.dtype, device=q.device)
+    pyq, ldyq = _expect("q_out", yq, shape, types, dev, dense=False), hq * D
+    if q_out is not None:
+        ldyq = _token_rows("q_out", yq, D)
+    pk = pyk = yk = None
+    hk = ldk = ldyk = 0
+    if k is not None:
+        hk = k.shape[2]
+        pk, ldk = _expect("k", k, (Bn, T, hk, D), types, dev, dense=False), _token_rows("k", k, D)
+        yk = k_out if k_out is not None else torch.empty(k.shape, dtype=q.dtype, device=q.device)
+        pyk, ldyk = _expect("k_out", yk, k.shape, types, dev, dense=False), hk * D
+        if k_out is not None:
+            ldyk = _token_rows("k_out", yk, D)
+    _check(fn(rope._ref, ppos, apart, pq, ldq, hq, pyq, ldyq, pk, ldk, hk, pyk, ldyk, _dt(q), Bn, T, _raw_stream(dev)))
     return yq, yk
 
 
@@ -454,34 +485,36 @@ def rope_bwd(rope: Rope, pos: torch.Tensor, dq: torch.Tensor, dk=None, q_out=Non
 
 def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_NONE, residual=None, out_dtype=torch.bfloat16, save_z: bool = False, out=None):
     """act(x W^T + bias) + residual for x [M, K]; with `save_z` (y, z), z for linear_bwd."""
+    dev = _on(x)
     M, K = x.shape
     N = W.shape[0]
-    _expect("x", x, (M, K), torch.bfloat16)
-    _expect("W", W, (N, K), torch.bfloat16)
-    _expect("bias", bias, (N,), torch.bfloat16)
-    y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=x.device)
-    _expect("out", y, (M, N), *_FLOATS)
-    _expect("residual", residual, (M, N), y.dtype)
-    z = torch.empty((M, N), dtype=torch.bfloat16, device=x.device) if save_z else None
-    _check(_lib.sd_linear_fwd(_ptr(x), _ptr(W), _ptr(bias), act, _ptr(residual), _ptr(y), _dt(y), _ptr(z), M, N, K, _stream()))
+    px = _expect("x", x, (M, K), _BF16, dev)
+    pw = _expect("W", W, (N, K), _BF16, dev)
+    pb = _expect("bias", bias, (N,), _BF16, dev)
+    y = out if out is not None else x.new_empty((M, N), dtype=out_dtype)
+    py = _expect("out", y, (M, N), _FLOATS, dev)
+    pr = _expect("residual", residual, (M, N), (y.dtype,), dev)
+    z = x.new_empty((M, N)) if save_z else None
+    _check(_lib.sd_linear_fwd(px, pw, pb, act, pr, py, _dt(y), z.data_ptr() if save_z else None, M, N, K, _raw_stream(dev)))
     return (y, z) if save_z else y
 
 
 def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: int = SD_ACT_NONE, grads: Sequence[bool] = (True, True, True),
                dw_dtype=torch.bfloat16, ws=None):
     """(dx, dW, dbias) of linear_fwd, each None where `grads` does not ask for it."""
+    dev = _on(x)
     M, K = x.shape
     N = W.shape[0]
-    _expect("x", x, (M, K), torch.bfloat16)
-    _expect("W", W, (N, K), torch.bfloat16)
-    _expect("dy", dy, (M, N), *_FLOATS)
-    _expect("z", z, (M, N), torch.bfloat16)
-    dx = torch.empty((M, K), dtype=torch.bfloat16, device=x.device) if grads[0] else None
-    dW = torch.empty((N, K), dtype=dw_dtype, device=x.device) if grads[1] else None
-    db = torch.empty(N, dtype=torch.float32, device=x.device) if grads[2] else None
+    px = _expect("x", x, (M, K), _BF16, dev)
+    pw = _expect("W", W, (N, K), _BF16, dev)
+    pd = _expect("dy", dy, (M, N), _FLOATS, dev)
+    pz = _expect("z", z, (M, N), _BF16, dev)
+    dx = torch.empty_like(x) if grads[0] else None
+    dW = torch.empty_like(W, dtype=dw_dtype) if grads[1] else None
+    db = x.new_empty((N,), dtype=torch.float32) if grads[2] else None
     w = _ws(_lib.sd_linear_bwd_workspace_bytes(M, N, K), ws)
-    _check(_lib.sd_linear_bwd(_ptr(dy), _dt(dy), _ptr(x), _ptr(W), _ptr(z), act, _ptr(dx), _ptr(dW), _dt(dW) if dW is not None else SD_BF16, _ptr(db),
-                              M, N, K, _ptr(w), w.numel(), _stream()))
+    _check(_lib.sd_linear_bwd(pd, _dt(dy), px, pw, pz, act, _ptr(dx), _ptr(dW), _dt(dW) if dW is not None else SD_BF16, _ptr(db),
+                              M, N, K, _ptr(w), w.numel(), _raw_stream(dev)))
     return dx, dW, db
 
 

@@ -147,6 +147,16 @@ __device__ __forceinline__ void load_problem(const GemmProblem& p, ProblemRegs& 
     r.d = *reinterpret_cast<const u32x4u*>(pw + 40);
     r.e = *reinterpret_cast<const u32x4u*>(pw + 44);
 }
+__device__ __forceinline__ GemmProblem problem_of(const ProblemRegs& r) {
+    ProblemWords words;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { words.w[i] = r.a[i]; words.w[16 + i] = r.b[i]; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) words.w[32 + i] = r.c[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { words.w[40 + i] = r.d[i]; words.w[44 + i] = r.e[i]; }
+    return __builtin_bit_cast(GemmProblem, words);
+}
 __device__ __forceinline__ bool gemm_pick_tile(const GemmGroup& g, int& tile, GemmProblem& P, int& zero_n, int32_t*& zero_ptr) {
     const uint32_t* const hw = reinterpret_cast<const uint32_t*>(&g);
     u32x16u ha = *reinterpret_cast<const u32x16u*>(hw);
@@ -176,14 +186,7 @@ __device__ __forceinline__ bool gemm_pick_tile(const GemmGroup& g, int& tile, Ge
             asm volatile("" : "+s"(r.a), "+s"(r.b), "+s"(r.c), "+s"(r.d), "+s"(r.e));
         }
     }
-    ProblemWords words;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) { words.w[i] = r.a[i]; words.w[16 + i] = r.b[i]; }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) words.w[32 + i] = r.c[i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { words.w[40 + i] = r.d[i]; words.w[44 + i] = r.e[i]; }
-    P = __builtin_bit_cast(GemmProblem, words);
+    P = problem_of(r);
     return true;
 }
 

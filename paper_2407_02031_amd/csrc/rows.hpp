@@ -18,6 +18,18 @@ __device__ __forceinline__ void store4(float* p, f32x4 v) { *reinterpret_cast<f3
 __device__ __forceinline__ void store4(__bf16* p, f32x4 v) {
     *reinterpret_cast<bf16x4u*>(p) = bf16x4u{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
 }
+// eight of them
+struct f32x8 { f32x4 lo, hi; };
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+__device__ __forceinline__ f32x8 load8(const float* p) { return f32x8{load4(p), load4(p + 4)}; }
+__device__ __forceinline__ f32x8 load8(const __bf16* p) {
+    const bf16x8u v = *reinterpret_cast<const bf16x8u*>(p);
+    return f32x8{f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]}, f32x4{(float)v[4], (float)v[5], (float)v[6], (float)v[7]}};
+}
+__device__ __forceinline__ void store8(__bf16* p, const f32x8& v) {
+    *reinterpret_cast<bf16x8u*>(p) =
+        bf16x8u{(__bf16)v.lo[0], (__bf16)v.lo[1], (__bf16)v.lo[2], (__bf16)v.lo[3], (__bf16)v.hi[0], (__bf16)v.hi[1], (__bf16)v.hi[2], (__bf16)v.hi[3]};
+}
 
 // out0[c] = sum over g of partials[g][c], c < n0, and out1[c - n0] for n0 <= c < n0 + n1; rows of `partials` are n0 + n1
 // long.  In a fixed order.  An output that is null is not written.

@@ -92,17 +92,37 @@ def test_linear_refusals(B):
     assert L.sd_linear_bwd_workspace_bytes(0, 8, 8) == 256 and L.sd_linear_bwd_workspace_bytes(100, 13, 8) >= 100 * 16 * 2 + 2 * 13 * 4
 
 
+def test_linear_bwd_launches(B):
+    """Which launches a choice of gradients takes: nothing sums the parts of a product that is not wanted."""
+    L = B.lib()
+
+    def names(dx, dW, db, act=0, M=1, N=5120, K=64):
+        with B.dry_run() as n:
+            assert L.sd_linear_bwd(PY, 0, PX, PW, PZ, act, PA if dx else None, PB if dW else None, 0, PC if db else None, M, N, K, 1 << 20, 1 << 40, None) == 0
+        return n
+    gemm, guarded = ("gemm bwd 128x128/4 waves/2 stages" + g for g in ("", " guard"))
+    # one row: dx in parts, dW whole, dbias of one row block
+    assert names(1, 0, 0) == [gemm, "part sums"] and names(0, 1, 0) == [guarded] and names(0, 0, 1) == ["dz sums only"]
+    assert names(1, 1, 1) == ["dz sums only", guarded, "part sums"] and names(0, 1, 0, act=1) == ["dz no sums", guarded]
+    # many rows of few columns: dW in parts, dx whole, dbias of many row blocks
+    assert names(1, 0, 0, M=8192, N=64) == [gemm] and names(0, 1, 0, M=8192, N=64) == [gemm, "part sums"] and names(0, 0, 1, M=8192, N=64) == ["dz sums only", "part sums"]
+
+
 def test_binding_refuses_what_the_c_call_cannot_see(B):
     import torch
     x = torch.zeros(4, 64)
     with pytest.raises(ValueError, match="not on a GPU"):
         B.layernorm_fwd(x)
-    with pytest.raises(TypeError):
-        B.layernorm_fwd(x.half())
     with pytest.raises(ValueError, match="axes"):
         B.Rope(64, [])
     with pytest.raises(ValueError, match="shape"):
-        B._expect("x", x, (4, 65), torch.float32)
+        B._expect("x", x, (4, 65), (torch.float32,), -1)
+    with pytest.raises(TypeError, match="bfloat16"):
+        B._expect("x", x, (4, 64), (torch.bfloat16,), -1)
+    with pytest.raises(ValueError, match="others"):
+        B._expect("x", x, (4, 64), (torch.float32,), 0)
+    with pytest.raises(ValueError, match="contiguous"):
+        B._expect("x", x.T, (64, 4), (torch.float32,), -1)
     q = torch.zeros(2, 5, 3, 8)
     assert B._token_rows("q", q, 8) == 24 and B._token_rows("q", q[:, :, :2], 8) == 24
     assert B._token_rows("q", q[:1, :1], 8) == 24 and B._token_rows("q", torch.zeros(2, 1, 3, 8), 8) == 24
