@@ -52,8 +52,9 @@ __device__ __forceinline__ void apply_act(int kind, f32x4 (&v)[N]) {
     else if (kind == SD_ACT_RELU) each([](float z) { return z < 0.f ? 0.f : z; });
 }
 // act'(z)
-__device__ __forceinline__ float act_slope(int kind, float z) {
-    if (kind == SD_ACT_GELU) {
+template <int KIND>
+__device__ __forceinline__ float act_slope(float z) {
+    if (KIND == SD_ACT_GELU) {
         // Phi(z) + z phi(z), Phi from gelu_erf's polynomial
         const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678118654752440f, fabsf(z), 1.0f));
         float p = fmaf(1.061405429f, t, -1.453152027f);
@@ -64,15 +65,15 @@ __device__ __forceinline__ float act_slope(int kind, float z) {
         const float half = 0.5f * p * e;                  // Phi(-|z|)
         return (z < 0.f ? half : 1.f - half) + z * e * 0.39894228040143267794f;
     }
-    if (kind == SD_ACT_GELU_TANH) {
+    if (KIND == SD_ACT_GELU_TANH) {
         const float s = gelu_tanh_gate(z);
         return s + z * s * (1.f - s) * (2.f * 0.79788456080286535588f) * fmaf(3.f * 0.044715f * z, z, 1.f);
     }
-    if (kind == SD_ACT_SILU) {
+    if (KIND == SD_ACT_SILU) {
         const float s = sigmoid(z);
         return s * fmaf(z, 1.f - s, 1.f);
     }
-    if (kind == SD_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;   // (NaN stays)
+    if (KIND == SD_ACT_RELU) return z > 0.f ? 1.f : z <= 0.f ? 0.f : z;   // (NaN stays)
     return 1.f;
 }
 

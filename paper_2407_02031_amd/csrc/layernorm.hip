@@ -12,6 +12,8 @@
 // element far from all others.)
 #include "rows.hpp"
 
+#include <algorithm>
+
 namespace sd {
 
 // sums over the TPR threads of a row, in every one of them
@@ -66,65 +68,74 @@ __device__ __forceinline__ void each_chunk(int t, int C, F f) {
 }
 
 constexpr int LN_THREADS = 256;
+constexpr int ln_bwd_threads(int tpr) { return tpr > 512 ? tpr : tpr == 64 ? 512 : 256; }
 template <int TPR>
 constexpr int ln_block() { return TPR > LN_THREADS ? TPR : LN_THREADS; }
 
+// A wavefront (or workgroup) takes every `gridDim.x`-th row of its kind, and asks for the next one before it works on one: gamma and beta are
+// read once, and the loads of a row fly while the one before is reduced and stored.
 template <class X, class Y, int TPR, int J, int JW>
 __global__ __launch_bounds__(ln_block<TPR>()) void ln_fwd_kernel(const X* x, const uint16_t* __restrict__ gamma, const uint16_t* __restrict__ beta,
                                                                  float eps, Y* y, float* __restrict__ mean, float* __restrict__ rstd, int M, int C) {
     constexpr int RPB = ln_block<TPR>() / TPR;
     __shared__ float sh[TPR > 64 ? 2 * TPR / 64 : 1];
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    const int64_t stride = (int64_t)gridDim.x * RPB;
     if (row >= M) return;      // (whole wavefronts; a block of one row is never past the end)
-    const X* const xr = x + row * C;
     const __bf16* const gb = reinterpret_cast<const __bf16*>(gamma);
     const __bf16* const bb = reinterpret_cast<const __bf16*>(beta);
-    f32x4 v[J], g[J], b[J];
-    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) { v[j] = load4(xr + c.at); });
+    f32x4 next[J], v[J], g[J], b[J];
+    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) { next[j] = load4(x + row * C + c.at); });
     each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
         g[j] = gamma ? load4(gb + c.at) : f32x4{1.f, 1.f, 1.f, 1.f};
         b[j] = beta ? load4(bb + c.at) : f32x4{0.f, 0.f, 0.f, 0.f};
     });
     const float inv = 1.0f / (float)C;
-    float s[2] = {0.f, 0.f}, one[1] = {0.f};
-    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+    for (; row < M; row += stride) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) one[0] += c.on(e) ? v[j][e] : 0.f;
-    });
-    row_sums<TPR>(one, sh);
-    const float m0 = one[0] * inv;
-    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+        for (int j = 0; j < J; ++j) v[j] = next[j];
+        if (row + stride < M) each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) { next[j] = load4(x + (row + stride) * C + c.at); });
+        float s[2] = {0.f, 0.f}, one[1] = {0.f};
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[j][e] -= m0;
-            const float d = c.on(e) ? v[j][e] : 0.f;
-            s[0] += d;
-            s[1] += d * d;
-        }
-    });
-    row_sums<TPR>(s, sh);
-    const float dm = s[0] * inv;
-    float var = s[1] * inv - dm * dm;
-    var = var < 0.f ? 0.f : var;       // (NaN stays)
-    const float r = 1.0f / sqrtf(var + eps);
-    if (mean && t == 0) mean[row] = m0 + dm;
-    if (rstd && t == 0) rstd[row] = r;
-    Y* const yr = y + row * C;
-    each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
-        f32x4 o;
+            for (int e = 0; e < 4; ++e) one[0] += c.on(e) ? v[j][e] : 0.f;
+        });
+        row_sums<TPR>(one, sh);
+        const float m0 = one[0] * inv;
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (v[j][e] - dm) * r * g[j][e] + b[j][e];
-        c.store(yr, C, o);
-    });
+            for (int e = 0; e < 4; ++e) {
+                v[j][e] -= m0;
+                const float d = c.on(e) ? v[j][e] : 0.f;
+                s[0] += d;
+                s[1] += d * d;
+            }
+        });
+        row_sums<TPR>(s, sh);
+        const float dm = s[0] * inv;
+        float var = s[1] * inv - dm * dm;
+        var = var < 0.f ? 0.f : var;       // (NaN stays)
+        const float r = 1.0f / sqrtf(var + eps);
+        if (mean && t == 0) mean[row] = m0 + dm;
+        if (rstd && t == 0) rstd[row] = r;
+        Y* const yr = y + row * C;
+        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+            f32x4 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (v[j][e] - dm) * r * g[j][e] + b[j][e];
+            c.store(yr, C, o);
+        });
+    }
 }
 
-// A workgroup takes every `gridDim.x`-th group of rows, keeps the sums of its columns in registers, and leaves them in
-// partials[blockIdx.x], gradient of gamma first; sum_partials adds those up.
-template <class X, class D, int TPR, int J, int JW, bool GRADS>
-__global__ __launch_bounds__(ln_block<TPR>()) void ln_bwd_kernel(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                 const uint16_t* __restrict__ gamma, X* dx, float* __restrict__ partials, int M, int C) {
-    constexpr int RPB = ln_block<TPR>() / TPR;
+// Backward, rows: a workgroup takes every `groups`-th group of rows.  GRADS: it keeps the sums of its columns in registers and leaves them in
+// partials[group], gradient of gamma first, for sum_partials to add up.  (The next row's loads ahead of a row's work, as in the
+// forward kernel, gain nothing here: a row is two rows of loads, and the registers cost wavefronts; 8192 x 1280 bf16 17.8 us against 16.4.)
+template <class X, class D, int TPR, int J, int JW, bool GRADS, int NT>
+__device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* __restrict__ gamma,
+                                            X* dx, float* __restrict__ partials, int M, int C, int group, int groups) {
+    constexpr int RPB = NT / TPR;
     __shared__ float sh[TPR > 64 ? 2 * TPR / 64 : 1];
     __shared__ f32x4 comb[GRADS && RPB > 1 ? (RPB - 1) * 64 * 2 : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -135,7 +146,7 @@ __global__ __launch_bounds__(ln_block<TPR>()) void ln_bwd_kernel(const D* dy, co
         if (GRADS) ag[GRADS ? j : 0] = ab[GRADS ? j : 0] = f32x4{0.f, 0.f, 0.f, 0.f};
     });
     const float inv = 1.0f / (float)C;
-    for (int64_t row = (int64_t)blockIdx.x * RPB + sub; row < M; row += (int64_t)gridDim.x * RPB) {
+    for (int64_t row = (int64_t)group * RPB + sub; row < M; row += (int64_t)groups * RPB) {
         f32x4 v[J], d[J];
         each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
             v[j] = load4(x + row * C + c.at);
@@ -167,7 +178,7 @@ __global__ __launch_bounds__(ln_block<TPR>()) void ln_bwd_kernel(const D* dy, co
         });
     }
     if constexpr (GRADS) {
-        float* const out = partials + (int64_t)blockIdx.x * 2 * C;
+        float* const out = partials + (int64_t)group * 2 * C;
         each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
             if constexpr (RPB > 1) {      // the wavefronts' sums, in their order
                 __syncthreads();
@@ -188,27 +199,77 @@ __global__ __launch_bounds__(ln_block<TPR>()) void ln_bwd_kernel(const D* dy, co
         });
     }
 }
-
-// 64 columns a workgroup; 16 wavefronts take every 16th row each, and their sums are added in order.
-__global__ __launch_bounds__(1024) void sum_partials_kernel(const float* __restrict__ partials, int G, float* __restrict__ out0, int n0, float* __restrict__ out1, int n1) {
-    __shared__ float sh[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, n = n0 + n1;
-    float a = 0.f;
-    if (c < n)
-#pragma unroll 8
-        for (int g = wave; g < G; g += 16) a += partials[(int64_t)g * n + c];
-    sh[wave][lane] = a;
-    __syncthreads();
-    if (wave == 0 && c < n) {
+// ... and 16 columns' gradients from all rows, which need no row's sums: NT / 16 rows at a time, four of those in flight
+template <class X, class D, int NT>
+__device__ __forceinline__ void ln_bwd_columns(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, float* dgamma, float* dbeta, int M, int C, int block) {
+    constexpr int SUB = NT / 16, BATCH = 4;
+    __shared__ float2 sh[NT / 64 * 16];
+    const int col = block * 16 + (threadIdx.x & 15), at = min(col, C - 1);
+    float a = 0.f, b = 0.f;
+    for (int r = threadIdx.x >> 4; r < M; r += SUB * BATCH) {
+        float v[BATCH], d[BATCH], m[BATCH], s[BATCH];
 #pragma unroll
-        for (int w = 1; w < 16; ++w) a += sh[w][lane];
-        float* const out = c < n0 ? out0 : out1;
-        if (out) out[c < n0 ? c : c - n0] = a;
+        for (int i = 0; i < BATCH; ++i) {
+            const int64_t row = min(r + i * SUB, M - 1);
+            v[i] = (float)x[row * C + at];
+            d[i] = (float)dy[row * C + at];
+            m[i] = mean[row];
+            s[i] = rstd[row];
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+            if (r + i * SUB < M) {
+                a += d[i] * ((v[i] - m[i]) * s[i]);
+                b += d[i];
+            }
     }
+    a += __shfl_xor(a, 16);
+    b += __shfl_xor(b, 16);
+    a += __shfl_xor(a, 32);
+    b += __shfl_xor(b, 32);
+    if ((threadIdx.x & 63) < 16) sh[threadIdx.x / 64 * 16 + (threadIdx.x & 15)] = make_float2(a, b);
+    __syncthreads();
+    if (threadIdx.x >= 16 || col >= C) return;
+    for (int w = 1; w < NT / 64; ++w) {
+        a += sh[w * 16 + threadIdx.x].x;
+        b += sh[w * 16 + threadIdx.x].y;
+    }
+    if (dgamma) dgamma[col] = a;
+    if (dbeta) dbeta[col] = b;
+}
+template <class X, class D, int TPR, int J, int JW, bool GRADS, int NT>
+__global__ __launch_bounds__(NT) void ln_bwd_kernel(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* __restrict__ gamma,
+                                                    X* dx, float* __restrict__ partials, int M, int C) {
+    ln_bwd_rows<X, D, TPR, J, JW, GRADS, NT>(dy, x, mean, rstd, gamma, dx, partials, M, C, blockIdx.x, gridDim.x);
+}
+// Few rows: both in one launch.  The column workgroups read the rows a second time, out of the caches, which costs less than a launch.
+template <class X, class D, int TPR, int J, int JW, int NT>
+__global__ __launch_bounds__(NT) void ln_bwd_few_kernel(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* __restrict__ gamma,
+                                                        X* dx, float* dgamma, float* dbeta, int M, int C, int groups) {
+    if ((int)blockIdx.x < groups) ln_bwd_rows<X, D, TPR, J, JW, false, NT>(dy, x, mean, rstd, gamma, dx, nullptr, M, C, blockIdx.x, groups);
+    else ln_bwd_columns<X, D, NT>(dy, x, mean, rstd, dgamma, dbeta, M, C, (int)blockIdx.x - groups);
+}
+
+// 16 columns a workgroup, 32 rows at a time, so that nearly all of its loads are in flight together; the sums of a column's 32 threads are added in a fixed order.
+__global__ __launch_bounds__(512) void sum_partials_kernel(const float* __restrict__ partials, int G, float* __restrict__ out0, int n0, float* __restrict__ out1, int n1) {
+    __shared__ float sh[8][16];
+    const int n = n0 + n1, c = blockIdx.x * 16 + (threadIdx.x & 15), at = min(c, n - 1);
+    float a = 0.f;
+#pragma unroll 8
+    for (int g = threadIdx.x >> 4; g < G; g += 32) a += partials[(int64_t)g * n + at];
+    a += __shfl_xor(a, 16);
+    a += __shfl_xor(a, 32);
+    if ((threadIdx.x & 63) < 16) sh[threadIdx.x >> 6][threadIdx.x & 15] = a;
+    __syncthreads();
+    if (threadIdx.x >= 16 || c >= n) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) a += sh[w][threadIdx.x];
+    float* const out = c < n0 ? out0 : out1;
+    if (out) out[c < n0 ? c : c - n0] = a;
 }
 int launch_sum_partials(const float* partials, int G, float* out0, int n0, float* out1, int n1, hipStream_t stream) {
     if (SD_DRY_RUN("sum partials; ")) return SD_OK;
-    hipLaunchKernelGGL(sum_partials_kernel, dim3((n0 + n1 + 63) / 64), dim3(1024), 0, stream, partials, G, out0, n0, out1, n1);
+    hipLaunchKernelGGL(sum_partials_kernel, dim3((n0 + n1 + 15) / 16), dim3(512), 0, stream, partials, G, out0, n0, out1, n1);
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }
@@ -240,13 +301,21 @@ static int ln_check(const char* who, int x_dtype, int y_dtype, int M, int C) {
     return SD_OK;
 }
 
-// workgroups of the backward pass: two a CU, or one for every group of rows
-static int ln_bwd_groups(int M, int C) {
+// Workgroups of the forward pass: four a CU, or one for every group of rows where there are fewer
+static int ln_fwd_groups(int M, int C) {
     const int rpb = C > 2048 ? 1 : LN_THREADS / 64;
-    const int most = 512;
-    const int groups = M > 0 ? (M - 1) / rpb + 1 : 0;
-    return groups < most ? groups : most;
+    return std::min((M - 1) / rpb + 1, 1024);
 }
+// ... of the backward pass, eight wavefronts each.  With gradients of the weights one a CU, of short rows two: their sums of columns are written and read again (us at 128 / 256 /
+// 512 workgroups: 8192 x 1280 fp32 31.8 / 29.9 / 33.9, 2777 x 1155 bf16 17.3 / 16.4 / 21.7, 32768 x 320 51.6 / 32.3 / 26.4).  Without twice as many.
+static int ln_bwd_groups(int M, int C, bool grads) {
+    const int rpb = C > 2048 ? 1 : ln_bwd_threads(64) / 64;
+    const int groups = M > 0 ? (M - 1) / rpb + 1 : 0;
+    return std::min(groups, (C <= 768 || C > 2048 ? 512 : 256) * (grads ? 1 : 2));
+}
+// Few rows, all in one launch: what the columns read a second time lies in the caches (us, two launches / one: 3 x 950 7.4 / 3.1, 300 x 1280 10.3 / 5.1, 1000 x 640 10.1 / 6.9, 2048 x
+// 1280 15.5 / 15.9, 2777 x 1155 16.4 / 17.5).
+static bool ln_bwd_few(int M, int C) { return M <= 1024 && (int64_t)M * C <= 3 << 19; }
 
 }  // namespace sd
 
@@ -268,8 +337,8 @@ extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* 
                 using X = std::remove_pointer_t<decltype(xt)>;
                 using Y = std::remove_pointer_t<decltype(yt)>;
                 using S = decltype(shape);
-                    constexpr int B = ln_block<S::TPR>(), RPB = B / S::TPR;
-                hipLaunchKernelGGL((ln_fwd_kernel<X, Y, S::TPR, S::J, S::JW>), dim3((M - 1) / RPB + 1), dim3(B), 0, s, static_cast<const X*>(x), gamma, beta, eps,
+                    constexpr int B = ln_block<S::TPR>();
+                hipLaunchKernelGGL((ln_fwd_kernel<X, Y, S::TPR, S::J, S::JW>), dim3(ln_fwd_groups(M, C)), dim3(B), 0, s, static_cast<const X*>(x), gamma, beta, eps,
                                    static_cast<Y*>(y), mean, rstd, M, C);
                 SD_HIP_CHECK(hipGetLastError());
                 return (int)SD_OK;
@@ -280,7 +349,7 @@ extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* 
 
 extern "C" size_t sd_layernorm_bwd_workspace_bytes(int32_t M, int32_t C) {
     if (M <= 0 || C <= 0) return 256;
-    return round_up((size_t)ln_bwd_groups(M, C) * 2 * C * 4, 256);
+    return round_up((size_t)ln_bwd_groups(M, C, true) * 2 * C * 4, 256);
 }
 
 extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_dtype, const float* mean, const float* rstd, const uint16_t* gamma,
@@ -293,6 +362,8 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
                "layernorm_bwd: pointers must be 16-byte aligned");
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (M == 0) return grads ? launch_sum_partials(nullptr, 0, dgamma, C, dbeta, C, s) : SD_OK;    // sums over no rows
+    // (not in place: a row may be overwritten before a column has read it)
+    const bool few = grads && ln_bwd_few(M, C) && dx != x && dx != dy;
     float* partials = nullptr;
     if (grads) {
         Workspace w(ws, ws_bytes);
@@ -300,21 +371,24 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
         partials = static_cast<float*>(w.take(need));
         SD_REQUIRE(partials && w.ok() && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SD_EWORKSPACE, "layernorm_bwd: workspace of %zu bytes, need %zu, 256-byte aligned", ws_bytes, need);
     }
-    const int groups = ln_bwd_groups(M, C);
-    if (!SD_DRY_RUN("layernorm bwd; ")) {
+    const int groups = ln_bwd_groups(M, C, grads && !few);
+    if (!SD_DRY_RUN("layernorm bwd%s; ", few ? " few" : "")) {
         rc = by_type(x_dtype, [&](auto* xt) {
             return by_type(y_dtype, [&](auto* yt) {
                 return ln_by_length(C, [&](auto shape) {
                     using X = std::remove_pointer_t<decltype(xt)>;
                     using D = std::remove_pointer_t<decltype(yt)>;
                     using S = decltype(shape);
-                    constexpr int B = ln_block<S::TPR>();
-                    if (grads)
-                        hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, true>), dim3(groups), dim3(B), 0, s, static_cast<const D*>(dy), static_cast<const X*>(x), mean, rstd, gamma,
-                                           static_cast<X*>(dx), partials, M, C);
+                    constexpr int NT = ln_bwd_threads(S::TPR);
+                    const D* const d = static_cast<const D*>(dy);
+                    const X* const xp = static_cast<const X*>(x);
+                    X* const o = static_cast<X*>(dx);
+                    if (few)
+                        hipLaunchKernelGGL((ln_bwd_few_kernel<X, D, S::TPR, S::J, S::JW, NT>), dim3(groups + (C + 15) / 16), dim3(NT), 0, s, d, xp, mean, rstd, gamma, o, dgamma, dbeta, M, C, groups);
+                    else if (grads)
+                        hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, true, NT>), dim3(groups), dim3(NT), 0, s, d, xp, mean, rstd, gamma, o, partials, M, C);
                     else
-                        hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, false>), dim3(groups), dim3(B), 0, s, static_cast<const D*>(dy), static_cast<const X*>(x), mean, rstd, gamma,
-                                           static_cast<X*>(dx), partials, M, C);
+                        hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, false, NT>), dim3(groups), dim3(NT), 0, s, d, xp, mean, rstd, gamma, o, partials, M, C);
                     SD_HIP_CHECK(hipGetLastError());
                     return (int)SD_OK;
                 });
@@ -322,5 +396,5 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
         });
         if (rc) return rc;
     }
-    return grads ? launch_sum_partials(partials, groups, dgamma, C, dbeta, C, s) : SD_OK;
+    return grads && !few ? launch_sum_partials(partials, groups, dgamma, C, dbeta, C, s) : SD_OK;
 }

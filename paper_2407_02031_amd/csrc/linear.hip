@@ -15,90 +15,138 @@
 namespace sd {
 
 // ---------------------------------------------------------------------------------------
-// dz and its column sums.  512 columns and DZ_ROWS rows a workgroup: a lane has eight columns, a wavefront every fourth row.  The sums
-// of a workgroup's rows go to sums[row block] (of the one row block of a short dy, to the result itself).
+// dz and its column sums.  Bound by HBM (dy and z in, dz out).  CT threads have eight columns each; the NT / CT groups of them take rows in turn, four at
+// a time in flight.  The sums of a workgroup's rows go to sums[row block] (where there is one row block, to the result itself).
 // dz is rounded to bf16, which is what the matrix cores multiply (the sums are of what it was before); its rows are Np elements
 // long, N rounded up to a multiple of 8, with zeros behind N.
 // ---------------------------------------------------------------------------------------
-constexpr int DZ_ROWS = 64, DZ_COLS = 512;
-template <class D, bool STORE, bool SUMS>
-__global__ __launch_bounds__(256) void dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np) {
-    __shared__ f32x8 sh[3 * 64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int c = blockIdx.y * DZ_COLS + lane * 8;
-    const int64_t r0 = (int64_t)blockIdx.x * DZ_ROWS + wave;
-    const int64_t r1 = min((int64_t)M, ((int64_t)blockIdx.x + 1) * DZ_ROWS);
+template <class D, bool STORE, bool SUMS, int CT, int NT>
+__global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows) {
+    constexpr int SUB = NT / CT, BATCH = 4;
+    constexpr int PARTS = CT < 64 ? NT / 64 : SUB;          // sums of a column that meet in LDS
+    __shared__ f32x8 sh[PARTS > 1 ? (PARTS - 1) * CT : 1];
+    const int t = threadIdx.x % CT, sub = threadIdx.x / CT;
+    const int c = (blockIdx.y * CT + t) * 8;
+    const int64_t r0 = (int64_t)blockIdx.x * rows + sub;
+    const int64_t r1 = min((int64_t)M, ((int64_t)blockIdx.x + 1) * rows);
     const bool whole = c + 8 <= N;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     f32x8 sum = {zero, zero};
-    auto slope = [&](f32x8 g, const f32x8& v) {
-        if (z)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                g.lo[e] *= act_slope(act, v.lo[e]);
-                g.hi[e] *= act_slope(act, v.hi[e]);
-            }
-        if (SUMS) {
-            sum.lo += g.lo;
-            sum.hi += g.hi;
-        }
-        return g;
-    };
+    const __bf16* const zb = reinterpret_cast<const __bf16*>(z);
+    __bf16* const out = reinterpret_cast<__bf16*>(dz);
     // A row's last piece, where eight do not divide it, begins earlier, at N - 8: what it has in common with its neighbour's is written
     // twice, the same, and counted in the neighbour's sums alone.
     const int at = whole ? c : N - 8;
-    if (N >= 8 && c < Np) {
-#pragma unroll 4
-        for (int64_t r = r0; r < r1; r += 4) {
-            f32x8 v = {zero, zero};
-            if (z) v = load8(reinterpret_cast<const __bf16*>(z) + r * N + at);
-            const f32x8 g = slope(load8(dy + r * N + at), v);
-            if (STORE) {
-                store8(reinterpret_cast<__bf16*>(dz) + r * Np + at, g);
-                if (!whole)
-                    for (int e = N; e < Np; ++e) dz[r * Np + e] = 0;
-            }
-        }
-    } else if (c < Np) {
-        for (int64_t r = r0; r < r1; r += 4) {
-            f32x8 g = {zero, zero}, v = g;
+    auto all = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        auto slope = [&](f32x8 g, const f32x8& v) {
+            if (KIND != SD_ACT_NONE)
 #pragma unroll
-            for (int e = 0; e < 7; ++e)
-                if (e < N) {
-                    const float d = (float)dy[r * N + e], w = z ? bf16_to_f32(z[r * N + e]) : 0.f;
-                    if (e < 4) g.lo[e & 3] = d, v.lo[e & 3] = w;
-                    else g.hi[e & 3] = d, v.hi[e & 3] = w;
+                for (int e = 0; e < 4; ++e) {
+                    g.lo[e] *= act_slope<KIND>(v.lo[e]);
+                    g.hi[e] *= act_slope<KIND>(v.hi[e]);
                 }
-            g = slope(g, v);
-            if (STORE) store8(reinterpret_cast<__bf16*>(dz) + r * Np, g);
+            if (SUMS) {
+                sum.lo += g.lo;
+                sum.hi += g.hi;
+            }
+            return g;
+        };
+        if (N >= 8 && c < Np) {
+            for (int64_t r = r0; r < r1; r += SUB * BATCH) {
+                f32x8 g[BATCH], v[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int64_t o = min(r + i * SUB, r1 - 1) * N + at;
+                    g[i] = load8(dy + o);
+                    if (KIND != SD_ACT_NONE) v[i] = load8(zb + o);
+                }
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i)
+                    if (r + i * SUB < r1) {
+                        g[i] = slope(g[i], v[i]);
+                        if (STORE) store8(out + (r + i * SUB) * Np + at, g[i]);
+                    }
+            }
+        } else if (c < Np) {
+            for (int64_t r = r0; r < r1; r += SUB) {
+                f32x8 g = {zero, zero}, v = g;
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < N) {
+                        const float d = (float)dy[r * N + e], w = KIND != SD_ACT_NONE ? (float)zb[r * N + e] : 0.f;
+                        if (e < 4) g.lo[e & 3] = d, v.lo[e & 3] = w;
+                        else g.hi[e & 3] = d, v.hi[e & 3] = w;
+                    }
+                g = slope(g, v);
+                if (STORE) store8(out + r * Np, g);
+            }
         }
+    };
+    switch (act) {
+    case SD_ACT_GELU: all(std::integral_constant<int, SD_ACT_GELU>()); break;
+    case SD_ACT_GELU_TANH: all(std::integral_constant<int, SD_ACT_GELU_TANH>()); break;
+    case SD_ACT_SILU: all(std::integral_constant<int, SD_ACT_SILU>()); break;
+    case SD_ACT_RELU: all(std::integral_constant<int, SD_ACT_RELU>()); break;
+    default: all(std::integral_constant<int, SD_ACT_NONE>());
     }
+    if (STORE && N >= 8 && !whole && c < Np)
+        for (int64_t r = r0; r < r1; r += SUB)
+            for (int e = N; e < Np; ++e) dz[r * Np + e] = 0;
     if (SUMS) {
-        if (wave) sh[(wave - 1) * 64 + lane] = sum;
-        __syncthreads();
-        if (wave == 0) {
+        int part = sub;
+        if constexpr (CT < 64) {       // the rows of a wavefront
 #pragma unroll
-            for (int w = 0; w < 3; ++w) {
-                sum.lo += sh[w * 64 + lane].lo;
-                sum.hi += sh[w * 64 + lane].hi;
-            }
-            float* const out = sums + (int64_t)blockIdx.x * N + c;
-            if (whole) {
-                store4(out, sum.lo);
-                store4(out + 4, sum.hi);
-            } else {
-                const int first = N >= 8 ? N - 8 : 0;
+            for (int o = CT; o < 64; o *= 2)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (first + e >= c && first + e < N) out[first - c + e] = e < 4 ? sum.lo[e & 3] : sum.hi[e & 3];
+                for (int e = 0; e < 4; ++e) {
+                    sum.lo[e] += __shfl_xor(sum.lo[e], o);
+                    sum.hi[e] += __shfl_xor(sum.hi[e], o);
+                }
+            part = threadIdx.x >> 6;
+        }
+        if constexpr (PARTS > 1) {
+            if (part && (CT >= 64 || (threadIdx.x & 63) < CT)) sh[(part - 1) * CT + t] = sum;
+            __syncthreads();
+            if (threadIdx.x >= CT) return;
+#pragma unroll
+            for (int w = 0; w < PARTS - 1; ++w) {
+                sum.lo += sh[w * CT + t].lo;
+                sum.hi += sh[w * CT + t].hi;
             }
+        }
+        float* const to = sums + (int64_t)blockIdx.x * N + c;
+        if (whole) {
+            store4(to, sum.lo);
+            store4(to + 4, sum.hi);
+        } else {
+            const int first = N >= 8 ? N - 8 : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (first + e >= c && first + e < N) to[first - c + e] = e < 4 ? sum.lo[e & 3] : sum.hi[e & 3];
         }
     }
 }
+// How dz is cut.  Few rows: 32 columns and all rows a workgroup, so that no sums of row blocks are left.  Else 512 or 2048 columns, and as many rows as leave two
+// workgroups a CU, 8 to 32.
+struct DzCut {
+    int ct, nt, rows;
+    int64_t col_wgs, blocks;
+    DzCut(int64_t M, int64_t N) {
+        const int64_t Np = (N + 7) & ~7ll;
+        const bool few = M <= 256 || (M <= 1024 && M * N <= (1 << 20));
+        ct = few ? 4 : N > 1024 ? 256 : 64;
+        nt = few ? 1024 : 256;
+        col_wgs = (Np + ct * 8 - 1) / (ct * 8);
+        const int64_t r = M * col_wgs / 512;
+        rows = few ? 1024 : r >= 32 ? 32 : r >= 16 ? 16 : 8;
+        blocks = (M + rows - 1) / rows;
+    }
+};
 
 // ---------------------------------------------------------------------------------------
 // What is left in parts: dx, dW (as many fp32 matrices as their reductions were cut into) and dbias (a row for every
-// row block of dz), each added up in order, in one launch.  256 threads: 1024 elements of a matrix, or 64 columns of dbias.
+// row block of dz), each added up in order, in one launch.  256 threads: 1024 elements of a matrix, or 16 columns of dbias.
 // ---------------------------------------------------------------------------------------
 struct Parts {
     const float* parts;
@@ -133,19 +181,20 @@ __global__ __launch_bounds__(256) void part_sums_kernel(const PartSums a) {
         }
         wg -= a.m[i].wgs;
     }
-    __shared__ float sh[3][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = wg * 64 + lane;
+    __shared__ float sh[4][16];
+    const int c = wg * 16 + (threadIdx.x & 15), at = min(c, a.N - 1);
     float s = 0.f;
-    if (c < a.N)
 #pragma unroll 8
-        for (int b = wave; b < a.blocks; b += 4) s += a.sums[(int64_t)b * a.N + c];
-    if (wave) sh[wave - 1][lane] = s;
+    for (int b = threadIdx.x >> 4; b < a.blocks; b += 16) s += a.sums[(int64_t)b * a.N + at];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 63) < 16) sh[threadIdx.x >> 6][threadIdx.x & 15] = s;
     __syncthreads();
-    if (wave == 0 && c < a.N) a.dbias[c] = s + sh[0][lane] + sh[1][lane] + sh[2][lane];
+    if (threadIdx.x < 16 && c < a.N) a.dbias[c] = s + sh[1][threadIdx.x] + sh[2][threadIdx.x] + sh[3][threadIdx.x];
 }
 static Parts parts_of(const float* parts, void* out, bool f32, int64_t n, int count) { return Parts{parts, out, n, count, f32, (int32_t)((n / 4 + 255) / 256)}; }
 static int launch_part_sums(PartSums& a, hipStream_t stream) {
-    const int64_t wgs = (int64_t)a.m[0].wgs + a.m[1].wgs + (a.dbias ? (a.N + 63) / 64 : 0);
+    const int64_t wgs = (int64_t)a.m[0].wgs + a.m[1].wgs + (a.dbias ? (a.N + 15) / 16 : 0);
     if (wgs == 0 || SD_DRY_RUN("part sums; ")) return SD_OK;
     hipLaunchKernelGGL(part_sums_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
     SD_HIP_CHECK(hipGetLastError());
@@ -206,40 +255,91 @@ __global__ __launch_bounds__(64 * WGM * WGN, (gemm_min_waves<BM, BN, 64, WGM, WG
     else gemm_tile<BM, BN, 64, WGM, WGN, STAGES, false, GUARD, false>(P, P.tile_begin + t, lds, GemmTransposed<false, true>{});
 }
 
-// Into how many parts the reductions are cut: so that none is longer than what a workgroup's share of all steps is, two workgroups a CU,
-// but none shorter than BWD_STEPS, and no more problems than a launch holds.
-constexpr int BWD_BM = 128, BWD_BN = 128, BWD_STEPS = 4;
-// (From the sizes alone, as for both products: a gradient's bits do not depend on which others are wanted.)
+// 256x128 tiles of eight wavefronts, three stages, one workgroup a CU.  (us, both products, 128x128 tiles of four wavefronts two a CU / these: M = 8192, N = 5120,
+// K = 1280 253 / 229, 2048 x 5120 x 1280 77.3 / 75.9, 1024 x 1280 x 1280 21.4 / 21.3, 8192 x 640 x 640 34.4 / 32.6; 256x256 tiles 262, 85, 34, 47.)
+// Small ones: 64x128 tiles of four wavefronts, three stages, two workgroups a CU: where all of both products' tiles run at once, their reductions need
+// fewer cuts or none.
+constexpr int BWD_CUS = 256, BWD_PARTS = GEMM_MAX_PROBLEMS / 2;
+constexpr int BWD_BM = 256, BWD_SMALL_BM = 64, BWD_BN = 128;
+// How a product's reduction is cut: the first `whole` rows of the result not at all, the others into `parts` sums over consecutive steps, which
+// part_sums adds up.
+struct BwdCut {
+    int64_t rows, cols, steps, tiles_n, tiles;
+    int64_t whole;
+    int parts;
+    BwdCut(int64_t r, int64_t c, int64_t depth, int bm) : rows(r), cols(c), steps((depth + 63) / 64), tiles_n((c + BWD_BN - 1) / BWD_BN), tiles((r + bm - 1) / bm * tiles_n), whole(r), parts(1) {}
+    void all_in(int p) {
+        parts = p;
+        whole = p > 1 ? 0 : rows;
+    }
+    size_t bytes() const { return parts > 1 ? (size_t)parts * (rows - whole) * cols * 4 : 0; }
+};
+// From the sizes alone, as for both products: a gradient's bits do not depend on which others are wanted.
 struct BwdPlan {
-    int dx, dw;          // parts
-    BwdPlan(int64_t M, int64_t N, int64_t K) {
-        auto tiles = [](int64_t r, int64_t c) { return ((r + BWD_BM - 1) / BWD_BM) * ((c + BWD_BN - 1) / BWD_BN); };
-        const int64_t sx = (N + 63) / 64, sw = (M + 63) / 64;
-        const int64_t all = tiles(M, K) * sx + tiles(N, K) * sw;
-        const int64_t share = std::max<int64_t>(all / 512, BWD_STEPS);
-        auto parts = [&](int64_t steps) { return (int)std::min<int64_t>(std::max<int64_t>(steps / share, 1), GEMM_MAX_PROBLEMS / 2); };
-        dx = parts(sx);
-        dw = parts(sw);
+    BwdCut x, w;
+    bool small;
+    bool w_first;                  // the product of the longer sums goes first
+    static int64_t tiles(int64_t r, int64_t c, int bm) { return (r + bm - 1) / bm * ((c + BWD_BN - 1) / BWD_BN); }
+    static bool is_small(int64_t M, int64_t N, int64_t K) { return tiles(M, K, BWD_SMALL_BM) + tiles(N, K, BWD_SMALL_BM) <= 2 * BWD_CUS; }
+    BwdPlan(int64_t M, int64_t N, int64_t K) : BwdPlan(M, N, K, is_small(M, N, K)) {}
+    BwdPlan(int64_t M, int64_t N, int64_t K, bool sm) : x(M, K, N, sm ? BWD_SMALL_BM : BWD_BM), w(N, K, M, sm ? BWD_SMALL_BM : BWD_BM), small(sm) {
+        const int64_t all = x.tiles * x.steps + w.tiles * w.steps, share = (all + BWD_CUS - 1) / BWD_CUS;
+        const int64_t slots = small ? 2 * BWD_CUS : BWD_CUS, shortest = small ? 12 : 4;
+        int px = 1, pw = 1;
+        if (x.tiles + w.tiles <= slots) {
+            // one round: the longer sums are cut while CUs are idle and parts are not too short
+            for (;;) {
+                const bool xl = x.steps * pw >= w.steps * px;
+                const int p = (xl ? px : pw) + 1;
+                if (p > BWD_PARTS || (xl ? x : w).steps / p < shortest || (xl ? x.tiles * p + w.tiles * pw : x.tiles * px + w.tiles * p) > slots) break;
+                (xl ? px : pw) = p;
+            }
+        } else {
+            // several: no sum longer than a CU's share
+            px = (int)std::min<int64_t>((x.steps + share - 1) / share, BWD_PARTS);
+            pw = (int)std::min<int64_t>((w.steps + share - 1) / share, BWD_PARTS);
+        }
+        x.all_in(px);
+        w.all_in(pw);
+        w_first = w.steps * px > x.steps * pw;
+        // The other product's tiles fill up what the first one's leave; where the last of them would be a round of few, they are cut in four.  (M = 8192, N =
+        // 5120, K = 1280: 200 tiles of 128 steps, 320 of 80; the last 8 of these cut 201 us, not cut 229.)
+        BwdCut &a = w_first ? w : x, &b = w_first ? x : w;
+        if (x.tiles + w.tiles > slots && b.parts == 1 && b.steps >= 16) {
+            const int64_t an = a.tiles * a.parts, as = (a.steps + a.parts - 1) / a.parts, q = an / BWD_CUS, r = an % BWD_CUS;
+            // tiles of b that are done after d steps
+            auto done = [&](int64_t d) { return r * std::max<int64_t>((d - (q + 1) * as) / b.steps, 0) + (BWD_CUS - r) * std::max<int64_t>((d - q * as) / b.steps, 0); };
+            int64_t until = share;             // ... all of them
+            while (done(until) < b.tiles) until += std::min(b.steps - std::max<int64_t>(until - q * as, 0) % b.steps, b.steps - std::max<int64_t>(until - (q + 1) * as, 0) % b.steps);
+            const int64_t aim = share + share / 20 + 4;
+            const int64_t left = (b.tiles - std::min(done(aim), b.tiles) + b.tiles_n - 1) / b.tiles_n;     // rows of tiles
+            // a cut tile's parts are 0.5 MB written and read, 0.065 us of the chip's memory traffic each; a step takes 0.9 us
+            if (left > 0 && until > aim && left * b.tiles_n * 4 * 0.065 < (until - aim) * 0.9) {
+                b.parts = 4;
+                b.whole = std::max<int64_t>(0, (b.rows + BWD_BM - 1) / BWD_BM - left) * BWD_BM;
+            }
+        }
     }
 };
 // out [rows, cols] = P^T Q (pt) or P Q over `depth`; p [depth, rows] or [rows, depth], q [depth, cols]
-static void push_product(GemmGroup& g, bool pt, const uint16_t* p, int64_t ldp, const uint16_t* q, int64_t ldq, void* out, bool out_f32, int rows, int cols, int depth, int S, float* parts) {
-    const int steps = (depth + 63) / 64;
-    for (int i = 0; i < S; ++i) {
-        const int s0 = (int)((int64_t)steps * i / S), s1 = (int)((int64_t)steps * (i + 1) / S);
+static void push_product(GemmGroup& g, bool pt, const uint16_t* p, int64_t ldp, const uint16_t* q, int64_t ldq, void* out, bool out_f32, const BwdCut& c, int depth, float* parts) {
+    auto push = [&](int64_t row, int64_t rows, int64_t s0, int64_t s1, void* y, bool f32) {
+        if (rows <= 0) return;
         GemmProblem& P = g.p[g.n++];
-        P.p0 = p + (pt ? (int64_t)s0 * 64 * ldp : (int64_t)s0 * 64);
+        P.p0 = p + (pt ? s0 * 64 * ldp + row : row * ldp + s0 * 64);
         P.ldp0 = ldp;
-        P.q0 = q + (int64_t)s0 * 64 * ldq;
+        P.q0 = q + s0 * 64 * ldq;
         P.ldq0 = ldq;
-        P.Mp = rows;
-        P.N = cols;
-        P.K0 = std::min(depth, s1 * 64) - s0 * 64;
+        P.Mp = (int32_t)rows;
+        P.N = (int32_t)c.cols;
+        P.K0 = (int32_t)(std::min<int64_t>(depth, s1 * 64) - s0 * 64);
         P.alpha = 1.f;
-        P.ldy = cols;
-        P.y = S > 1 ? static_cast<void*>(parts + (int64_t)i * rows * cols) : out;
-        P.y_f32 = S > 1 || out_f32;
-    }
+        P.ldy = c.cols;
+        P.y = y;
+        P.y_f32 = f32;
+    };
+    push(0, c.whole, 0, c.steps, out, out_f32);
+    for (int i = 0; i < c.parts && c.parts > 1; ++i) push(c.whole, c.rows - c.whole, c.steps * i / c.parts, c.steps * (i + 1) / c.parts, parts + (size_t)i * (c.rows - c.whole) * c.cols, true);
 }
 template <int BM, int BN, int WGM, int WGN, int STAGES>
 static int launch_bwd(GemmGroup& g, int dw_from, int dw_to, bool guard, hipStream_t stream) {
@@ -362,10 +462,10 @@ struct BwdWs {
     size_t dz, sums, dx_parts, dw_parts;
     BwdWs(int64_t M, int64_t N, int64_t K) {
         dz = (size_t)M * ((N + 7) & ~7ll) * 2;
-        sums = (size_t)((M + DZ_ROWS - 1) / DZ_ROWS) * N * 4;
+        sums = (size_t)DzCut(M, N).blocks * N * 4;
         const BwdPlan p(M, N, K);
-        dx_parts = p.dx > 1 ? (size_t)p.dx * M * K * 4 : 0;
-        dw_parts = p.dw > 1 ? (size_t)p.dw * N * K * 4 : 0;
+        dx_parts = p.x.bytes();
+        dw_parts = p.w.bytes();
     }
     size_t total() const { return round_up(dz, 256) + round_up(sums, 256) + round_up(dx_parts, 256) + round_up(dw_parts, 256) + 256; }
 };
@@ -394,14 +494,19 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
     P.Mp = M; P.N = N; P.K0 = K; P.alpha = 1.f;
     if (act == SD_ACT_NONE && !z) return gemm16_takes(g) ? launch_gemm16(g, s) : launch_gemm_group(g, s);
     const GemmAct ext{z, act};
+    // The activation's tiles.  Large products: 128x256, eight wavefronts, three stages, one workgroup a CU, where they keep three CUs of four busy in every
+    // round (us with z kept, 128x128 tiles two a CU / 256x128 / these: 8192x4096x4096 309 / 235 / 223, 8192x1280x5120 126 / 126 / 121, 5120x1280x8192 112 / 95 / 93,
+    // 8192x5120x1280 115 / 118 / 117).  Others: the projections' rule.
+    const int64_t t = (int64_t)((M + 127) / 128) * ((N + 255) / 256);
+    if (!(residual && y_dtype == SD_F32) && t >= 192 && t * 4 >= (t + 255) / 256 * 256 * 3) return launch_ext<128, 256, 2, 4, 3, false>(g, K % 64 != 0, ext, s);
     const GemmChoice c = gemm_choice(g);
     switch (c.tiles) {
     case GEMM_64x64: return launch_ext<64, 64, 2, 2, 5, false>(g, c.guard, ext, s);
     case GEMM_64x128_3STAGES: return launch_act<64, 128, 2, 2, 3>(g, c, ext, s);
     case GEMM_64x128: return launch_act<64, 128, 2, 2, 2>(g, c, ext, s);
     case GEMM_128x128_ONE_ROUND: return launch_act<128, 128, 4, 2, 4>(g, c, ext, s);
-    case GEMM_256x128_ONE_ROUND: return launch_act<256, 128, 4, 2, 3>(g, c, ext, s);
-    case GEMM_256x256: return launch_ext<256, 256, 4, 2, 2, false>(g, c.guard, ext, s);
+    case GEMM_256x128_ONE_ROUND:
+    case GEMM_256x256: return launch_act<256, 128, 4, 2, 3>(g, c, ext, s);
     default: return launch_act<128, 128, 2, 2, 2>(g, c, ext, s);
     }
 }
@@ -441,22 +546,30 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
     float* const dx_parts = static_cast<float*>(w.take(b.dx_parts));
     float* const dw_parts = static_cast<float*>(w.take(b.dw_parts));
     const uint16_t* const zin = act == SD_ACT_NONE ? nullptr : z;
-    const int Np = (N + 7) & ~7, blocks = (M - 1) / DZ_ROWS + 1;
+    const int Np = (N + 7) & ~7;
+    const DzCut cut(M, N);
+    const int blocks = (int)cut.blocks;
     // dz is dy itself where nothing changes it on the way
     const bool plain = !zin && y_dtype == SD_BF16 && Np == N;
     const bool store = (dx || dW) && !plain;
     if ((store || dbias) && !SD_DRY_RUN("dz%s%s; ", store ? "" : " sums only", dbias ? "" : " no sums")) {
-        const dim3 grid((unsigned)blocks, (Np + DZ_COLS - 1) / DZ_COLS);
+        const dim3 grid((unsigned)blocks, (unsigned)cut.col_wgs);
         float* const to = blocks == 1 ? dbias : sums;
-        auto run = [&](auto* t) {
+        auto run = [&](auto* t, auto ct, auto nt) {
             using D = std::remove_pointer_t<decltype(t)>;
+            constexpr int CT = decltype(ct)::value, NT = decltype(nt)::value;
             const D* const d = static_cast<const D*>(dy);
-            if (store && dbias) hipLaunchKernelGGL((dz_kernel<D, true, true>), grid, dim3(256), 0, s, d, zin, act, dzbuf, to, M, N, Np);
-            else if (store) hipLaunchKernelGGL((dz_kernel<D, true, false>), grid, dim3(256), 0, s, d, zin, act, dzbuf, to, M, N, Np);
-            else hipLaunchKernelGGL((dz_kernel<D, false, true>), grid, dim3(256), 0, s, d, zin, act, dzbuf, to, M, N, Np);
+            if (store && dbias) hipLaunchKernelGGL((dz_kernel<D, true, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
+            else if (store) hipLaunchKernelGGL((dz_kernel<D, true, false, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
+            else hipLaunchKernelGGL((dz_kernel<D, false, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
         };
-        if (y_dtype == SD_F32) run(static_cast<float*>(nullptr));
-        else run(static_cast<__bf16*>(nullptr));
+        auto by_cut = [&](auto* t) {
+            if (cut.ct == 4) run(t, std::integral_constant<int, 4>(), std::integral_constant<int, 1024>());
+            else if (cut.ct == 64) run(t, std::integral_constant<int, 64>(), std::integral_constant<int, 256>());
+            else run(t, std::integral_constant<int, 256>(), std::integral_constant<int, 256>());
+        };
+        if (y_dtype == SD_F32) by_cut(static_cast<float*>(nullptr));
+        else by_cut(static_cast<__bf16*>(nullptr));
         SD_HIP_CHECK(hipGetLastError());
     }
     if (dbias && blocks > 1) {
@@ -469,20 +582,24 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
         const uint16_t* const dz = plain ? static_cast<const uint16_t*>(dy) : dzbuf;
         GemmGroup g;
         memset(&g, 0, sizeof(g));
-        // the longer parts first
-        const bool dw_first = dW && (!dx || ((M + 63) / 64) / plan.dw >= ((N + 63) / 64) / plan.dx);
+        const bool dw_first = dW && (!dx || plan.w_first);
         auto push_dw = [&] {
-            if (dW) push_product(g, true, dz, Np, x, K, dW, dw_dtype == SD_F32, N, K, M, plan.dw, dw_parts);
+            if (dW) push_product(g, true, dz, Np, x, K, dW, dw_dtype == SD_F32, plan.w, M, dw_parts);
         };
         if (dw_first) push_dw();
         const int dx_from = g.n;
-        if (dx) push_product(g, false, dz, Np, W, K, dx, false, M, K, N, plan.dx, dx_parts);
+        if (dx) push_product(g, false, dz, Np, W, K, dx, false, plan.x, N, dx_parts);
         const int dx_to = g.n;
         if (!dw_first) push_dw();
         const bool guard = (dW && M % 64 != 0) || (dx && N % 64 != 0);
-        if ((rc = launch_bwd<BWD_BM, BWD_BN, 2, 2, 2>(g, dw_first ? 0 : dx_to, dw_first ? dx_from : g.n, guard, s))) return rc;
-        if (dx && plan.dx > 1) left.m[0] = parts_of(dx_parts, dx, false, (int64_t)M * K, plan.dx);
-        if (dW && plan.dw > 1) left.m[1] = parts_of(dw_parts, dW, dw_dtype == SD_F32, (int64_t)N * K, plan.dw);
+        const int dw_from = dw_first ? 0 : dx_to, dw_to = dw_first ? dx_from : g.n;
+        rc = plan.small ? launch_bwd<BWD_SMALL_BM, BWD_BN, 2, 2, 3>(g, dw_from, dw_to, guard, s) : launch_bwd<BWD_BM, BWD_BN, 4, 2, 3>(g, dw_from, dw_to, guard, s);
+        if (rc) return rc;
+        auto rest = [&](const BwdCut& c, const float* parts, void* out, bool f32) {
+            return parts_of(parts, static_cast<char*>(out) + c.whole * c.cols * (f32 ? 4 : 2), f32, (c.rows - c.whole) * c.cols, c.parts);
+        };
+        if (dx && plan.x.parts > 1) left.m[0] = rest(plan.x, dx_parts, dx, false);
+        if (dW && plan.w.parts > 1) left.m[1] = rest(plan.w, dw_parts, dW, dw_dtype == SD_F32);
     }
     return launch_part_sums(left, s);
 }

@@ -28,6 +28,7 @@ struct RopeArgs {
     int32_t T, n_axes, tokens;             // tokens of a workgroup
     int32_t heads_q, heads, D, R;
     int32_t units, rot_units;              // of a head; the first of them turn
+    uint32_t by_token, by_head;            // 2^32 / (units of a token), / (units of a head), rounded up (divisors of 1 aside); the first 0 for one token a workgroup
     int32_t axis_halves;
     int32_t first[ROPE_AXES + 1];          // first pair of each axis, then R
     float sign;
@@ -47,7 +48,7 @@ __device__ __forceinline__ T& elem(typename RopeVec<T, V>::type& v, int i) { ret
 template <class T, int V, bool INTER>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(const RopeArgs a) {
     typedef typename RopeVec<T, V>::type vec;
-    __shared__ float2 table[ROPE_TABLE];
+    extern __shared__ float2 table[];
     const int64_t row0 = (int64_t)blockIdx.x * a.tokens;
     const int tokens = (int)min((int64_t)a.tokens, a.rows - row0);
     // ---- cosines and sines of the tokens' angles
@@ -71,53 +72,75 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_kernel(const RopeArgs a) {
         table[i] = make_float2(c, a.sign * s);
     }
     __syncthreads();
-    // ---- the heads
+    // ---- the heads: a thread's units are 256 apart, BATCH of them in flight together
     const int per = a.heads * a.units, n = tokens * per;
-    for (int i = threadIdx.x; i < n; i += ROPE_THREADS) {
-        const int tok = i / per, rem = i - tok * per;
-        const int head = rem / a.units, u = rem - head * a.units;
-        const bool isq = head < a.heads_q;
-        const int64_t row = row0 + tok;
-        const int h = (isq ? head : head - a.heads_q) * a.D;
-        const T* const x = static_cast<const T*>(isq ? a.q : a.k) + row * (isq ? a.ldq : a.ldk) + h;
-        T* const y = static_cast<T*>(isq ? a.yq : a.yk) + row * (isq ? a.ldyq : a.ldyk) + h;
-        const float2* const cs = table + tok * a.R;
-        if constexpr (INTER) {
-            vec v = *reinterpret_cast<const vec*>(x + u * V);
-            if (u < a.rot_units)
+    constexpr int BATCH = 4, PIECES = INTER ? 1 : 2;
+    for (int i0 = threadIdx.x; i0 < n; i0 += ROPE_THREADS * BATCH) {
+        vec v[BATCH][PIECES];
+        T* out[BATCH];
+        int lo[BATCH], hi[BATCH], at[BATCH];          // of the pieces; of the unit's first cosine, or -1
 #pragma unroll
-                for (int e = 0; e < V; e += 2) {
-                    const float2 f = cs[u * (V / 2) + e / 2];
-                    const float lo = (float)elem<T, V>(v, e), hi = (float)elem<T, V>(v, e + 1);
-                    elem<T, V>(v, e) = (T)(lo * f.x - hi * f.y);
-                    elem<T, V>(v, e + 1) = (T)(lo * f.y + hi * f.x);
-                }
-            *reinterpret_cast<vec*>(y + u * V) = v;
-        } else {
+        for (int k = 0; k < BATCH; ++k) {
+            const int i = min(i0 + k * ROPE_THREADS, n - 1);
+            const int tok = per == 1 ? i : (int)__umulhi((uint32_t)i, a.by_token), rem = i - tok * per;
+            const int head = a.units == 1 ? rem : (int)__umulhi((uint32_t)rem, a.by_head), u = rem - head * a.units;
+            const bool isq = head < a.heads_q;
+            const int64_t row = row0 + tok;
+            const int h = (isq ? head : head - a.heads_q) * a.D;
+            const T* const x = static_cast<const T*>(isq ? a.q : a.k) + row * (isq ? a.ldq : a.ldk) + h;
+            out[k] = static_cast<T*>(isq ? a.yq : a.yk) + row * (isq ? a.ldyq : a.ldyk) + h;
             const bool turn = u < a.rot_units;
-            const int p = u * V;
-            int lo = p, hi = p + a.R;
-            if (!turn) {
-                lo = 2 * a.R + (u - a.rot_units) * 2 * V;
-                hi = lo + V;
-            } else if (a.axis_halves) {
-                int ax = 0;
+            if constexpr (INTER) {
+                lo[k] = u * V;
+                hi[k] = 0;
+                at[k] = turn ? tok * a.R + u * (V / 2) : -1;
+                v[k][0] = *reinterpret_cast<const vec*>(x + lo[k]);
+            } else {
+                const int p = u * V;
+                lo[k] = p;
+                hi[k] = p + a.R;
+                if (!turn) {
+                    lo[k] = 2 * a.R + (u - a.rot_units) * 2 * V;
+                    hi[k] = lo[k] + V;
+                } else if (a.axis_halves) {
+                    int first = 0, end = a.first[1];
 #pragma unroll
-                for (int j = 1; j < ROPE_AXES; ++j) ax += p >= a.first[j] ? 1 : 0;
-                lo = a.first[ax] + p;
-                hi = lo + a.first[ax + 1] - a.first[ax];
-            }
-            vec l = *reinterpret_cast<const vec*>(x + lo), r = *reinterpret_cast<const vec*>(x + hi);
-            if (turn)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float2 f = cs[p + e];
-                    const float c = (float)elem<T, V>(l, e), d = (float)elem<T, V>(r, e);
-                    elem<T, V>(l, e) = (T)(c * f.x - d * f.y);
-                    elem<T, V>(r, e) = (T)(c * f.y + d * f.x);
+                    for (int j = 1; j < ROPE_AXES; ++j)
+                        if (p >= a.first[j]) first = a.first[j], end = a.first[j + 1];
+                    lo[k] = first + p;
+                    hi[k] = lo[k] + end - first;
                 }
-            *reinterpret_cast<vec*>(y + lo) = l;
-            *reinterpret_cast<vec*>(y + hi) = r;
+                at[k] = turn ? tok * a.R + p : -1;
+                v[k][0] = *reinterpret_cast<const vec*>(x + lo[k]);
+                v[k][PIECES - 1] = *reinterpret_cast<const vec*>(x + hi[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            if (i0 + k * ROPE_THREADS >= n) break;
+            vec &l = v[k][0], &r = v[k][PIECES - 1];
+            if (at[k] >= 0) {
+                const float2* const cs = table + at[k];
+                if constexpr (INTER) {
+#pragma unroll
+                    for (int e = 0; e < V; e += 2) {
+                        const float2 f = cs[e / 2];
+                        const float c = (float)elem<T, V>(l, e), d = (float)elem<T, V>(l, e + 1);
+                        elem<T, V>(l, e) = (T)(c * f.x - d * f.y);
+                        elem<T, V>(l, e + 1) = (T)(c * f.y + d * f.x);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float2 f = cs[e];
+                        const float c = (float)elem<T, V>(l, e), d = (float)elem<T, V>(r, e);
+                        elem<T, V>(l, e) = (T)(c * f.x - d * f.y);
+                        elem<T, V>(r, e) = (T)(c * f.y + d * f.x);
+                    }
+                }
+            }
+            *reinterpret_cast<vec*>(out[k] + lo[k]) = l;
+            if constexpr (!INTER) *reinterpret_cast<vec*>(out[k] + hi[k]) = r;
         }
     }
 }
@@ -132,7 +155,10 @@ static int launch_rope(RopeArgs& a, hipStream_t stream) {
     tokens = tokens < 1 ? 1 : tokens > ROPE_MAX_TOKENS ? ROPE_MAX_TOKENS : tokens;
     while (tokens * a.R > ROPE_TABLE) --tokens;
     a.tokens = tokens;
-    hipLaunchKernelGGL((rope_kernel<T, V, INTER>), dim3((unsigned)((a.rows - 1) / tokens + 1)), dim3(ROPE_THREADS), 0, stream, a);
+    // (exact: a unit's number times the divisor stays below 2^32)
+    a.by_token = tokens == 1 ? 0 : (uint32_t)((1ull << 32) / per + 1);
+    a.by_head = (uint32_t)((1ull << 32) / a.units + 1);
+    hipLaunchKernelGGL((rope_kernel<T, V, INTER>), dim3((unsigned)((a.rows - 1) / tokens + 1)), dim3(ROPE_THREADS), tokens * a.R * sizeof(float2), stream, a);
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }

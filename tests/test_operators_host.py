@@ -100,12 +100,16 @@ def test_linear_bwd_launches(B):
         with B.dry_run() as n:
             assert L.sd_linear_bwd(PY, 0, PX, PW, PZ, act, PA if dx else None, PB if dW else None, 0, PC if db else None, M, N, K, 1 << 20, 1 << 40, None) == 0
         return n
-    gemm, guarded = ("gemm bwd 128x128/4 waves/2 stages" + g for g in ("", " guard"))
+    gemm, guarded = ("gemm bwd 64x128/4 waves/3 stages" + g for g in ("", " guard"))
     # one row: dx in parts, dW whole, dbias of one row block
     assert names(1, 0, 0) == [gemm, "part sums"] and names(0, 1, 0) == [guarded] and names(0, 0, 1) == ["dz sums only"]
     assert names(1, 1, 1) == ["dz sums only", guarded, "part sums"] and names(0, 1, 0, act=1) == ["dz no sums", guarded]
     # many rows of few columns: dW in parts, dx whole, dbias of many row blocks
     assert names(1, 0, 0, M=8192, N=64) == [gemm] and names(0, 1, 0, M=8192, N=64) == [gemm, "part sums"] and names(0, 0, 1, M=8192, N=64) == ["dz sums only", "part sums"]
+    # large ones: dW whole, the last tiles of dx in parts; all of dW in parts
+    gemm = "gemm bwd 256x128/8 waves/3 stages"
+    assert names(1, 0, 0, M=8192, K=1280) == [gemm, "part sums"] and names(0, 1, 0, M=8192, K=1280) == [gemm]
+    assert names(0, 1, 0, M=16384, N=1280, K=1280) == [gemm, "part sums"] and names(1, 0, 0, M=16384, N=1280, K=1280) == [gemm]
 
 
 def test_binding_refuses_what_the_c_call_cannot_see(B):
