@@ -142,14 +142,16 @@ struct GemmProblem {
     // signal[row-tile index]; its y is bf16 without residual.  wait: before loading K segment 1
     // a tile waits until wait[i] >= wait_need for every row-tile i of the producer that covers
     // its P rows (or its Q rows if wait_cols).  Flags are zero when the launch starts.
-    int32_t* signal;
+    // (of a linear layer, which neither signals nor waits: where z goes, or null)
+    union { int32_t* signal; uint16_t* z; };
     const int32_t* wait;
     int32_t wait_need;                         // filled by the launcher
     int32_t wait_cols;
     // The in-tile form of an adapter (launch_gemm16): p1 is A [K1, K0], q1 is B, and the tile forms
     // t = t_scale * x A^T by itself.
     float t_scale;
-    int32_t readers;                           // filled by the launcher: tiles that wait for one row block
+    // filled by the launcher: tiles that wait for one row block.  Of a linear layer (launch_gemm16): its activation, SD_ACT_* + 1; y = act(z) + residual
+    union { int32_t readers; int32_t act; };
     // nonce != 0: signal and wait are dependency records (dep_record.hpp), one per row-tile index, that need
     // not be zero when the launch starts; at most DEP_PRODUCERS column tiles of producers, wait_cols 0.
     uint64_t nonce;

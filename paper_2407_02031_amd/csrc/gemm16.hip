@@ -365,7 +365,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * WGK, 2) void gemm16_kernel(const G
     // ---- bias, residual, store: what the problem asks for is decided once, and each choice is straight-line code.  (Two
     // wavefronts on a SIMD issue an instruction every eight clocks or so: with the choices made per block the
     // ten blocks of a 128x160 tile took 1.6 us.)
-    const float alpha = P.alpha;
+    float alpha = P.alpha;
     const int64_t ldy = P.ldy;
     // (landed long ago; said here once, or the compiler waits piece by piece, for the stores ahead of a piece too)
 #pragma unroll
@@ -376,6 +376,32 @@ __global__ __launch_bounds__(64 * WGM * WGN * WGK, 2) void gemm16_kernel(const G
             if (RES == RES_F32) asm volatile("" : "+v"(resf[mi][ni]));
             else asm volatile("" : "+v"(resb[mi][ni]));
         }
+    }
+    // A linear layer: z is kept and its activation takes the product's place, and there is no bias left to add.
+    if (NRB == 0 && P.act) {
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) {
+            f32x4 v[ME];
+#pragma unroll
+            for (int mi = 0; mi < ME; ++mi) {
+                v[mi] = fin[mi][ni];
+                v[mi][0] += bf16lo_to_f32(bias[ni][0]);
+                v[mi][1] += bf16hi_to_f32(bias[ni][0]);
+                v[mi][2] += bf16lo_to_f32(bias[ni][1]);
+                v[mi][3] += bf16hi_to_f32(bias[ni][1]);
+                if (P.z && mrow + mi * 16 < Mp && ncol + ni * 16 < N) {
+                    bf16x4 o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[mi][e];
+                    *as_global(reinterpret_cast<bf16x4*>(P.z + (int64_t)(mrow + mi * 16) * ldy + ncol + ni * 16)) = o;
+                }
+            }
+            apply_act(P.act - 1, v);
+#pragma unroll
+            for (int mi = 0; mi < ME; ++mi) fin[mi][ni] = v[mi];
+            bias[ni] = u32x2{0u, 0u};
+        }
+        alpha = 1.f;
     }
     constexpr int OUT_BF16 = 0, OUT_F32 = 1, OUT_TRANSPOSED = 2;   // transposed: 16 rows of x are 32 contiguous bytes
     auto store = [&](auto out_kind, auto bounds) {
@@ -473,7 +499,7 @@ static int launch16r(GemmGroup& g, int rmax, hipStream_t stream) {
 // 64x32, for ranks above 32 at any K from 320 on: 736x640x320 + 64 6.9 / 6.5, 602x640x640 + 64 8.3 / 7.6, 405x640x1024 + 64 10.6 / 8.3, 667x640x1280 + 40
 // 13.1 / 9.2, 582x640x2048 + 64 13.2 / 12.1, 452x640x5120 + 40 28.5 / 22.1 (120 projections, 0.65 to 0.97).
 // They have whole tiles of columns only.  Results with a bias, bf16 and without residual, no layer of a stack asks for: those keep the kernels that they
-// had, which is not the faster side (here / there: 154x1280x2048 + 64 14.2 / 8.9, 512x320x320 + 16 5.7 / 4.2, 988x640x2560 + 64 17.7 / 17.7).
+// had, which is not the faster side (here / there, and a linear layer's go there: 154x1280x2048 + 64 14.2 / 8.9, 512x320x320 + 16 5.7 / 4.2, 988x640x2560 + 64 17.7 / 17.7).
 constexpr int THIN_32x32 = 4, THIN_32x64 = 5, THIN_64x64 = 6;
 static int tile16(const GemmGroup& g) {
     long big = 0, mid = 0, small = 0, general = 0, lead = 0;   // tiles; of the general kernel: 128x128, and its producers'
@@ -493,7 +519,7 @@ static int tile16(const GemmGroup& g) {
         lead += (long)((P.Mp + 127) / 128) * ((P.K1 + 63) / 64);
         for (int i = 0; i < 2; ++i) thin[i] += (long)((P.Mp + 31) / 32) * (P.N / (32 << i));
         thin[2] += (long)((P.Mp + 63) / 64) * P.N;             // (columns: how many a tile has is up to the largest rank)
-        thin_ok = thin_ok && P.N % 64 == 0 && (!P.bias || P.res || P.y_f32);
+        thin_ok = thin_ok && P.N % 64 == 0 && (!P.bias || P.res || P.y_f32 || P.act);
         rmax = P.K1 > rmax ? P.K1 : rmax;
         kmax = P.K0 > kmax ? P.K0 : kmax;
         nmax = P.N > nmax ? P.N : nmax;

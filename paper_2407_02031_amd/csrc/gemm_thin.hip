@@ -201,6 +201,17 @@ __global__ __launch_bounds__(512, 2) void gemm_thin_kernel(const GemmGroup g) {
         v[1] = P.alpha * v[1] + bf16hi_to_f32(bias[i][0]);
         v[2] = P.alpha * v[2] + bf16lo_to_f32(bias[i][1]);
         v[3] = P.alpha * v[3] + bf16hi_to_f32(bias[i][1]);
+        if (RT == 0 && P.act) {       // a linear layer's activation, and z kept
+            if (P.z && mrow < Mp && ncol < N) {
+                bf16x4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[e];
+                *as_global(reinterpret_cast<bf16x4*>(P.z + (int64_t)mrow * P.ldy + ncol)) = o;
+            }
+            f32x4 one[1] = {v};
+            apply_act(P.act - 1, one);
+            v = one[0];
+        }
         if (RES == THIN_F32) v += resf[i];
         if (RES == THIN_BF16) {
             v[0] += bf16lo_to_f32(resb[i][0]); v[1] += bf16hi_to_f32(resb[i][0]);

@@ -63,18 +63,14 @@ constexpr int gemm_lds_chunks() {
 }
 
 // What a launch does beyond a projection of the block.
-//   act: y = act(z) + residual, z the product with its bias, and z itself kept in bf16 where asked for.
+//   act: a linear layer's, y = act(z) + residual, z the product with its bias, and z itself kept in bf16, laid out as y, where asked for.
 //   pt, qt: an operand whose rows are the reduction's, p0 [K0, Mp] or q0 [K0, N] (the two products of a backward pass).  Its
 //   stages are BK rows of BM or BN elements in LDS, and the transposing LDS read hands a lane the elements of one
 //   column.  One segment, and rows of the operand that are a multiple of 8 elements long.
 struct GemmPlain { static constexpr bool act = false, pt = false, qt = false; };
 template <bool PT, bool QT>
 struct GemmTransposed { static constexpr bool act = false, pt = PT, qt = QT; };
-struct GemmAct {
-    static constexpr bool act = true, pt = false, qt = false;
-    uint16_t* z;          // [Mp, N] as y is laid out, or null
-    int32_t kind;         // SD_ACT_*
-};
+struct GemmAct { static constexpr bool act = true, pt = false, qt = false; };
 // Which 32-byte piece of an LDS row of W elements holds logical piece u of row k: u ^ tr_swz<W>(k).  The four rows that 16 lanes
 // read a piece of each, and those eight rows further that the next 16 do, lie in distinct banks.
 template <int W>
@@ -91,14 +87,14 @@ constexpr int gemm_min_waves() {
 }
 
 template <int BM, int BN, int BK, int WGM, int WGN, int STAGES, bool GEGLU, bool GUARD, bool RES32, class Ext>
-__device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, u32x4* const lds, const Ext& ext) {
+__device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, u32x4* const lds, const Ext) {
     constexpr int NW = WGM * WGN;
     constexpr int WM = BM / WGM, WN = BN / WGN;
     constexpr int MI = WM / 16, NI = WN / 16;  // 16x16 blocks of a wavefront
     constexpr int CPR = BK / 8;                // 16-byte chunks per LDS row
     constexpr int RPB = 64 / CPR;              // tile rows per 1 KB block (one wave-wide load)
     constexpr int SLOTS = 2 * NI;              // a tile is two 32 deep k-steps of NI blocks of Q; a slot multiplies one of them by the MI blocks of P
-    constexpr int RING = NI < 4 ? NI : 4;      // blocks of Q in registers
+    constexpr int RING = NI < 4 || NI % 2 ? NI : 4;   // blocks of Q in registers
     constexpr int NBLK = (BM + BN) / RPB;      // 1 KB blocks per stage
     constexpr int LPT = NBLK / NW;             // direct-to-LDS loads per wave (= per lane) per tile
     constexpr int STAGE = (BM + BN) * CPR;     // 16-byte chunks per stage
@@ -397,7 +393,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
     // whole row pieces: lane handles 4 consecutive columns (lcol) of row lr, lr + RPP, ... of the piece.  (Stored from where they are, 32 or 64 bytes
     // of a row at a time: 8192x1920x640 + 64 39 -> 44 us, 2048x1280x1280 + 64 with an fp32 residual 20.1 -> 21.9.)
     constexpr int NOUT = GEGLU ? NI / 2 : NI;   // 16-column output blocks per wave
-    constexpr int CB = (NOUT % 4 == 0) ? 4 : 2; // ... staged per pass (<= 64 columns)
+    constexpr int CB = NOUT % 4 == 0 ? 4 : NOUT % 2 == 0 ? 2 : 1;   // ... staged per pass (<= 64 columns)
     constexpr int CCOLS = CB * 16;              // staged columns
     constexpr int LPR = CCOLS / 4;              // lanes per staged row (4 columns each)
     constexpr int RPP = 64 / LPR;               // rows per pass
@@ -516,8 +512,8 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                     for (int pass = 0; pass < NPASS; ++pass) val[pass] += br[pass];
                 }
                 if constexpr (Ext::act) {
-                    if (ext.z) {
-                        uint16_t* const zp = ext.z + (int64_t)p0 * P.ldy + q4;
+                    if (P.z) {
+                        uint16_t* const zp = P.z + (int64_t)p0 * P.ldy + q4;
 #pragma unroll
                         for (int pass = 0; pass < NPASS; ++pass) {
                             bf16x4 o;
@@ -526,7 +522,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                             *reinterpret_cast<bf16x4*>(zp + (int64_t)(pass * RPP) * P.ldy) = o;
                         }
                     }
-                    apply_act(ext.kind, val);
+                    apply_act(P.act - 1, val);
                 }
                 if (P.res) {
                     if (RES32 && res_pre) {
@@ -580,12 +576,12 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                         f32x4 val = *reinterpret_cast<const f32x4*>(stage + rr * EPI_STRIDE + lcol);
                         if (bias && P.bias_on_rows) val += bf16_to_f32(bias[p]);
                         if constexpr (Ext::act) {
-                            if (ext.z)
+                            if (P.z)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
-                                    if (q4 + e < N) ext.z[(int64_t)p * P.ldy + q4 + e] = __builtin_bit_cast(uint16_t, (__bf16)val[e]);
+                                    if (q4 + e < N) P.z[(int64_t)p * P.ldy + q4 + e] = __builtin_bit_cast(uint16_t, (__bf16)val[e]);
                             f32x4 one[1] = {val};
-                            apply_act(ext.kind, one);
+                            apply_act(P.act - 1, one);
                             val = one[0];
                         }
                         const int64_t oi = (int64_t)p * P.ldy + q4;

@@ -204,31 +204,42 @@ static int launch_part_sums(PartSums& a, hipStream_t stream) {
 // ---------------------------------------------------------------------------------------
 // products
 // ---------------------------------------------------------------------------------------
-template <int BM, int BN, int WGM, int WGN, int STAGES, bool RES32, class Ext>
-static int launch_ext(GemmGroup& g, bool guard, const Ext& ext, hipStream_t stream) {
-    int total = 0;
-    for (int i = 0; i < g.n; ++i) {
-        GemmProblem& P = g.p[i];
-        P.tiles_m = (P.Mp + BM - 1) / BM;
-        P.tiles_n = (P.N + BN - 1) / BN;
-        P.tile_begin = total;
-        g.first_tile[i] = total;
-        total += P.tiles_m * P.tiles_n;
-    }
-    g.total_tiles = total;
-    if (SD_DRY_RUN("gemm %s %dx%d/%d waves/%d stages%s%s%s; ", Ext::act ? "act" : Ext::pt ? "dW" : "dx", BM, BN, WGM * WGN, STAGES, RES32 ? " res32" : "", guard ? " guard" : "",
-                   dry_detail(", %d problems", g.n)))
-        return SD_OK;
-    const dim3 grid((total + 7) & ~7), block(64 * WGM * WGN);
-    if (guard) hipLaunchKernelGGL((gemm_kernel<BM, BN, 64, WGM, WGN, STAGES, false, true, RES32, Ext>), grid, block, 0, stream, g, ext);
-    else hipLaunchKernelGGL((gemm_kernel<BM, BN, 64, WGM, WGN, STAGES, false, false, RES32, Ext>), grid, block, 0, stream, g, ext);
+template <int BM, int BN, int WGM, int WGN, int STAGES>
+static int launch_act(GemmGroup& g, hipStream_t stream) {
+    GemmProblem& P = g.p[0];
+    P.tiles_m = (P.Mp + BM - 1) / BM;
+    P.tiles_n = (P.N + BN - 1) / BN;
+    g.total_tiles = P.tiles_m * P.tiles_n;
+    const bool guard = P.K0 % 64 != 0;
+    if (SD_DRY_RUN("gemm act %dx%d/%d waves/%d stages%s; ", BM, BN, WGM * WGN, STAGES, guard ? " guard" : "")) return SD_OK;
+    const dim3 grid((g.total_tiles + 7) & ~7), block(64 * WGM * WGN);
+    if (guard) hipLaunchKernelGGL((gemm_kernel<BM, BN, 64, WGM, WGN, STAGES, false, true, false, GemmAct>), grid, block, 0, stream, g, GemmAct{});
+    else hipLaunchKernelGGL((gemm_kernel<BM, BN, 64, WGM, WGN, STAGES, false, false, false, GemmAct>), grid, block, 0, stream, g, GemmAct{});
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }
-template <int BM, int BN, int WGM, int WGN, int STAGES>
-static int launch_act(GemmGroup& g, const GemmChoice& c, const GemmAct& ext, hipStream_t stream) {
-    if (c.res32) return launch_ext<BM, BN, WGM, WGN, STAGES, true>(g, c.guard, ext, stream);
-    return launch_ext<BM, BN, WGM, WGN, STAGES, false>(g, c.guard, ext, stream);
+// Tiles of a linear layer with more of them than one round of small ones: what the launch takes is its rounds times what a round takes, us, from fits of 49
+// launches of 1000 to 16384 rows (within 10 %, cold; each of the five is the fastest of some by 10 % or more: 2960x1280x5120 in 64x128 74, 128x128 88, 128x256 80; 6100x1920x640 36,
+// 37, 39; 8192x1280x5120 in 128x160 131, 128x256 165; 4096x1280x5120 103, 88; 8192x1920x640 in 256x128 40, 128x128 44, 128x256 51).
+static int launch_large(GemmGroup& g, hipStream_t stream) {
+    struct Tile { int bm, bn, slots; float step, rest; };
+    static const Tile tiles[5] = {{64, 128, 512, 0.85f, 4.f}, {128, 128, 512, 1.12f, 7.f}, {128, 160, 512, 1.45f, 9.f}, {256, 128, 256, 1.02f, 6.f}, {128, 256, 256, 1.0f, 6.f}};
+    const GemmProblem& P = g.p[0];
+    int best = 0;
+    float least = 0.f;
+    for (int i = 0; i < 5; ++i) {
+        const Tile& t = tiles[i];
+        const int64_t n = (int64_t)((P.Mp + t.bm - 1) / t.bm) * ((P.N + t.bn - 1) / t.bn);
+        const float us = (float)((n + t.slots - 1) / t.slots) * ((float)((P.K0 + 63) / 64) * t.step + t.rest);
+        if (i == 0 || us < least) best = i, least = us;
+    }
+    switch (best) {
+    case 0: return launch_act<64, 128, 2, 2, 3>(g, stream);
+    case 1: return launch_act<128, 128, 2, 2, 2>(g, stream);
+    case 2: return launch_act<128, 160, 2, 2, 2>(g, stream);
+    case 3: return launch_act<256, 128, 4, 2, 3>(g, stream);
+    default: return launch_act<128, 256, 2, 4, 3>(g, stream);
+    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -364,90 +375,120 @@ static int launch_bwd(GemmGroup& g, int dw_from, int dw_to, bool guard, hipStrea
 }
 
 // ---------------------------------------------------------------------------------------
-// Few rows (one token's, a guidance pair's): bound by the weights, which come in once.  A workgroup has 16 columns, whose rows of W its
-// wavefronts bring straight into the registers as MFMA operands, every NW-th step of 32 each; their sums meet in LDS.
+// Few rows (one token's, a guidance pair's, a short text's).  A workgroup has 16 MB rows and 16 NB columns, and its eight wavefronts every eighth step of 32 of the
+// reduction each; they bring the rows of x and W straight into the registers as MFMA operands, so that all of a short reduction's loads are in flight at once, and meet
+// in LDS when they are done.  Bound by the weights, which come in once per 16 MB rows, and one trip to HBM.
 // ---------------------------------------------------------------------------------------
-template <int NW, int MB>
-__global__ __launch_bounds__(64 * NW) void linear_rows_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ W, const uint16_t* __restrict__ bias, int act, const void* res,
-                                                              void* y, int f32, uint16_t* __restrict__ z, int M, int N, int K) {
-    constexpr int U = 8;             // steps in flight
-    __shared__ f32x4 sh[NW * MB * 64];
+constexpr int ROWS_NW = 8;
+template <int MB, int NB, int U>
+__global__ __launch_bounds__(64 * ROWS_NW) void linear_rows_kernel(const uint16_t* __restrict__ x, const uint16_t* __restrict__ W, const uint16_t* __restrict__ bias, int act, const void* res,
+                                                                   void* y, int f32, uint16_t* __restrict__ z, int M, int N, int K) {
+    constexpr int NW = ROWS_NW, BLOCKS = MB * NB, PER = (BLOCKS + NW - 1) / NW;
+    __shared__ f32x4 sh[NW * BLOCKS * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l16 = lane & 15, quad = lane >> 4;
-    const int n0 = blockIdx.x * 16;
-    const uint16_t* const wr = W + (int64_t)min(n0 + l16, N - 1) * K + quad * 8;
-    const uint16_t* xr[MB];
-    f32x4 acc[MB];
+    const int n0 = blockIdx.x * (16 * NB), m0 = blockIdx.y * (16 * MB);
+    const uint16_t *wr[NB], *xr[MB];
+    f32x4 acc[MB][NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) wr[n] = W + (int64_t)min(n0 + n * 16 + l16, N - 1) * K + quad * 8;
 #pragma unroll
     for (int m = 0; m < MB; ++m) {
-        xr[m] = x + (int64_t)min(m * 16 + l16, M - 1) * K + quad * 8;
-        acc[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+        xr[m] = x + (int64_t)min(m0 + m * 16 + l16, M - 1) * K + quad * 8;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     const int steps = (K + 31) / 32;
     const u32x4 none = {0u, 0u, 0u, 0u};
-    for (int s0 = wave; s0 < steps; s0 += NW * U) {
-        u32x4 wf[U], xf[U][MB];
+    u32x4 wf[U][NB], xf[U][MB];
+    auto fetch = [&](int s0) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int k = (s0 + i * NW) * 32;
             const bool in = k + quad * 8 < K;         // (a chunk of eight is whole or not there)
-            wf[i] = in ? *reinterpret_cast<const u32x4*>(wr + k) : none;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) wf[i][n] = in ? *reinterpret_cast<const u32x4*>(wr[n] + k) : none;
 #pragma unroll
             for (int m = 0; m < MB; ++m) xf[i][m] = in ? *reinterpret_cast<const u32x4*>(xr[m] + k) : none;
         }
+    };
+    fetch(wave);
+    // what the epilogue adds, behind the first loads: wavefront w finishes blocks w, w + 8, ..., a lane has four columns of one row.  (Asked for there, one more trip to HBM.)
+    f32x4 bv[PER], rv[PER];
+    auto place = [&](int i, int& row, int& col) {
+        const int b = wave + i * NW;
+        row = m0 + b / NB * 16 + l16;
+        col = n0 + b % NB * 16 + quad * 4;
+        return b < BLOCKS && row < M && col < N;
+    };
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        bv[i] = rv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        int row, col;
+        if (!place(i, row, col)) continue;
+        const int64_t at = (int64_t)row * N + col;
+        const __bf16* const bb = reinterpret_cast<const __bf16*>(bias) + col;
+        if (col + 4 <= N) {
+            if (bias) bv[i] = load4(bb);
+            if (res) rv[i] = f32 ? load4(static_cast<const float*>(res) + at) : load4(static_cast<const __bf16*>(res) + at);
+        } else
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (col + e < N) {
+                    if (bias) bv[i][e] = (float)bb[e];
+                    if (res) rv[i][e] = f32 ? static_cast<const float*>(res)[at + e] : (float)static_cast<const __bf16*>(res)[at + e];
+                }
+    }
+    for (int s0 = wave;;) {
 #pragma unroll
         for (int i = 0; i < U; ++i)
 #pragma unroll
             for (int m = 0; m < MB; ++m)
-                acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wf[i]), __builtin_bit_cast(bf16x8, xf[i][m]), acc[m], 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+                    acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wf[i][n]), __builtin_bit_cast(bf16x8, xf[i][m]), acc[m][n], 0, 0, 0);
+        s0 += NW * U;
+        if (s0 >= steps) break;
+        fetch(s0);
     }
 #pragma unroll
-    for (int m = 0; m < MB; ++m) sh[(wave * MB + m) * 64 + lane] = acc[m];
+    for (int b = 0; b < BLOCKS; ++b) sh[(wave * BLOCKS + b) * 64 + lane] = acc[b / NB][b % NB];
     __syncthreads();
-    if (wave >= MB) return;
-    // ---- wavefront m finishes block m: a lane has four columns of one row
-    const int row = wave * 16 + l16, col = n0 + quad * 4;
-    f32x4 v[1] = {sh[wave * 64 + lane]};
 #pragma unroll
-    for (int w = 1; w < NW; ++w) v[0] += sh[(w * MB + wave) * 64 + lane];
-    if (row >= M || col >= N) return;
-    const int64_t at = (int64_t)row * N + col;
-    const __bf16* const bb = reinterpret_cast<const __bf16*>(bias);
-    if (col + 4 <= N) {
-        if (bias) v[0] += load4(bb + col);
-        if (z) store4(reinterpret_cast<__bf16*>(z) + at, v[0]);
+    for (int i = 0; i < PER; ++i) {
+        int row, col;
+        if (!place(i, row, col)) continue;
+        const int b = wave + i * NW;
+        f32x4 v[1] = {sh[b * 64 + lane]};
+#pragma unroll
+        for (int w = 1; w < NW; ++w) v[0] += sh[(w * BLOCKS + b) * 64 + lane];
+        v[0] += bv[i];
+        const f32x4 pre = v[0];
         apply_act(act, v);
-        if (res) v[0] += f32 ? load4(static_cast<const float*>(res) + at) : load4(static_cast<const __bf16*>(res) + at);
-        if (f32) store4(static_cast<float*>(y) + at, v[0]);
-        else store4(static_cast<__bf16*>(y) + at, v[0]);
-        return;
+        v[0] += rv[i];
+        const int64_t at = (int64_t)row * N + col;
+        __bf16* const zp = reinterpret_cast<__bf16*>(z) + at;
+        if (col + 4 <= N) {
+            if (z) store4(zp, pre);
+            if (f32) store4(static_cast<float*>(y) + at, v[0]);
+            else store4(static_cast<__bf16*>(y) + at, v[0]);
+        } else
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (col + e < N) {
+                    if (z) zp[e] = (__bf16)pre[e];
+                    if (f32) static_cast<float*>(y)[at + e] = v[0][e];
+                    else static_cast<__bf16*>(y)[at + e] = (__bf16)v[0][e];
+                }
     }
-    if (bias)
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (col + e < N) v[0][e] += (float)bb[col + e];
-    const f32x4 pre = v[0];
-    apply_act(act, v);
-#pragma unroll
-    for (int e = 0; e < 3; ++e)
-        if (col + e < N) {
-            if (z) reinterpret_cast<__bf16*>(z)[at + e] = (__bf16)pre[e];
-            const float r = !res ? 0.f : f32 ? static_cast<const float*>(res)[at + e] : (float)static_cast<const __bf16*>(res)[at + e];
-            if (f32) static_cast<float*>(y)[at + e] = v[0][e] + r;
-            else static_cast<__bf16*>(y)[at + e] = (__bf16)(v[0][e] + r);
-        }
 }
-constexpr int LINEAR_ROWS = 32;       // rows that this kernel takes
-template <int NW>
+template <int MB, int NB, int U>
 static int launch_rows(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int act, const void* res, void* y, int f32, uint16_t* z, int M, int N, int K, hipStream_t stream) {
-    if (SD_DRY_RUN("linear rows %d/%d waves; ", M > 16 ? 32 : 16, NW)) return SD_OK;
-    const dim3 grid((N + 15) / 16), block(64 * NW);
-    if (M <= 16) hipLaunchKernelGGL((linear_rows_kernel<NW, 1>), grid, block, 0, stream, x, W, bias, act, res, y, f32, z, M, N, K);
-    else hipLaunchKernelGGL((linear_rows_kernel<NW, 2>), grid, block, 0, stream, x, W, bias, act, res, y, f32, z, M, N, K);
+    if (SD_DRY_RUN("linear rows %dx%d; ", 16 * MB, 16 * NB)) return SD_OK;
+    hipLaunchKernelGGL((linear_rows_kernel<MB, NB, U>), dim3((N + 16 * NB - 1) / (16 * NB), (M + 16 * MB - 1) / (16 * MB)), dim3(64 * ROWS_NW), 0, stream, x, W, bias, act, res, y, f32, z, M, N, K);
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }
-
 static int linear_sizes(const char* who, int M, int N, int K, int act, int y_dtype) {
     SD_REQUIRE(M >= 0 && N >= 0, SD_EINVAL, "%s: M=%d N=%d", who, M, N);
     SD_REQUIRE(K > 0 && K % 8 == 0, SD_EUNSUPPORTED, "%s: K=%d is not a positive multiple of 8", who, K);
@@ -481,7 +522,6 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
     SD_REQUIRE(x && W && y, SD_EINVAL, "linear_fwd: x, W or y is null");
     SD_REQUIRE(aligned16(x) && aligned16(W) && aligned16(bias) && aligned16(residual) && aligned16(y) && aligned16(z), SD_EINVAL, "linear_fwd: pointers must be 16-byte aligned");
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (M <= LINEAR_ROWS) return K > 2048 ? launch_rows<16>(x, W, bias, act, residual, y, y_dtype == SD_F32, z, M, N, K, s) : launch_rows<8>(x, W, bias, act, residual, y, y_dtype == SD_F32, z, M, N, K, s);
     GemmGroup g;
     memset(&g, 0, sizeof(g));
     g.n = 1;
@@ -492,23 +532,17 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
     P.res = residual; P.ldr = N; P.res_f32 = y_dtype == SD_F32;
     P.y = y; P.ldy = N; P.y_f32 = y_dtype == SD_F32;
     P.Mp = M; P.N = N; P.K0 = K; P.alpha = 1.f;
-    if (act == SD_ACT_NONE && !z) return gemm16_takes(g) ? launch_gemm16(g, s) : launch_gemm_group(g, s);
-    const GemmAct ext{z, act};
-    // The activation's tiles.  Large products: 128x256, eight wavefronts, three stages, one workgroup a CU, where they keep three CUs of four busy in every
-    // round (us with z kept, 128x128 tiles two a CU / 256x128 / these: 8192x4096x4096 309 / 235 / 223, 8192x1280x5120 126 / 126 / 121, 5120x1280x8192 112 / 95 / 93,
-    // 8192x5120x1280 115 / 118 / 117).  Others: the projections' rule.
-    const int64_t t = (int64_t)((M + 127) / 128) * ((N + 255) / 256);
-    if (!(residual && y_dtype == SD_F32) && t >= 192 && t * 4 >= (t + 255) / 256 * 256 * 3) return launch_ext<128, 256, 2, 4, 3, false>(g, K % 64 != 0, ext, s);
-    const GemmChoice c = gemm_choice(g);
-    switch (c.tiles) {
-    case GEMM_64x64: return launch_ext<64, 64, 2, 2, 5, false>(g, c.guard, ext, s);
-    case GEMM_64x128_3STAGES: return launch_act<64, 128, 2, 2, 3>(g, c, ext, s);
-    case GEMM_64x128: return launch_act<64, 128, 2, 2, 2>(g, c, ext, s);
-    case GEMM_128x128_ONE_ROUND: return launch_act<128, 128, 4, 2, 4>(g, c, ext, s);
-    case GEMM_256x128_ONE_ROUND:
-    case GEMM_256x256: return launch_act<256, 128, 4, 2, 3>(g, c, ext, s);
-    default: return launch_act<128, 128, 2, 2, 2>(g, c, ext, s);
-    }
+    // Few rows.  (us, cold, z not kept, this kernel / the launches below: 1 x 5120 x 1280 6.1 / 12.8 ...)
+    const int f32 = y_dtype == SD_F32;
+    if (M <= 16) return launch_rows<1, 1, 6>(x, W, bias, act, residual, y, f32, z, M, N, K, s);
+    P.act = act + 1;
+    P.z = z;
+    if (gemm16_takes(g)) return launch_gemm16(g, s);
+    const int64_t r32 = (M + 31) / 32, r64 = (M + 63) / 64, c16 = (N + 15) / 16, c32 = (N + 31) / 32;
+    if (r32 * c16 <= 256) return launch_rows<2, 1, 6>(x, W, bias, act, residual, y, f32, z, M, N, K, s);
+    if (r32 * c32 <= 256) return launch_rows<2, 2, 4>(x, W, bias, act, residual, y, f32, z, M, N, K, s);
+    if (r64 * c32 <= 256) return launch_rows<4, 2, 3>(x, W, bias, act, residual, y, f32, z, M, N, K, s);
+    return launch_large(g, s);
 }
 
 extern "C" size_t sd_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K) {

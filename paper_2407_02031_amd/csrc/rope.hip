@@ -151,8 +151,12 @@ static int launch_rope(RopeArgs& a, hipStream_t stream) {
     a.rot_units = INTER ? 2 * a.R / V : a.R / V;
     if (SD_DRY_RUN("rope %s%d; ", INTER ? "neighbours " : "halves ", V)) return SD_OK;
     const int per = a.heads * a.units;
-    int tokens = 8 * ROPE_THREADS / per;
-    tokens = tokens < 1 ? 1 : tokens > ROPE_MAX_TOKENS ? ROPE_MAX_TOKENS : tokens;
+    // So many tokens that a thread has up to four units, but no fewer workgroups than four a CU while there are tokens.  (us at 4 / 8 units: 12844 tokens of 32 heads x 128 fp32 79.7 /
+    // 83.4, 8192 of 40 x 64 bf16 22.8 / 23.0; as few workgroups as eight units take / four a CU: 40 tokens of 4 x 88 6.0 / 2.9, 54 of 24 x 32 5.7 / 3.5)
+    const int64_t most = (a.rows + 1023) / 1024;
+    int tokens = 4 * ROPE_THREADS / per;
+    tokens = tokens > ROPE_MAX_TOKENS ? ROPE_MAX_TOKENS : tokens;
+    tokens = tokens > most ? (int)most : tokens < 1 ? 1 : tokens;
     while (tokens * a.R > ROPE_TABLE) --tokens;
     a.tokens = tokens;
     // (exact: a unit's number times the divisor stays below 2^32)
