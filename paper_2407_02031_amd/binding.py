@@ -382,6 +382,14 @@ def _expect(name: str, t: Optional[torch.Tensor], shape, dtypes, dev: int, dense
     raise ValueError(f"{name}: not contiguous")
 
 
+def _scratch(x: torch.Tensor, nbytes: int, ws: Optional[torch.Tensor], dev: int):
+    """A workspace beside x, its address and its size; or the caller's."""
+    if ws is None:
+        w = x.new_empty((nbytes,), dtype=torch.uint8)
+        return w, w.data_ptr(), nbytes
+    return ws, _expect("ws", ws, (ws.numel(),), (torch.uint8,), dev), ws.numel()
+
+
 def layernorm_fwd(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, out_dtype=torch.bfloat16, stats: bool = False, out=None):
     """Layer norm over the last axis of x [..., C], bf16 or fp32; y, or with `stats` (y, mean, rstd) for layernorm_bwd."""
     dev, shape = _on(x), x.shape
@@ -390,13 +398,16 @@ def layernorm_fwd(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, out
     px = _expect("x", x, shape, _FLOATS, dev)
     pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
     pb = _expect("beta", beta, (Cc,), _BF16, dev)
-    y = out if out is not None else torch.empty_like(x, dtype=out_dtype)
-    py = _expect("out", y, shape, _FLOATS, dev)
-    mean = rstd = None
+    if out is None:
+        y = torch.empty_like(x, dtype=out_dtype)
+        py = y.data_ptr()
+    else:
+        y, py = out, _expect("out", out, shape, _FLOATS, dev)
+    mean = rstd = pm = pr = None
     if stats:
         mean, rstd = x.new_empty(shape[:-1], dtype=torch.float32), x.new_empty(shape[:-1], dtype=torch.float32)
-    _check(_lib.sd_layernorm_fwd(px, _dt(x), pg, pb, eps, py, _dt(y), mean.data_ptr() if stats else None, rstd.data_ptr() if stats else None, M, Cc,
-                                 _raw_stream(dev)))
+        pm, pr = mean.data_ptr(), rstd.data_ptr()
+    _check(_lib.sd_layernorm_fwd(px, _dt(x), pg, pb, eps, py, _dt(y), pm, pr, M, Cc, _raw_stream(dev)))
     return (y, mean, rstd) if stats else y
 
 
@@ -410,14 +421,18 @@ def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: t
     pm = _expect("mean", mean, shape[:-1], _F32, dev)
     pr = _expect("rstd", rstd, shape[:-1], _F32, dev)
     pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
-    dx = out if out is not None else torch.empty_like(x)
-    po = _expect("out", dx, shape, (x.dtype,), dev)
-    dg = db = w = None
+    if out is None:
+        dx = torch.empty_like(x)
+        po = dx.data_ptr()
+    else:
+        dx, po = out, _expect("out", out, shape, (x.dtype,), dev)
+    dg = db = pdg = pdb = pw = None
+    nw = 0
     if weight_grads:
         dg, db = x.new_empty((Cc,), dtype=torch.float32), x.new_empty((Cc,), dtype=torch.float32)
-        w = _ws(_lib.sd_layernorm_bwd_workspace_bytes(M, Cc), ws)
-    _check(_lib.sd_layernorm_bwd(pd, _dt(dy), px, _dt(x), pm, pr, pg, po, _ptr(dg), _ptr(db), M, Cc, _ptr(w), w.numel() if weight_grads else 0,
-                                 _raw_stream(dev)))
+        pdg, pdb = dg.data_ptr(), db.data_ptr()
+        w, pw, nw = _scratch(x, _lib.sd_layernorm_bwd_workspace_bytes(M, Cc), ws, dev)
+    _check(_lib.sd_layernorm_bwd(pd, _dt(dy), px, _dt(x), pm, pr, pg, po, pdg, pdb, M, Cc, pw, nw, _raw_stream(dev)))
     return dx, dg, db
 
 
@@ -437,6 +452,8 @@ def _token_rows(name: str, t: torch.Tensor, head_dim: int) -> int:
     Bn, T, H, D = t.shape
     if D != head_dim:
         raise ValueError(f"{name}: head dim {D}, expected {head_dim}")
+    if t.is_contiguous():
+        return H * D
     sb, st, sh, sd = t.stride()
     ld = st if T > 1 else sb if Bn > 1 else H * D
     if (sd != 1 or (H > 1 and sh != D) or (Bn > 1 and sb != T * ld)) and t.numel():
@@ -454,20 +471,21 @@ def _rope(fn, rope: Rope, pos: torch.Tensor, q: torch.Tensor, k, q_out, k_out):
         apart = 0 if pos.shape[0] == 1 else T * n
         ppos = _expect("pos", pos, (Bn if apart else 1, T, n), _F32, dev)
     types = (q.dtype,)
-    pq, ldq = _expect("q", q, shape, types, dev, dense=False), _token_rows("q", q, rope.head_dim)
-    yq = q_out if q_out is not None else torch.empty(shape, dtype=q.dtype, device=q.device)
-    pyq, ldyq = _expect("q_out", yq, shape, types, dev, dense=False), hq * D
-    if q_out is not None:
-        ldyq = _token_rows("q_out", yq, D)
+
+    def place(name, t, shape, out):
+        p, ld = _expect(name, t, shape, types, dev, dense=False), _token_rows(name, t, D)
+        if out is None:
+            y = t.new_empty(shape)
+            return p, ld, y, y.data_ptr(), shape[2] * D
+        return p, ld, out, _expect(name + "_out", out, shape, types, dev, dense=False), _token_rows(name + "_out", out, D)
+    if D != rope.head_dim:
+        raise ValueError(f"q: head dim {D}, expected {rope.head_dim}")
+    pq, ldq, yq, pyq, ldyq = place("q", q, shape, q_out)
     pk = pyk = yk = None
     hk = ldk = ldyk = 0
     if k is not None:
         hk = k.shape[2]
-        pk, ldk = _expect("k", k, (Bn, T, hk, D), types, dev, dense=False), _token_rows("k", k, D)
-        yk = k_out if k_out is not None else torch.empty(k.shape, dtype=q.dtype, device=q.device)
-        pyk, ldyk = _expect("k_out", yk, k.shape, types, dev, dense=False), hk * D
-        if k_out is not None:
-            ldyk = _token_rows("k_out", yk, D)
+        pk, ldk, yk, pyk, ldyk = place("k", k, (Bn, T, hk, D), k_out)
     _check(fn(rope._ref, ppos, apart, pq, ldq, hq, pyq, ldyq, pk, ldk, hk, pyk, ldyk, _dt(q), Bn, T, _raw_stream(dev)))
     return yq, yk
 
@@ -491,8 +509,11 @@ def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_NO
     px = _expect("x", x, (M, K), _BF16, dev)
     pw = _expect("W", W, (N, K), _BF16, dev)
     pb = _expect("bias", bias, (N,), _BF16, dev)
-    y = out if out is not None else x.new_empty((M, N), dtype=out_dtype)
-    py = _expect("out", y, (M, N), _FLOATS, dev)
+    if out is None:
+        y = x.new_empty((M, N), dtype=out_dtype)
+        py = y.data_ptr()
+    else:
+        y, py = out, _expect("out", out, (M, N), _FLOATS, dev)
     pr = _expect("residual", residual, (M, N), (y.dtype,), dev)
     z = x.new_empty((M, N)) if save_z else None
     _check(_lib.sd_linear_fwd(px, pw, pb, act, pr, py, _dt(y), z.data_ptr() if save_z else None, M, N, K, _raw_stream(dev)))
@@ -512,9 +533,9 @@ def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: 
     dx = torch.empty_like(x) if grads[0] else None
     dW = torch.empty_like(W, dtype=dw_dtype) if grads[1] else None
     db = x.new_empty((N,), dtype=torch.float32) if grads[2] else None
-    w = _ws(_lib.sd_linear_bwd_workspace_bytes(M, N, K), ws)
-    _check(_lib.sd_linear_bwd(pd, _dt(dy), px, pw, pz, act, _ptr(dx), _ptr(dW), _dt(dW) if dW is not None else SD_BF16, _ptr(db),
-                              M, N, K, _ptr(w), w.numel(), _raw_stream(dev)))
+    w, pws, nws = _scratch(x, _lib.sd_linear_bwd_workspace_bytes(M, N, K), ws, dev)
+    _check(_lib.sd_linear_bwd(pd, _dt(dy), px, pw, pz, act, dx.data_ptr() if grads[0] else None, dW.data_ptr() if grads[1] else None,
+                              _dt(dW) if grads[1] else SD_BF16, db.data_ptr() if grads[2] else None, M, N, K, pws, nws, _raw_stream(dev)))
     return dx, dW, db
 
 
