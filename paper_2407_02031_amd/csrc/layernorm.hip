@@ -20,20 +20,23 @@ namespace sd {
 template <int TPR, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* sh) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+    for (int i = 0; i < N; ++i) {
+        if constexpr (TPR == 16) v[i] = dpp_add(dpp_add(dpp_add(dpp_add(v[i], 0), 1), 2), 3);
+        else v[i] = wave_sum(v[i]);
+    }
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
-        const int wave = threadIdx.x >> 6;
+        const int first = threadIdx.x / TPR * W, wave = threadIdx.x >> 6;      // (of this row's wavefronts)
         __syncthreads();                   // the last sums have been read
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
-            for (int i = 0; i < N; ++i) sh[i * W + wave] = v[i];
+            for (int i = 0; i < N; ++i) sh[i * 16 + wave] = v[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             v[i] = 0.f;
 #pragma unroll
-            for (int w = 0; w < W; ++w) v[i] += sh[i * W + w];
+            for (int w = 0; w < W; ++w) v[i] += sh[i * 16 + first + w];
         }
     }
 }
@@ -68,7 +71,7 @@ __device__ __forceinline__ void each_chunk(int t, int C, F f) {
 }
 
 constexpr int LN_THREADS = 256;
-constexpr int ln_bwd_threads(int tpr) { return tpr > 512 ? tpr : tpr == 64 ? 512 : 256; }
+constexpr int ln_bwd_threads(int tpr) { return tpr > 512 ? tpr : 512; }
 template <int TPR>
 constexpr int ln_block() { return TPR > LN_THREADS ? TPR : LN_THREADS; }
 
@@ -78,7 +81,7 @@ template <class X, class Y, int TPR, int J, int JW>
 __global__ __launch_bounds__(ln_block<TPR>()) void ln_fwd_kernel(const X* x, const uint16_t* __restrict__ gamma, const uint16_t* __restrict__ beta,
                                                                  float eps, Y* y, float* __restrict__ mean, float* __restrict__ rstd, int M, int C) {
     constexpr int RPB = ln_block<TPR>() / TPR;
-    __shared__ float sh[TPR > 64 ? 2 * TPR / 64 : 1];
+    __shared__ float sh[TPR > 64 ? 32 : 1];
     const int t = threadIdx.x % TPR;
     int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
     const int64_t stride = (int64_t)gridDim.x * RPB;
@@ -136,8 +139,9 @@ template <class X, class D, int TPR, int J, int JW, bool GRADS, int NT>
 __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* __restrict__ gamma,
                                             X* dx, float* __restrict__ partials, int M, int C, int group, int groups) {
     constexpr int RPB = NT / TPR;
-    __shared__ float sh[TPR > 64 ? 2 * TPR / 64 : 1];
-    __shared__ f32x4 comb[GRADS && RPB > 1 ? (RPB - 1) * 64 * 2 : 1];
+    __shared__ float sh[TPR > 64 ? 32 : 1];
+    constexpr int SETS = TPR < 64 ? NT / 64 : RPB;          // sums of a column that meet in LDS
+    __shared__ f32x4 comb[GRADS && SETS > 1 ? (SETS - 1) * TPR * 2 : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const __bf16* const gb = reinterpret_cast<const __bf16*>(gamma);
     f32x4 g[J], ag[GRADS ? J : 1], ab[GRADS ? J : 1];
@@ -146,7 +150,11 @@ __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float
         if (GRADS) ag[GRADS ? j : 0] = ab[GRADS ? j : 0] = f32x4{0.f, 0.f, 0.f, 0.f};
     });
     const float inv = 1.0f / (float)C;
-    for (int64_t row = (int64_t)group * RPB + sub; row < M; row += (int64_t)groups * RPB) {
+    for (int64_t row0 = (int64_t)group * RPB; row0 < M; row0 += (int64_t)groups * RPB) {
+        // (a row past the end works on the last one, and neither adds nor stores: rows of several wavefronts meet at barriers)
+        const int64_t row = min(row0 + sub, (int64_t)M - 1);
+        const bool mine = row0 + sub < M;
+        if (TPR <= 64 && !mine) break;
         f32x4 v[J], d[J];
         each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
             v[j] = load4(x + row * C + c.at);
@@ -159,7 +167,7 @@ __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float
             for (int e = 0; e < 4; ++e) {
                 const float dd = c.on(e) ? d[j][e] : 0.f;
                 v[j][e] = c.on(e) ? (v[j][e] - m) * r : 0.f;
-                if (GRADS) {
+                if (GRADS && (TPR <= 64 || mine)) {
                     ag[GRADS ? j : 0][e] += dd * v[j][e];
                     ab[GRADS ? j : 0][e] += dd;
                 }
@@ -170,30 +178,46 @@ __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float
         });
         row_sums<TPR>(s, sh);
         const float c1 = s[0] * inv, c2 = s[1] * inv;
-        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
-            f32x4 o;
+        if (TPR <= 64 || mine)
+            each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
+                f32x4 o;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = r * (d[j][e] - c1 - v[j][e] * c2);
-            c.store(dx + row * C, C, o);
-        });
+                for (int e = 0; e < 4; ++e) o[e] = r * (d[j][e] - c1 - v[j][e] * c2);
+                c.store(dx + row * C, C, o);
+            });
     }
     if constexpr (GRADS) {
         float* const out = partials + (int64_t)group * 2 * C;
+        int set = sub;
+        bool lead = true;            // of the threads that hold the same columns' sums
+        if constexpr (TPR < 64) {
+            set = threadIdx.x >> 6;
+            lead = (threadIdx.x & 63) < TPR;
+        }
         each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
-            if constexpr (RPB > 1) {      // the wavefronts' sums, in their order
-                __syncthreads();
-                if (sub > 0) {
-                    comb[((sub - 1) * 2) * 64 + t] = ag[j];
-                    comb[((sub - 1) * 2 + 1) * 64 + t] = ab[j];
-                }
-                __syncthreads();
-                if (sub > 0) return;
+            if constexpr (TPR < 64)
 #pragma unroll
-                for (int w = 0; w < RPB - 1; ++w) {
-                    ag[j] += comb[w * 2 * 64 + t];
-                    ab[j] += comb[(w * 2 + 1) * 64 + t];
+                for (int o = TPR; o < 64; o *= 2)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        ag[j][e] += __shfl_xor(ag[j][e], o);
+                        ab[j][e] += __shfl_xor(ab[j][e], o);
+                    }
+            if constexpr (SETS > 1) {      // the wavefronts' sums, in their order
+                __syncthreads();
+                if (set > 0 && lead) {
+                    comb[((set - 1) * 2) * TPR + t] = ag[j];
+                    comb[((set - 1) * 2 + 1) * TPR + t] = ab[j];
                 }
-            }
+                __syncthreads();
+                if (set > 0 || !lead) return;
+#pragma unroll
+                for (int w = 0; w < SETS - 1; ++w) {
+                    ag[j] += comb[w * 2 * TPR + t];
+                    ab[j] += comb[(w * 2 + 1) * TPR + t];
+                }
+            } else if (!lead)
+                return;
             c.store(out, C, ag[j]);
             c.store(out + C, C, ab[j]);
         });
@@ -274,12 +298,21 @@ int launch_sum_partials(const float* partials, int G, float* out0, int n0, float
     return SD_OK;
 }
 
-// Threads a row and chunks a thread, from the row's length: a wavefront up to 2048 elements, then 256 threads up to 8192.
+// Threads a row and chunks a thread, from the row's length: a wavefront up to 2048 elements, 256 threads up to 8192, and 16 threads for short rows, of which a wavefront's
+// lanes would have little each (us, 64 / 16 threads a row: 32768 rows forward of 64 10.7 / 4.8, of 128 11.8 / 8.2, of 320 19.3 / 14.1; backward with gradients of the weights of 64 15.3 / 9.6, of 128
+// 17.0 / 14.4, but of 256 19.7 / 25.3, 320 25.8 / 27.8: a thread's sums of columns take the registers of the wavefronts that would hide its loads).
 template <int TPR_, int J_, int JW_>
 struct LnShape { static constexpr int TPR = TPR_, J = J_, JW = JW_; };
 template <class F>
-static int ln_by_length(int C, F f) {
-    if (C <= 64 * 4) return f(LnShape<64, 1, 0>());
+static int ln_by_length(int C, bool backward, F f) {
+    if (C <= 16 * 4) return f(LnShape<16, 1, 0>());
+    if (C <= 16 * 4 * 2) return f(LnShape<16, 2, 1>());
+    if (backward) {
+        if (C <= 64 * 4) return f(LnShape<64, 1, 0>());
+    } else {
+        if (C <= 16 * 4 * 5) return f(LnShape<16, 5, 2>());
+        if (C <= 16 * 4 * 8) return f(LnShape<16, 8, 5>());
+    }
     if (C <= 64 * 4 * 3) return f(LnShape<64, 3, 1>());
     if (C <= 64 * 4 * 5) return f(LnShape<64, 5, 3>());
     if (C <= 64 * 4 * 8) return f(LnShape<64, 8, 5>());
@@ -287,6 +320,7 @@ static int ln_by_length(int C, F f) {
     if (C <= 256 * 4 * 8) return f(LnShape<256, 8, 4>());
     return f(LnShape<1024, 4, 2>());
 }
+static int ln_threads_per_row(int C, bool backward) { return C <= (backward ? 128 : 512) ? 16 : C <= 2048 ? 64 : C <= 8192 ? 256 : 1024; }
 template <class F>
 static int by_type(int dtype, F f) {
     if (dtype == SD_F32) return f(static_cast<float*>(nullptr));
@@ -303,19 +337,21 @@ static int ln_check(const char* who, int x_dtype, int y_dtype, int M, int C) {
 
 // Workgroups of the forward pass: four a CU, or one for every group of rows where there are fewer
 static int ln_fwd_groups(int M, int C) {
-    const int rpb = C > 2048 ? 1 : LN_THREADS / 64;
+    const int tpr = ln_threads_per_row(C, false), rpb = tpr > LN_THREADS ? 1 : LN_THREADS / tpr;
     return std::min((M - 1) / rpb + 1, 1024);
 }
 // ... of the backward pass, eight wavefronts each.  With gradients of the weights one a CU, of short rows two: their sums of columns are written and read again (us at 128 / 256 /
-// 512 workgroups: 8192 x 1280 fp32 31.8 / 29.9 / 33.9, 2777 x 1155 bf16 17.3 / 16.4 / 21.7, 32768 x 320 51.6 / 32.3 / 26.4).  Without twice as many.
+// 512 workgroups: 8192 x 1280 fp32 31.8 / 29.9 / 33.9, 2777 x 1155 bf16 17.3 / 16.4 / 21.7, 32768 x 320 51.6 / 32.3 / 26.4), and of rows that take a workgroup no fewer than four rows to
+// each (500 x 4096, 500 / 125 workgroups, 21.0 / 13.3).  Without twice as many.
 static int ln_bwd_groups(int M, int C, bool grads) {
-    const int rpb = C > 2048 ? 1 : ln_bwd_threads(64) / 64;
+    const int tpr = ln_threads_per_row(C, true), rpb = tpr > 512 ? 1 : 512 / tpr;
     const int groups = M > 0 ? (M - 1) / rpb + 1 : 0;
-    return std::min(groups, (C <= 768 || C > 2048 ? 512 : 256) * (grads ? 1 : 2));
+    if (!grads) return std::min(groups, C <= 768 ? 1024 : 512);
+    return std::min(tpr > 64 ? (groups + 3) / 4 : groups, C <= 768 ? 512 : 256);
 }
-// Few rows, all in one launch: what the columns read a second time lies in the caches (us, two launches / one: 3 x 950 7.4 / 3.1, 300 x 1280 10.3 / 5.1, 1000 x 640 10.1 / 6.9, 2048 x
-// 1280 15.5 / 15.9, 2777 x 1155 16.4 / 17.5).
-static bool ln_bwd_few(int M, int C) { return M <= 1024 && (int64_t)M * C <= 3 << 19; }
+// Few rows, all in one launch: what the columns read a second time lies in the caches (us, two launches / one: 3 x 950 7.4 / 3.1, 300 x 1280 10.3 / 5.1, 1000 x 640 10.1 / 6.9, 500 x
+// 4096 13.3 / 8.7, 2048 x 1280 15.5 / 15.9, 2777 x 1155 16.4 / 17.5).
+static bool ln_bwd_few(int M, int C) { return M <= 1024 && (int64_t)M * C <= 1 << 22; }
 
 }  // namespace sd
 
@@ -333,7 +369,7 @@ extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* 
     hipStream_t s = static_cast<hipStream_t>(stream);
     return by_type(x_dtype, [&](auto* xt) {
         return by_type(y_dtype, [&](auto* yt) {
-            return ln_by_length(C, [&](auto shape) {
+            return ln_by_length(C, false, [&](auto shape) {
                 using X = std::remove_pointer_t<decltype(xt)>;
                 using Y = std::remove_pointer_t<decltype(yt)>;
                 using S = decltype(shape);
@@ -375,7 +411,7 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
     if (!SD_DRY_RUN("layernorm bwd%s; ", few ? " few" : "")) {
         rc = by_type(x_dtype, [&](auto* xt) {
             return by_type(y_dtype, [&](auto* yt) {
-                return ln_by_length(C, [&](auto shape) {
+                return ln_by_length(C, true, [&](auto shape) {
                     using X = std::remove_pointer_t<decltype(xt)>;
                     using D = std::remove_pointer_t<decltype(yt)>;
                     using S = decltype(shape);

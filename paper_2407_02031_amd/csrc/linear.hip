@@ -127,7 +127,7 @@ __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const 
         }
     }
 }
-// How dz is cut.  Few rows: 32 columns and all rows a workgroup, so that no sums of row blocks are left.  Else 512 or 2048 columns, and as many rows as leave two
+// How dz is cut.  Few rows: 16 columns and all rows a workgroup, so that no sums of row blocks are left.  Else 512 or 2048 columns, and as many rows as leave two
 // workgroups a CU, 8 to 32.
 struct DzCut {
     int ct, nt, rows;
@@ -135,7 +135,7 @@ struct DzCut {
     DzCut(int64_t M, int64_t N) {
         const int64_t Np = (N + 7) & ~7ll;
         const bool few = M <= 256 || (M <= 1024 && M * N <= (1 << 20));
-        ct = few ? 4 : N > 1024 ? 256 : 64;
+        ct = few ? 2 : N > 1024 ? 256 : 64;
         nt = few ? 1024 : 256;
         col_wgs = (Np + ct * 8 - 1) / (ct * 8);
         const int64_t r = M * col_wgs / 512;
@@ -266,13 +266,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, (gemm_min_waves<BM, BN, 64, WGM, WG
     else gemm_tile<BM, BN, 64, WGM, WGN, STAGES, false, GUARD, false>(P, P.tile_begin + t, lds, GemmTransposed<false, true>{});
 }
 
-// 256x128 tiles of eight wavefronts, three stages, one workgroup a CU.  (us, both products, 128x128 tiles of four wavefronts two a CU / these: M = 8192, N = 5120,
-// K = 1280 253 / 229, 2048 x 5120 x 1280 77.3 / 75.9, 1024 x 1280 x 1280 21.4 / 21.3, 8192 x 640 x 640 34.4 / 32.6; 256x256 tiles 262, 85, 34, 47.)
-// Small ones: 64x128 tiles of four wavefronts, three stages, two workgroups a CU: where all of both products' tiles run at once, their reductions need
-// fewer cuts or none.
+// Two kernels: 256x128 tiles of eight wavefronts, three stages, one workgroup a CU, and 64x128 ones of four, two a CU.  (Of the former, us, both products, 128x128 tiles of four
+// wavefronts two a CU / these: M = 8192, N = 5120, K = 1280 253 / 229, 2048 x 5120 x 1280 77.3 / 75.9, 8192 x 640 x 640 34.4 / 32.6; 256x256 tiles 262, 85, 47.  The latter take
+// small products, which then need fewer cuts or none: 300 x 515 x 1024 8.0 us where the larger tiles with three parts took 15.8.)
 constexpr int BWD_CUS = 256, BWD_PARTS = GEMM_MAX_PROBLEMS / 2;
 constexpr int BWD_BM = 256, BWD_SMALL_BM = 64, BWD_BN = 128;
-// How a product's reduction is cut: the first `whole` rows of the result not at all, the others into `parts` sums over consecutive steps, which
+// How a product's reduction is cut: the first `whole` rows of the result not at all, the others into `parts` sums over consecutive steps of 64, which
 // part_sums adds up.
 struct BwdCut {
     int64_t rows, cols, steps, tiles_n, tiles;
@@ -285,30 +284,52 @@ struct BwdCut {
     }
     size_t bytes() const { return parts > 1 ? (size_t)parts * (rows - whole) * cols * 4 : 0; }
 };
+// Tiles of two kinds on so many slots, the longer ones first: `an` of as steps, dealt evenly, then bn of bs where one is free
+template <class I>
+struct BwdRounds {
+    I q, r, as, bn, bs, slots;
+    BwdRounds(int64_t an, int64_t as_, int64_t bn_, int64_t bs_, int slots_) : q((I)an / slots_), r((I)an % slots_), as((I)as_), bn((I)bn_), bs((I)bs_), slots(slots_) {}
+    // of the second kind done after d steps
+    I done(I d) const { return r * (std::max<I>(d - (q + 1) * as, 0) / bs) + (slots - r) * (std::max<I>(d - q * as, 0) / bs); }
+    // steps until all are done
+    I until() const {
+        I d = std::max<I>((q + (r > 0)) * as, (r * as + q * slots * as + bn * bs + slots - 1) / slots);
+        while (done(d) < bn) d += std::min<I>(bs - std::max<I>(d - q * as, 0) % bs, bs - std::max<I>(d - (q + 1) * as, 0) % bs);
+        return d;
+    }
+};
 // From the sizes alone, as for both products: a gradient's bits do not depend on which others are wanted.
 struct BwdPlan {
     BwdCut x, w;
     bool small;
     bool w_first;                  // the product of the longer sums goes first
-    static int64_t tiles(int64_t r, int64_t c, int bm) { return (r + bm - 1) / bm * ((c + BWD_BN - 1) / BWD_BN); }
-    static bool is_small(int64_t M, int64_t N, int64_t K) { return tiles(M, K, BWD_SMALL_BM) + tiles(N, K, BWD_SMALL_BM) <= 2 * BWD_CUS; }
-    BwdPlan(int64_t M, int64_t N, int64_t K) : BwdPlan(M, N, K, is_small(M, N, K)) {}
-    BwdPlan(int64_t M, int64_t N, int64_t K, bool sm) : x(M, K, N, sm ? BWD_SMALL_BM : BWD_BM), w(N, K, M, sm ? BWD_SMALL_BM : BWD_BM), small(sm) {
-        const int64_t all = x.tiles * x.steps + w.tiles * w.steps, share = (all + BWD_CUS - 1) / BWD_CUS;
-        const int64_t slots = small ? 2 * BWD_CUS : BWD_CUS, shortest = small ? 12 : 4;
-        int px = 1, pw = 1;
-        if (x.tiles + w.tiles <= slots) {
-            // one round: the longer sums are cut while CUs are idle and parts are not too short
-            for (;;) {
-                const bool xl = x.steps * pw >= w.steps * px;
-                const int p = (xl ? px : pw) + 1;
-                if (p > BWD_PARTS || (xl ? x : w).steps / p < shortest || (xl ? x.tiles * p + w.tiles * pw : x.tiles * px + w.tiles * p) > slots) break;
-                (xl ? px : pw) = p;
-            }
-        } else {
-            // several: no sum longer than a CU's share
-            px = (int)std::min<int64_t>((x.steps + share - 1) / share, BWD_PARTS);
-            pw = (int)std::min<int64_t>((w.steps + share - 1) / share, BWD_PARTS);
+    BwdPlan(int64_t M, int64_t N, int64_t K) : x(M, K, N, BWD_BM), w(N, K, M, BWD_BM), small(false) {
+        // What a choice takes, us: its steps and its first loads and stores (a step of the small tiles waits less where they have a CU to themselves), the parts written and read again at
+        // 4 TB/s, and the launch that adds them up
+        float least = 0.f;
+        int px = 0, pw = 0;
+        for (int sm = 1; sm >= 0; --sm) {
+            const int bm = sm ? BWD_SMALL_BM : BWD_BM;
+            const BwdCut cx(M, K, N, bm), cw(N, K, M, bm);
+            const int slots = sm ? 2 * BWD_CUS : BWD_CUS;
+            if (sm && cx.tiles + cw.tiles > 2 * slots) continue;
+            // (in 32 bits where they do, which is cheaper)
+            const bool narrow = cx.tiles * cx.steps + cw.tiles * cw.steps < (1 << 26);
+            for (int a = 1; a <= BWD_PARTS; a += a >= 4 ? 2 : 1)
+                for (int b = 1; b <= BWD_PARTS; b += b >= 4 ? 2 : 1) {
+                    if ((a > 1 && cx.steps < 4 * a) || (b > 1 && cw.steps < 4 * b)) break;
+                    const int64_t sx = (cx.steps + a - 1) / a, sw = (cw.steps + b - 1) / b, nx = cx.tiles * a, nw = cw.tiles * b;
+                    const bool wl = sw > sx;
+                    const int64_t an = wl ? nw : nx, as = wl ? sw : sx, bn = wl ? nx : nw, bs = wl ? sx : sw;
+                    const int64_t d = narrow ? BwdRounds<int32_t>(an, as, bn, bs, slots).until() : BwdRounds<int64_t>(an, as, bn, bs, slots).until();
+                    const float parts = (a > 1 ? (float)a * M * K : 0.f) + (b > 1 ? (float)b * N * K : 0.f);
+                    const float us = (sm ? d * (nx + nw > BWD_CUS ? 0.85f : 0.57f) + 4.f : d * 0.9f + 6.f) + (parts > 0 ? 2.5f + parts * 2e-6f : 0.f);
+                    if (px == 0 || us < least) least = us, px = a, pw = b, small = sm;
+                }
+        }
+        if (small) {
+            x = BwdCut(M, K, N, BWD_SMALL_BM);
+            w = BwdCut(N, K, M, BWD_SMALL_BM);
         }
         x.all_in(px);
         w.all_in(pw);
@@ -316,16 +337,12 @@ struct BwdPlan {
         // The other product's tiles fill up what the first one's leave; where the last of them would be a round of few, they are cut in four.  (M = 8192, N =
         // 5120, K = 1280: 200 tiles of 128 steps, 320 of 80; the last 8 of these cut 201 us, not cut 229.)
         BwdCut &a = w_first ? w : x, &b = w_first ? x : w;
-        if (x.tiles + w.tiles > slots && b.parts == 1 && b.steps >= 16) {
-            const int64_t an = a.tiles * a.parts, as = (a.steps + a.parts - 1) / a.parts, q = an / BWD_CUS, r = an % BWD_CUS;
-            // tiles of b that are done after d steps
-            auto done = [&](int64_t d) { return r * std::max<int64_t>((d - (q + 1) * as) / b.steps, 0) + (BWD_CUS - r) * std::max<int64_t>((d - q * as) / b.steps, 0); };
-            int64_t until = share;             // ... all of them
-            while (done(until) < b.tiles) until += std::min(b.steps - std::max<int64_t>(until - q * as, 0) % b.steps, b.steps - std::max<int64_t>(until - (q + 1) * as, 0) % b.steps);
-            const int64_t aim = share + share / 20 + 4;
-            const int64_t left = (b.tiles - std::min(done(aim), b.tiles) + b.tiles_n - 1) / b.tiles_n;     // rows of tiles
+        if (!small && b.parts == 1 && b.steps >= 16) {
+            const BwdRounds<int64_t> t(a.tiles * a.parts, (a.steps + a.parts - 1) / a.parts, b.tiles, b.steps, BWD_CUS);
+            const int64_t share = (a.tiles * a.steps + b.tiles * b.steps + BWD_CUS - 1) / BWD_CUS, aim = std::max(share, (t.q + (t.r > 0)) * t.as) + share / 20 + 4;
+            const int64_t left = (b.tiles - std::min(t.done(aim), b.tiles) + b.tiles_n - 1) / b.tiles_n;     // rows of tiles
             // a cut tile's parts are 0.5 MB written and read, 0.065 us of the chip's memory traffic each; a step takes 0.9 us
-            if (left > 0 && until > aim && left * b.tiles_n * 4 * 0.065 < (until - aim) * 0.9) {
+            if (left > 0 && t.until() > aim && left * b.tiles_n * 4 * 0.065 < (t.until() - aim) * 0.9) {
                 b.parts = 4;
                 b.whole = std::max<int64_t>(0, (b.rows + BWD_BM - 1) / BWD_BM - left) * BWD_BM;
             }
@@ -532,7 +549,9 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
     P.res = residual; P.ldr = N; P.res_f32 = y_dtype == SD_F32;
     P.y = y; P.ldy = N; P.y_f32 = y_dtype == SD_F32;
     P.Mp = M; P.N = N; P.K0 = K; P.alpha = 1.f;
-    // Few rows.  (us, cold, z not kept, this kernel / the launches below: 1 x 5120 x 1280 6.1 / 12.8 ...)
+    // Up to 16 rows, and what the projections' one-round tiles do not take (their rule; K % 64, N % 4): straight from the weights, by the smallest tiles that are
+    // one round.  (us, cold, these kernels / 64x128 tiles: 1 x 5120 x 1280 6.1 / 12.8, 1 x 1280 x 5120 9.5 / 38.4, 300 x 1280 x 1280 10.2 / 13.9, but 500 x 1280 x 1280, two rounds,
+    // 17.9 / 14.8.)
     const int f32 = y_dtype == SD_F32;
     if (M <= 16) return launch_rows<1, 1, 6>(x, W, bias, act, residual, y, f32, z, M, N, K, s);
     P.act = act + 1;
@@ -598,7 +617,7 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
             else hipLaunchKernelGGL((dz_kernel<D, false, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
         };
         auto by_cut = [&](auto* t) {
-            if (cut.ct == 4) run(t, std::integral_constant<int, 4>(), std::integral_constant<int, 1024>());
+            if (cut.ct == 2) run(t, std::integral_constant<int, 2>(), std::integral_constant<int, 1024>());
             else if (cut.ct == 64) run(t, std::integral_constant<int, 64>(), std::integral_constant<int, 256>());
             else run(t, std::integral_constant<int, 256>(), std::integral_constant<int, 256>());
         };
