@@ -303,7 +303,8 @@ int sd_groupnorm_silu_fwd(const uint16_t* x, uint16_t* y, const uint16_t* gamma,
  *   gamma, beta  device [C] bf16; NULL: ones, zeros
  *   mean, rstd   device [M] fp32 or NULL: kept for the backward pass
  * Backward: n = (x - mean) rstd, g = dy gamma;  dx = rstd (g - sum_c g / C - n sum_c (g n) / C),
- *   dgamma = sum_m dy n, dbeta = sum_m dy, added up in a fixed order.
+ *   dgamma = sum_m dy n, dbeta = sum_m dy, added up in an order that the sizes fix (and, for few rows,
+ *   whether dx is one of the inputs).
  *   dy           device [M, C] of y_dtype;  dx device [M, C] of x_dtype; may alias x, or dy if the types
  *                are the same
  *   dgamma, dbeta device [C] fp32, overwritten (zeros for M = 0); NULL: not wanted.  With neither of

@@ -141,7 +141,7 @@ __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float
     constexpr int RPB = NT / TPR;
     __shared__ float sh[TPR > 64 ? 32 : 1];
     constexpr int SETS = TPR < 64 ? NT / 64 : RPB;          // sums of a column that meet in LDS
-    __shared__ f32x4 comb[GRADS && SETS > 1 ? (SETS - 1) * TPR * 2 : 1];
+    __shared__ f32x4 comb[GRADS ? SETS * 2 * J * TPR : 1];
     const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
     const __bf16* const gb = reinterpret_cast<const __bf16*>(gamma);
     f32x4 g[J], ag[GRADS ? J : 1], ab[GRADS ? J : 1];
@@ -188,39 +188,36 @@ __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float
     }
     if constexpr (GRADS) {
         float* const out = partials + (int64_t)group * 2 * C;
+        // the wavefronts' sums meet in LDS at once, and all threads add them up, in the order of the wavefronts
         int set = sub;
         bool lead = true;            // of the threads that hold the same columns' sums
         if constexpr (TPR < 64) {
-            set = threadIdx.x >> 6;
-            lead = (threadIdx.x & 63) < TPR;
-        }
-        each_chunk<TPR, J, JW>(t, C, [&](int j, auto c) {
-            if constexpr (TPR < 64)
 #pragma unroll
-                for (int o = TPR; o < 64; o *= 2)
+            for (int o = TPR; o < 64; o *= 2)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         ag[j][e] += __shfl_xor(ag[j][e], o);
                         ab[j][e] += __shfl_xor(ab[j][e], o);
                     }
-            if constexpr (SETS > 1) {      // the wavefronts' sums, in their order
-                __syncthreads();
-                if (set > 0 && lead) {
-                    comb[((set - 1) * 2) * TPR + t] = ag[j];
-                    comb[((set - 1) * 2 + 1) * TPR + t] = ab[j];
-                }
-                __syncthreads();
-                if (set > 0 || !lead) return;
+            set = threadIdx.x >> 6;
+            lead = (threadIdx.x & 63) < TPR;
+        }
+        if (lead)
 #pragma unroll
-                for (int w = 0; w < SETS - 1; ++w) {
-                    ag[j] += comb[w * 2 * TPR + t];
-                    ab[j] += comb[(w * 2 + 1) * TPR + t];
-                }
-            } else if (!lead)
-                return;
-            c.store(out, C, ag[j]);
-            c.store(out + C, C, ab[j]);
-        });
+            for (int j = 0; j < J; ++j) {
+                comb[(set * 2 * J + j) * TPR + t] = ag[j];
+                comb[(set * 2 * J + J + j) * TPR + t] = ab[j];
+            }
+        __syncthreads();
+        for (int p = threadIdx.x; p < 2 * J * TPR; p += NT) {
+            f32x4 v = comb[p];
+#pragma unroll
+            for (int w = 1; w < SETS; ++w) v += comb[w * 2 * J * TPR + p];
+            const bool beta = p >= J * TPR;
+            Chunk<false>(p - (beta ? J * TPR : 0), C).store(out + (beta ? C : 0), C, v);
+        }
     }
 }
 // ... and 16 columns' gradients from all rows, which need no row's sums: NT / 16 rows at a time, four of those in flight

@@ -21,14 +21,15 @@ namespace sd {
 // long, N rounded up to a multiple of 8, with zeros behind N.
 // ---------------------------------------------------------------------------------------
 template <class D, bool STORE, bool SUMS, int CT, int NT>
-__global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows) {
+__global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
     constexpr int SUB = NT / CT, BATCH = 4;
     constexpr int PARTS = CT < 64 ? NT / 64 : SUB;          // sums of a column that meet in LDS
     __shared__ f32x8 sh[PARTS > 1 ? (PARTS - 1) * CT : 1];
     const int t = threadIdx.x % CT, sub = threadIdx.x / CT;
-    const int c = (blockIdx.y * CT + t) * 8;
-    const int64_t r0 = (int64_t)blockIdx.x * rows + sub;
-    const int64_t r1 = min((int64_t)M, ((int64_t)blockIdx.x + 1) * rows);
+    const int cols = (int)blockIdx.x / blocks, block = (int)blockIdx.x - cols * blocks;
+    const int c = (cols * CT + t) * 8;
+    const int64_t r0 = (int64_t)block * rows + sub;
+    const int64_t r1 = min((int64_t)M, ((int64_t)block + 1) * rows);
     const bool whole = c + 8 <= N;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     f32x8 sum = {zero, zero};
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const 
                 sum.hi += sh[w * CT + t].hi;
             }
         }
-        float* const to = sums + (int64_t)blockIdx.x * N + c;
+        float* const to = sums + (int64_t)block * N + c;
         if (whole) {
             store4(to, sum.lo);
             store4(to + 4, sum.hi);
@@ -323,7 +324,7 @@ struct BwdPlan {
                     const int64_t an = wl ? nw : nx, as = wl ? sw : sx, bn = wl ? nx : nw, bs = wl ? sx : sw;
                     const int64_t d = narrow ? BwdRounds<int32_t>(an, as, bn, bs, slots).until() : BwdRounds<int64_t>(an, as, bn, bs, slots).until();
                     const float parts = (a > 1 ? (float)a * M * K : 0.f) + (b > 1 ? (float)b * N * K : 0.f);
-                    const float us = (sm ? d * (nx + nw > BWD_CUS ? 0.85f : 0.57f) + 4.f : d * 0.9f + 6.f) + (parts > 0 ? 2.5f + parts * 2e-6f : 0.f);
+                    const float us = (sm ? d * (nx + nw > BWD_CUS ? 0.85f : 0.57f) + 4.f : d * 0.9f + 6.f) + (parts > 0 ? 4.5f + parts * 2e-6f : 0.f);
                     if (px == 0 || us < least) least = us, px = a, pw = b, small = sm;
                 }
         }
@@ -606,15 +607,15 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
     const bool plain = !zin && y_dtype == SD_BF16 && Np == N;
     const bool store = (dx || dW) && !plain;
     if ((store || dbias) && !SD_DRY_RUN("dz%s%s; ", store ? "" : " sums only", dbias ? "" : " no sums")) {
-        const dim3 grid((unsigned)blocks, (unsigned)cut.col_wgs);
+        const dim3 grid((unsigned)(cut.blocks * cut.col_wgs));
         float* const to = blocks == 1 ? dbias : sums;
         auto run = [&](auto* t, auto ct, auto nt) {
             using D = std::remove_pointer_t<decltype(t)>;
             constexpr int CT = decltype(ct)::value, NT = decltype(nt)::value;
             const D* const d = static_cast<const D*>(dy);
-            if (store && dbias) hipLaunchKernelGGL((dz_kernel<D, true, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
-            else if (store) hipLaunchKernelGGL((dz_kernel<D, true, false, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
-            else hipLaunchKernelGGL((dz_kernel<D, false, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows);
+            if (store && dbias) hipLaunchKernelGGL((dz_kernel<D, true, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows, blocks);
+            else if (store) hipLaunchKernelGGL((dz_kernel<D, true, false, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows, blocks);
+            else hipLaunchKernelGGL((dz_kernel<D, false, true, CT, NT>), grid, dim3(NT), 0, s, d, zin, act, dzbuf, to, M, N, Np, cut.rows, blocks);
         };
         auto by_cut = [&](auto* t) {
             if (cut.ct == 2) run(t, std::integral_constant<int, 2>(), std::integral_constant<int, 1024>());

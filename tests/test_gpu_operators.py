@@ -351,6 +351,27 @@ def test_linear_fwd_large(B, M, N, K):
     check_lin_fwd(B, x, W, bias, 0, res, torch.float32, False)
 
 
+@pytest.mark.parametrize("M,N,K,kernel", [
+    (16, 333, 648, "linear rows 16x16"), (31, 130, 1000, "linear rows 32x16"), (77, 1493, 200, "linear rows 32x32"), (500, 999, 72, "linear rows 64x32"), (9031, 8, 16, "linear rows 64x32"),
+    (22, 64, 320, "thin 32x32/0"), (33, 4288, 320, "thin 32x64/0"), (97, 4736, 1088, "thin 64x64/0"), (17, 76, 192, "gemm16 64x80/0"), (681, 2752, 64, "gemm16 64x160/0"), (5028, 832, 128, "gemm16 128x160/0"),
+    (588, 899, 64, "gemm act 64x128/4 waves/3 stages"), (588, 899, 72, "gemm act 64x128/4 waves/3 stages guard"), (9235, 796, 64, "gemm act 128x128/4 waves/2 stages"),
+    (9235, 792, 24, "gemm act 128x128/4 waves/2 stages guard"), (6555, 1283, 128, "gemm act 128x160/4 waves/2 stages"), (2770, 2986, 8, "gemm act 128x160/4 waves/2 stages guard"),
+    (6940, 1088, 192, "gemm act 256x128/8 waves/3 stages"), (11162, 593, 24, "gemm act 256x128/8 waves/3 stages guard"), (8281, 453, 256, "gemm act 128x256/8 waves/3 stages"), (8434, 401, 72, "gemm act 128x256/8 waves/3 stages guard")])
+def test_linear_fwd_every_kernel(B, M, N, K, kernel):
+    """Each kernel with and without z and residual, results of both types; the choice does not depend on them."""
+    import torch
+    x, W, bias, g = lin_inputs(M, N, K, M + K)
+    for yt in (torch.bfloat16, torch.float32):
+        res = torch.randn(M, N, generator=g, device="cuda").to(yt)
+        with B.dry_run() as names:
+            B.linear_fwd(x, W, bias, 1, residual=res, out_dtype=yt, save_z=True)
+            B.linear_fwd(x, W, None, 0, out_dtype=yt)
+        assert names == [kernel] * 2
+        check_lin_fwd(B, x, W, bias, 3, res, yt, True)
+        check_lin_fwd(B, x, W, None, 1, None, yt, True)
+        check_lin_fwd(B, x, W, bias, 0, res, yt, False)
+
+
 def check_lin_bwd(B, dy, x, W, z, act, dwt):
     import torch
     M, K = x.shape
@@ -401,6 +422,60 @@ def test_linear_bwd_large(B, M, N, K):
     z = (1.5 * torch.randn(M, N, generator=g, device="cuda")).bfloat16()
     check_lin_bwd(B, dy, x, W, z, 2, torch.bfloat16)
     check_lin_bwd(B, dy, x, W, None, 0, torch.float32)
+
+
+@pytest.mark.parametrize("M,N,K,launches", [
+    (300, 64, 64, "gemm bwd 64x128/4 waves/3 stages guard, 1 of dW, 1 of dx"), (64, 1408, 640, "gemm bwd 64x128/4 waves/3 stages, 1 of dW, 4 of dx"),
+    (2, 4680, 520, "gemm bwd 64x128/4 waves/3 stages guard, 1 of dW, 8 of dx"), (17000, 260, 136, "gemm bwd 64x128/4 waves/3 stages guard, 8 of dW, 1 of dx"),
+    (4096, 1280, 264, "gemm bwd 64x128/4 waves/3 stages, 4 of dW, 1 of dx"), (5760, 768, 832, "gemm bwd 256x128/8 waves/3 stages, 4 of dW, 1 of dx"),
+    (9000, 2300, 200, "gemm bwd 256x128/8 waves/3 stages guard, 6 of dW, 2 of dx"), (8192, 5120, 1280, "gemm bwd 256x128/8 waves/3 stages, 1 of dW, 5 of dx")])
+def test_linear_bwd_every_cut(B, M, N, K, launches):
+    import torch
+    x, W, bias, g = lin_inputs(M, N, K, M)
+    z = (1.5 * torch.randn(M, N, generator=g, device="cuda")).bfloat16()
+    for yt, act, dwt in ((torch.bfloat16, 3, torch.bfloat16), (torch.float32, 2, torch.float32)):
+        dy = torch.randn(M, N, generator=g, device="cuda").to(yt)
+        with B.dry_run(True) as names:
+            B.linear_bwd(dy, x, W, z, act, dw_dtype=dwt)
+        assert names[1] == launches
+        check_lin_bwd(B, dy, x, W, z, act, dwt)
+
+
+def test_linear_more_columns_than_a_grid_has_rows(B):
+    import torch
+    M, N, K = 2, 1100000, 8
+    x, W, bias, g = lin_inputs(M, N, K, 3)
+    check_lin_fwd(B, x, W, bias, 2, None, torch.bfloat16, True)
+    dy = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    dx, dW, db = B.linear_bwd(dy, x, W)
+    dz = dy.double()
+    rx = dz @ W.double()
+    within(dx, rx, (N + 8) * U * (dz.abs() @ W.double().abs()))
+    within(dW, dz.T @ x.double(), (M + 8) * U * (dz.abs().T @ x.double().abs()))
+    within(db, dz.sum(0), 4 * U * dz.abs().sum(0))
+
+
+def test_linear_offsets_past_32_bits(B):
+    """Rows of x and y behind 2^31 elements: the same bits as at the start."""
+    import torch
+    M, N, K = 600064, 4096, 4096
+    x, W, bias, g = lin_inputs(64, N, K, 3)
+    big = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    big.view(M // 64, 64, K).copy_(x.expand(M // 64, 64, K))
+    y, z = B.linear_fwd(big, W, bias, 3, save_z=True)
+    for t in (y, z):
+        t = t.view(M // 64, 64, N)
+        assert torch.equal(t[0], t[-1]) and torch.equal(t[0], t[M // 128])
+    check = B.linear_fwd(big[:128].clone(), W, bias, 3)
+    assert float((check.float() - y[:128].float()).abs().max()) <= 2.0 ** -7 * float(y[:128].float().abs().max())
+    del y
+    dx, dW, db = B.linear_bwd(z, big, W)
+    t = dx.view(M // 64, 64, K)
+    assert torch.equal(t[0], t[M // 128])
+    rw = z[:64].double().T @ x.double() * (M // 64)
+    # a thread's rows, its share of the row blocks, and the joins: fewer than 1300 additions in a row; the products' sums in fewer than M / 32, and one rounding
+    within(db, z[:64].double().sum(0) * (M // 64), 1300 * U * z[:64].double().abs().sum(0) * (M // 64))
+    within(dW, rw, M / 32 * U * (z[:64].double().abs().T @ x.double().abs() * (M // 64)))
 
 
 def test_linear_gradients_against_differences(B):
@@ -578,3 +653,34 @@ def test_feed_forward_gradients_as_they_would_be_used(B):
     # up to seven roundings to bf16 on the way to each gradient, 2^-8 each, independent
     for got, want in zip((dx, dg, db, dw1, dc1, dw2, dc2), ref):
         assert float((got.double() - want).norm() / want.norm()) <= math.sqrt(7) * 2.0 ** -8
+
+
+def test_two_streams_at_once(B):
+    """Calls on two streams, a workspace each, give what each gives alone."""
+    import torch
+    M, N, K = 3000, 640, 320
+    jobs = []
+    for i in range(2):
+        x, W, bias, g = lin_inputs(M, N, K, 20 + i)
+        dy = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+        h = torch.randn(M, K, generator=g, device="cuda")
+        q, pos = torch.randn(1, M, 5, 64, generator=g, device="cuda").bfloat16(), torch.rand(M, 2, generator=g, device="cuda") * 64
+        jobs.append((x, W, bias, dy, h, q, pos))
+    rope = B.Rope(64, [16, 16])
+
+    def work(x, W, bias, dy, h, q, pos):
+        y, z = B.linear_fwd(x, W, bias, 2, save_z=True)
+        n, mean, rstd = B.layernorm_fwd(h, stats=True)
+        return (y, *B.linear_bwd(dy, x, W, z, 2), n, *B.layernorm_bwd(n, h, mean, rstd), B.rope_fwd(rope, pos, q)[0])
+    want = [work(*j) for j in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in jobs]
+    got = [[], []]
+    for rep in range(5):
+        for s, j, o in zip(streams, jobs, got):
+            with torch.cuda.stream(s):
+                o.append(work(*j))
+    torch.cuda.synchronize()
+    for o, w in zip(got, want):
+        for r in o:
+            assert all(torch.equal(a, b) for a, b in zip(r, w))
