@@ -220,43 +220,55 @@ __device__ __forceinline__ void ln_bwd_rows(const D* dy, const X* x, const float
         }
     }
 }
-// ... and 16 columns' gradients from all rows, which need no row's sums: NT / 16 rows at a time, four of those in flight
+// ... and 16 columns' gradients from all rows, which need no row's sums: four threads a row, NT / 4 rows at a time, four of those in flight.  Neighbouring columns go to the same XCD, whose
+// L2 then holds the lines that they share.
 template <class X, class D, int NT>
-__device__ __forceinline__ void ln_bwd_columns(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, float* dgamma, float* dbeta, int M, int C, int block) {
-    constexpr int SUB = NT / 16, BATCH = 4;
-    __shared__ float2 sh[NT / 64 * 16];
-    const int col = block * 16 + (threadIdx.x & 15), at = min(col, C - 1);
-    float a = 0.f, b = 0.f;
-    for (int r = threadIdx.x >> 4; r < M; r += SUB * BATCH) {
-        float v[BATCH], d[BATCH], m[BATCH], s[BATCH];
+__device__ __forceinline__ void ln_bwd_columns(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, float* dgamma, float* dbeta, int M, int C, int block, int blocks) {
+    constexpr int SUB = NT / 4, BATCH = 4;
+    __shared__ f32x4 sh[2][NT / 64][4];
+    const int per = (blocks + 7) / 8, mine = (block & 7) * per + (block >> 3);
+    const Chunk<false> c(mine * 4 + (threadIdx.x & 3), C);
+    f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+    if ((block >> 3) < per && c.first < C)
+        for (int r = threadIdx.x >> 2; r < M; r += SUB * BATCH) {
+            f32x4 v[BATCH], d[BATCH];
+            float m[BATCH], s[BATCH];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int64_t row = min(r + i * SUB, M - 1);
-            v[i] = (float)x[row * C + at];
-            d[i] = (float)dy[row * C + at];
-            m[i] = mean[row];
-            s[i] = rstd[row];
+            for (int i = 0; i < BATCH; ++i) {
+                const int64_t row = min(r + i * SUB, M - 1);
+                v[i] = load4(x + row * C + c.at);
+                d[i] = load4(dy + row * C + c.at);
+                m[i] = mean[row];
+                s[i] = rstd[row];
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i)
+                if (r + i * SUB < M)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        a[e] += d[i][e] * ((v[i][e] - m[i]) * s[i]);
+                        b[e] += d[i][e];
+                    }
         }
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i)
-            if (r + i * SUB < M) {
-                a += d[i] * ((v[i] - m[i]) * s[i]);
-                b += d[i];
-            }
+    for (int o = 4; o < 64; o *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a[e] += __shfl_xor(a[e], o);
+            b[e] += __shfl_xor(b[e], o);
+        }
+    if ((threadIdx.x & 63) < 4) {
+        sh[0][threadIdx.x >> 6][threadIdx.x & 3] = a;
+        sh[1][threadIdx.x >> 6][threadIdx.x & 3] = b;
     }
-    a += __shfl_xor(a, 16);
-    b += __shfl_xor(b, 16);
-    a += __shfl_xor(a, 32);
-    b += __shfl_xor(b, 32);
-    if ((threadIdx.x & 63) < 16) sh[threadIdx.x / 64 * 16 + (threadIdx.x & 15)] = make_float2(a, b);
     __syncthreads();
-    if (threadIdx.x >= 16 || col >= C) return;
+    if (threadIdx.x >= 4 || (block >> 3) >= per || c.first >= C) return;
     for (int w = 1; w < NT / 64; ++w) {
-        a += sh[w * 16 + threadIdx.x].x;
-        b += sh[w * 16 + threadIdx.x].y;
+        a += sh[0][w][threadIdx.x];
+        b += sh[1][w][threadIdx.x];
     }
-    if (dgamma) dgamma[col] = a;
-    if (dbeta) dbeta[col] = b;
+    if (dgamma) c.store(dgamma, C, a);
+    if (dbeta) c.store(dbeta, C, b);
 }
 template <class X, class D, int TPR, int J, int JW, bool GRADS, int NT>
 __global__ __launch_bounds__(NT) void ln_bwd_kernel(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* __restrict__ gamma,
@@ -268,7 +280,7 @@ template <class X, class D, int TPR, int J, int JW, int NT>
 __global__ __launch_bounds__(NT) void ln_bwd_few_kernel(const D* dy, const X* x, const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* __restrict__ gamma,
                                                         X* dx, float* dgamma, float* dbeta, int M, int C, int groups) {
     if ((int)blockIdx.x < groups) ln_bwd_rows<X, D, TPR, J, JW, false, NT>(dy, x, mean, rstd, gamma, dx, nullptr, M, C, blockIdx.x, groups);
-    else ln_bwd_columns<X, D, NT>(dy, x, mean, rstd, dgamma, dbeta, M, C, (int)blockIdx.x - groups);
+    else ln_bwd_columns<X, D, NT>(dy, x, mean, rstd, dgamma, dbeta, M, C, (int)blockIdx.x - groups, (int)gridDim.x - groups);
 }
 
 // 16 columns a workgroup, 32 rows at a time, so that nearly all of its loads are in flight together; the sums of a column's 32 threads are added in a fixed order.
@@ -346,9 +358,9 @@ static int ln_bwd_groups(int M, int C, bool grads) {
     if (!grads) return std::min(groups, C <= 768 ? 1024 : 512);
     return std::min(tpr > 64 ? (groups + 3) / 4 : groups, C <= 768 ? 512 : 256);
 }
-// Few rows, all in one launch: what the columns read a second time lies in the caches (us, two launches / one: 3 x 950 7.4 / 3.1, 300 x 1280 10.3 / 5.1, 1000 x 640 10.1 / 6.9, 500 x
-// 4096 13.3 / 8.7, 2048 x 1280 15.5 / 15.9, 2777 x 1155 16.4 / 17.5).
-static bool ln_bwd_few(int M, int C) { return M <= 1024 && (int64_t)M * C <= 1 << 22; }
+// Few rows, all in one launch: what the columns read a second time lies in the caches, but there are few of their workgroups (us, two launches / one: 3 x 950 6.1 / 3.1, 300 x 1280 8.6 / 5.1, 1000 x 640 8.4 /
+// 6.6, 500 x 4096 15.8 / 7.4, 1200 x 1000 10.1 / 7.2, 2048 x 1280 14.7 / 15.0, 2777 x 1155 15.2 / 16.5, 4096 x 1280 15.7 / 23.8).
+static bool ln_bwd_few(int M, int C) { return M <= 1536 && (int64_t)M * C <= 1 << 22; }
 
 }  // namespace sd
 
@@ -417,7 +429,7 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
                     const X* const xp = static_cast<const X*>(x);
                     X* const o = static_cast<X*>(dx);
                     if (few)
-                        hipLaunchKernelGGL((ln_bwd_few_kernel<X, D, S::TPR, S::J, S::JW, NT>), dim3(groups + (C + 15) / 16), dim3(NT), 0, s, d, xp, mean, rstd, gamma, o, dgamma, dbeta, M, C, groups);
+                        hipLaunchKernelGGL((ln_bwd_few_kernel<X, D, S::TPR, S::J, S::JW, NT>), dim3(groups + ((C + 15) / 16 + 7) / 8 * 8), dim3(NT), 0, s, d, xp, mean, rstd, gamma, o, dgamma, dbeta, M, C, groups);
                     else if (grads)
                         hipLaunchKernelGGL((ln_bwd_kernel<X, D, S::TPR, S::J, S::JW, true, NT>), dim3(groups), dim3(NT), 0, s, d, xp, mean, rstd, gamma, o, partials, M, C);
                     else

@@ -324,7 +324,7 @@ struct BwdPlan {
                     const int64_t an = wl ? nw : nx, as = wl ? sw : sx, bn = wl ? nx : nw, bs = wl ? sx : sw;
                     const int64_t d = narrow ? BwdRounds<int32_t>(an, as, bn, bs, slots).until() : BwdRounds<int64_t>(an, as, bn, bs, slots).until();
                     const float parts = (a > 1 ? (float)a * M * K : 0.f) + (b > 1 ? (float)b * N * K : 0.f);
-                    const float us = (sm ? d * (nx + nw > BWD_CUS ? 0.85f : 0.57f) + 4.f : d * 0.9f + 6.f) + (parts > 0 ? 4.5f + parts * 2e-6f : 0.f);
+                    const float us = (sm ? d * (nx + nw > BWD_CUS ? 0.85f : 0.57f) + 4.f : d * 0.9f + 6.f) + (parts > 0 ? 6.f + parts * 2e-6f : 0.f);
                     if (px == 0 || us < least) least = us, px = a, pw = b, small = sm;
                 }
         }
