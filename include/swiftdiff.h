@@ -50,7 +50,7 @@ extern "C" {
 #define SD_ACT_GELU 1      /* z Phi(z), exact (erf) form                              */
 #define SD_ACT_GELU_TANH 2 /* its tanh form                                           */
 #define SD_ACT_SILU 3      /* z / (1 + exp(-z))                                       */
-#define SD_ACT_RELU 4
+#define SD_ACT_RELU 4      /* its slope at 0 is 0                                     */
 
 /* One linear projection with an optional rank-r adapter (Section 2, "Low-Rank
  * Adaptation": the patched weight is the base weight plus a rank-r product).
@@ -331,7 +331,8 @@ int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_d
  *   q, k       device [Bn * T] rows of heads x head_dim elements, ld elements apart (the queries and keys of packed
  *              rows, for instance); heads_k = 0: queries alone (k, yk NULL)
  *   yq, yk     rows like those; may be the same rows as q and k (in place), else they do not overlap them
- * head_dim is a multiple of 8, at most 256 (SD_EUNSUPPORTED otherwise); ld are multiples of 8. */
+ * head_dim is a multiple of 8, at most 256, and Bn * T below 2^29, or 2^24 where a token has many heads
+ * (SD_EUNSUPPORTED otherwise); ld are multiples of 8. */
 #define SD_ROPE_INTERLEAVED 0
 #define SD_ROPE_HALVES 1
 #define SD_ROPE_AXIS_HALVES 2
@@ -355,7 +356,7 @@ int sd_rope_bwd(const sd_rope* r, const float* pos, int64_t pos_stride, const vo
  *   x         device [M, K] bf16;  W device [N, K] bf16;  bias device [N] bf16 or NULL
  *   act       SD_ACT_*
  *   residual  device [M, N] of y_dtype or NULL; may alias y
- *   y         device [M, N] of y_dtype, bf16 or fp32
+ *   y         device [M, N] of y_dtype, bf16 or fp32; neither y nor z aliases x or W
  *   z         device [M, N] bf16 or NULL: what the backward pass of an activation needs
  * Backward: dz = dy act'(z);  dx = dz W,  dW = dz^T x,  dbias = sum_m dz.  (The residual's gradient is dy.)
  *   dy        device [M, N] of y_dtype;  z as kept by the forward call (not read for SD_ACT_NONE)
@@ -364,7 +365,7 @@ int sd_rope_bwd(const sd_rope* r, const float* pos, int64_t pos_stride, const vo
  *             aliases an input.
  *   The products multiply dz in bf16 (rounded once) and sum in fp32; dbias sums dz as it was before.  All sums
  *   are in a fixed order.
- * K is a multiple of 8 (SD_EUNSUPPORTED otherwise); M and N are any. */
+ * K is a multiple of 8, M below 2^28, N and K below 2^22 (SD_EUNSUPPORTED otherwise). */
 int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int32_t act, const void* residual, void* y, int32_t y_dtype, uint16_t* z,
                   int32_t M, int32_t N, int32_t K, void* stream);
 size_t sd_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K);

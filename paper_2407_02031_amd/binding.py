@@ -382,6 +382,12 @@ def _expect(name: str, t: Optional[torch.Tensor], shape, dtypes, dev: int, dense
     raise ValueError(f"{name}: not contiguous")
 
 
+def _sizes(*n: int) -> None:
+    """ctypes keeps the lowest 32 bits of a larger number and says nothing."""
+    if max(n) > 0x7fffffff:
+        raise ValueError(f"sizes {n}: below 2^31, please")
+
+
 def _scratch(x: torch.Tensor, nbytes: int, ws: Optional[torch.Tensor], dev: int):
     """A workspace beside x, its address and its size; or the caller's."""
     if ws is None:
@@ -395,6 +401,7 @@ def layernorm_fwd(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, out
     dev, shape = _on(x), x.shape
     Cc = shape[-1]
     M = x.numel() // Cc if Cc else 0
+    _sizes(M, Cc)
     px = _expect("x", x, shape, _FLOATS, dev)
     pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
     pb = _expect("beta", beta, (Cc,), _BF16, dev)
@@ -416,6 +423,7 @@ def layernorm_bwd(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: t
     dev, shape = _on(x), x.shape
     Cc = shape[-1]
     M = x.numel() // Cc if Cc else 0
+    _sizes(M, Cc)
     px = _expect("x", x, shape, _FLOATS, dev)
     pd = _expect("dy", dy, shape, _FLOATS, dev)
     pm = _expect("mean", mean, shape[:-1], _F32, dev)
@@ -465,6 +473,7 @@ def _rope(fn, rope: Rope, pos: torch.Tensor, q: torch.Tensor, k, q_out, k_out):
     dev, shape = _on(q), q.shape
     Bn, T, hq, D = shape
     n = len(rope.axis_pairs)
+    _sizes(Bn, T, hq)
     if pos.dim() == 2:
         apart, ppos = 0, _expect("pos", pos, (T, n), _F32, dev)
     else:
@@ -485,6 +494,7 @@ def _rope(fn, rope: Rope, pos: torch.Tensor, q: torch.Tensor, k, q_out, k_out):
     hk = ldk = ldyk = 0
     if k is not None:
         hk = k.shape[2]
+        _sizes(hk)
         pk, ldk, yk, pyk, ldyk = place("k", k, (Bn, T, hk, D), k_out)
     _check(fn(rope._ref, ppos, apart, pq, ldq, hq, pyq, ldyq, pk, ldk, hk, pyk, ldyk, _dt(q), Bn, T, _raw_stream(dev)))
     return yq, yk
@@ -506,6 +516,7 @@ def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_NO
     dev = _on(x)
     M, K = x.shape
     N = W.shape[0]
+    _sizes(M, N, K)
     px = _expect("x", x, (M, K), _BF16, dev)
     pw = _expect("W", W, (N, K), _BF16, dev)
     pb = _expect("bias", bias, (N,), _BF16, dev)
@@ -526,6 +537,7 @@ def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: 
     dev = _on(x)
     M, K = x.shape
     N = W.shape[0]
+    _sizes(M, N, K)
     px = _expect("x", x, (M, K), _BF16, dev)
     pw = _expect("W", W, (N, K), _BF16, dev)
     pd = _expect("dy", dy, (M, N), _FLOATS, dev)

@@ -67,7 +67,8 @@ __device__ __forceinline__ float act_slope(float z) {
     }
     if (KIND == SD_ACT_GELU_TANH) {
         const float s = gelu_tanh_gate(z);
-        return s + z * s * (1.f - s) * (2.f * 0.79788456080286535588f) * fmaf(3.f * 0.044715f * z, z, 1.f);
+        const float q = z * s * (1.f - s) * (2.f * 0.79788456080286535588f);      // (0 where z^2 would pass fp32)
+        return s + fmaf(q * z, 3.f * 0.044715f * z, q);
     }
     if (KIND == SD_ACT_SILU) {
         const float s = sigmoid(z);

@@ -374,6 +374,7 @@ extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* 
     SD_REQUIRE(x && y, SD_EINVAL, "layernorm_fwd: x or y is null");
     SD_REQUIRE(aligned16(x) && aligned16(y) && aligned16(gamma) && aligned16(beta) && aligned16(mean) && aligned16(rstd), SD_EINVAL,
                "layernorm_fwd: pointers must be 16-byte aligned");
+    SD_REQUIRE(x != y || x_dtype == y_dtype, SD_EINVAL, "layernorm_fwd: in place with two types");
     if (SD_DRY_RUN("layernorm fwd; ")) return SD_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     return by_type(x_dtype, [&](auto* xt) {
@@ -382,7 +383,7 @@ extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* 
                 using X = std::remove_pointer_t<decltype(xt)>;
                 using Y = std::remove_pointer_t<decltype(yt)>;
                 using S = decltype(shape);
-                    constexpr int B = ln_block<S::TPR>();
+                constexpr int B = ln_block<S::TPR>();
                 hipLaunchKernelGGL((ln_fwd_kernel<X, Y, S::TPR, S::J, S::JW>), dim3(ln_fwd_groups(M, C)), dim3(B), 0, s, static_cast<const X*>(x), gamma, beta, eps,
                                    static_cast<Y*>(y), mean, rstd, M, C);
                 SD_HIP_CHECK(hipGetLastError());
@@ -405,6 +406,7 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
     SD_REQUIRE(M == 0 || (dy && x && mean && rstd && dx), SD_EINVAL, "layernorm_bwd: dy, x, mean, rstd or dx is null");
     SD_REQUIRE(aligned16(dy) && aligned16(x) && aligned16(mean) && aligned16(rstd) && aligned16(gamma) && aligned16(dx) && aligned16(dgamma) && aligned16(dbeta), SD_EINVAL,
                "layernorm_bwd: pointers must be 16-byte aligned");
+    SD_REQUIRE(M == 0 || dx != dy || x_dtype == y_dtype, SD_EINVAL, "layernorm_bwd: in place of dy with two types");
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (M == 0) return grads ? launch_sum_partials(nullptr, 0, dgamma, C, dbeta, C, s) : SD_OK;    // sums over no rows
     // (not in place: a row may be overwritten before a column has read it)

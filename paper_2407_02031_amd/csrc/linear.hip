@@ -507,10 +507,12 @@ static int launch_rows(const uint16_t* x, const uint16_t* W, const uint16_t* bia
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }
+constexpr int LINEAR_MAX_M = 1 << 28, LINEAR_MAX_NK = 1 << 22;
 static int linear_sizes(const char* who, int M, int N, int K, int act, int y_dtype) {
     SD_REQUIRE(M >= 0 && N >= 0, SD_EINVAL, "%s: M=%d N=%d", who, M, N);
     SD_REQUIRE(K > 0 && K % 8 == 0, SD_EUNSUPPORTED, "%s: K=%d is not a positive multiple of 8", who, K);
-    SD_REQUIRE(K < (1 << 22) && N < (1 << 22), SD_EUNSUPPORTED, "%s: N=%d K=%d (below 2^22)", who, N, K);
+    // (threads of a launch stay below 2^32)
+    SD_REQUIRE(M < LINEAR_MAX_M && N < LINEAR_MAX_NK && K < LINEAR_MAX_NK, SD_EUNSUPPORTED, "%s: M=%d N=%d K=%d (M below 2^28, N and K below 2^22)", who, M, N, K);
     SD_REQUIRE((M / 64 + 1ll) * (N / 64 + 1) < (1ll << 30) && (M / 128 + 1ll) * (K / 128 + 1) < (1ll << 26), SD_EUNSUPPORTED, "%s: M=%d N=%d K=%d", who, M, N, K);
     SD_REQUIRE(act >= SD_ACT_NONE && act <= SD_ACT_RELU, SD_EINVAL, "%s: activation %d", who, act);
     SD_REQUIRE(y_dtype == SD_BF16 || y_dtype == SD_F32, SD_EINVAL, "%s: y_dtype=%d", who, y_dtype);
@@ -539,6 +541,7 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
     if (rc || M == 0 || N == 0) return rc;
     SD_REQUIRE(x && W && y, SD_EINVAL, "linear_fwd: x, W or y is null");
     SD_REQUIRE(aligned16(x) && aligned16(W) && aligned16(bias) && aligned16(residual) && aligned16(y) && aligned16(z), SD_EINVAL, "linear_fwd: pointers must be 16-byte aligned");
+    SD_REQUIRE(y != x && y != W && y != z && z != x && z != W && (!z || z != residual), SD_EINVAL, "linear_fwd: y or z in an input's place");
     hipStream_t s = static_cast<hipStream_t>(stream);
     GemmGroup g;
     memset(&g, 0, sizeof(g));
@@ -566,7 +569,7 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
 }
 
 extern "C" size_t sd_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K) {
-    if (M <= 0 || N <= 0 || K <= 0) return 256;
+    if (M <= 0 || N <= 0 || K <= 0 || M >= LINEAR_MAX_M || N >= LINEAR_MAX_NK || K >= LINEAR_MAX_NK) return 256;      // (nothing to do, or refused)
     return BwdWs(M, N, K).total();
 }
 
@@ -589,6 +592,8 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
     }
     SD_REQUIRE(dy && (!dW || x) && (!dx || W), SD_EINVAL, "linear_bwd: dy, x or W is null");
     SD_REQUIRE(act == SD_ACT_NONE || z, SD_EINVAL, "linear_bwd: an activation needs z");
+    for (const void* const out : {static_cast<const void*>(dx), static_cast<const void*>(dW), static_cast<const void*>(dbias)})
+        SD_REQUIRE(!out || (out != dy && out != x && out != W && out != z), SD_EINVAL, "linear_bwd: a gradient in an input's place");
     if (!dx && !dW && !dbias) return SD_OK;
     const size_t need = sd_linear_bwd_workspace_bytes(M, N, K);
     SD_REQUIRE(ws && ws_bytes >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SD_EWORKSPACE, "linear_bwd: workspace of %zu bytes, need %zu, 256-byte aligned", ws_bytes, need);

@@ -17,7 +17,6 @@ namespace sd {
 
 constexpr int ROPE_AXES = SD_ROPE_MAX_AXES, ROPE_MAX_D = 256, ROPE_THREADS = 256;
 constexpr int ROPE_MAX_TOKENS = 32;        // of a workgroup
-constexpr int ROPE_TABLE = 4096;           // cosine-sine pairs in LDS
 
 struct RopeArgs {
     const float* pos;
@@ -149,7 +148,6 @@ template <class T, int V, bool INTER>
 static int launch_rope(RopeArgs& a, hipStream_t stream) {
     a.units = INTER ? a.D / V : a.D / (2 * V);
     a.rot_units = INTER ? 2 * a.R / V : a.R / V;
-    if (SD_DRY_RUN("rope %s%d; ", INTER ? "neighbours " : "halves ", V)) return SD_OK;
     const int per = a.heads * a.units;
     // So many tokens that a thread has up to four units, but no fewer workgroups than four a CU while there are tokens.  (us at 4 / 8 units: 12844 tokens of 32 heads x 128 fp32 79.7 /
     // 83.4, 8192 of 40 x 64 bf16 22.8 / 23.0; as few workgroups as eight units take / four a CU: 40 tokens of 4 x 88 6.0 / 2.9, 54 of 24 x 32 5.7 / 3.5)
@@ -157,12 +155,15 @@ static int launch_rope(RopeArgs& a, hipStream_t stream) {
     int tokens = 4 * ROPE_THREADS / per;
     tokens = tokens > ROPE_MAX_TOKENS ? ROPE_MAX_TOKENS : tokens;
     tokens = tokens > most ? (int)most : tokens < 1 ? 1 : tokens;
-    while (tokens * a.R > ROPE_TABLE) --tokens;
+    static_assert(ROPE_MAX_TOKENS * (ROPE_MAX_D / 2) * sizeof(float2) <= 32768, "the table");
+    const int64_t groups = (a.rows - 1) / tokens + 1;
+    SD_REQUIRE(groups < (1 << 24), SD_EUNSUPPORTED, "rope: %lld tokens of %d heads", (long long)a.rows, a.heads);      // (threads of a launch stay below 2^32)
     a.tokens = tokens;
     // (exact: a unit's number times the divisor stays below 2^32)
     a.by_token = tokens == 1 ? 0 : (uint32_t)((1ull << 32) / per + 1);
     a.by_head = (uint32_t)((1ull << 32) / a.units + 1);
-    hipLaunchKernelGGL((rope_kernel<T, V, INTER>), dim3((unsigned)((a.rows - 1) / tokens + 1)), dim3(ROPE_THREADS), tokens * a.R * sizeof(float2), stream, a);
+    if (SD_DRY_RUN("rope %s%d; ", INTER ? "neighbours " : "halves ", V)) return SD_OK;
+    hipLaunchKernelGGL((rope_kernel<T, V, INTER>), dim3((unsigned)groups), dim3(ROPE_THREADS), tokens * a.R * sizeof(float2), stream, a);
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }
@@ -223,6 +224,7 @@ static int rope(const char* who, float sign, const sd_rope* r, const float* pos,
                "%s: queries need 16-byte aligned pointers and rows of a multiple of 8 elements, %lld at least", who, (long long)wq);
     SD_REQUIRE(heads_k == 0 || (k && yk && aligned16(k) && aligned16(yk) && ldk >= wk && ldyk >= wk && ldk % 8 == 0 && ldyk % 8 == 0), SD_EINVAL,
                "%s: keys need 16-byte aligned pointers and rows of a multiple of 8 elements, %lld at least", who, (long long)wk);
+    SD_REQUIRE(heads_q == 0 || heads_k == 0 || (yq != yk && yq != k && yk != q), SD_EINVAL, "%s: a result in the other's place", who);
     a.rows = (int64_t)Bn * T;
     SD_REQUIRE(a.rows <= 0x7fffffff, SD_EUNSUPPORTED, "%s: %lld tokens", who, (long long)a.rows);
     a.pos = pos; a.pos_stride = pos_stride; a.q = q; a.k = k; a.yq = yq; a.yk = yk;

@@ -525,6 +525,21 @@ def test_linear_edges(B):
     assert torch.equal(bad, want)
 
 
+@pytest.mark.parametrize("act", [1, 2, 3, 4])
+def test_slopes_far_out(B, act):
+    """dbias of one row is act'(z) itself: 0 or 1 far out, with no overflow on the way, and NaN where z is NaN."""
+    import torch
+    z = torch.tensor([-3e38, -1e30, -1e20, -3e18, -200.0, -30.0, -1.0, 0.0, 1.0, 30.0, 200.0, 3e18, 1e20, 1e30, 3e38, math.nan], device="cuda").bfloat16()[None]
+    x, W = torch.zeros(1, 8, dtype=torch.bfloat16, device="cuda"), torch.zeros(16, 8, dtype=torch.bfloat16, device="cuda")
+    db = B.linear_bwd(torch.ones_like(z), x, W, z, act, grads=(False, False, True))[2]
+    d = z[0, 4:11].double().requires_grad_()
+    # (the clamp in act64 has slope 1 at 0, relu by convention 0)
+    (d.relu() if act == 4 else act64(d, act)).sum().backward()
+    want = torch.cat([torch.zeros(4), d.grad.cpu(), torch.ones(4)]).cuda()
+    # erf's polynomial is off by 1.5e-7, the exponential and the reciprocal by 4 U each, products of |z| <= 200 by less
+    assert torch.allclose(db[:15].double(), want.double(), rtol=0, atol=2e-6) and torch.isnan(db[15])
+
+
 # ---- together --------------------------------------------------------------------------------------------------------------
 class Block:
     """A diffusion transformer's block out of the public calls: layer norm, packed projection, rotary positions, attention, projection into the fp32

@@ -92,6 +92,40 @@ def test_linear_refusals(B):
     assert L.sd_linear_bwd_workspace_bytes(0, 8, 8) == 256 and L.sd_linear_bwd_workspace_bytes(100, 13, 8) >= 100 * 16 * 2 + 2 * 13 * 4
 
 
+def test_results_in_an_inputs_place(B):
+    """What may be in place is, within one type; anything else would be read after it is overwritten."""
+    L = B.lib()
+    with B.dry_run():
+        assert ln_fwd(L, y=PX) == 0 and ln_fwd(L, y=PX, xt=1) == EINVAL
+        bwd = lambda dx, xt=0: L.sd_layernorm_bwd(PY, 0, PX, xt, PA, PB, None, dx, None, None, 4, 64, None, 0, None)
+        assert bwd(PX) == 0 and bwd(PY) == 0 and bwd(PX, 1) == 0 and bwd(PY, 1) == EINVAL
+        assert rope(B, yq=PX, yk=PZ) == 0 and rope(B, k=PX) == 0 and rope(B, yk=PX, yq=PX, k=None, hk=0) == 0
+        assert rope(B, yq=PZ) == EINVAL and rope(B, yk=PX) == EINVAL and rope(B, yk=PY) == EINVAL
+        assert lin_fwd(L, res=PY) == 0 and lin_fwd(L, z=PZ, res=PY) == 0
+        for kw in (dict(y=PX), dict(y=PW), dict(z=PX), dict(z=PW), dict(z=PY), dict(z=PZ, res=PZ)):
+            assert lin_fwd(L, **kw) == EINVAL, kw
+        lin = lambda dx=PA, dW=PB, db=PC: L.sd_linear_bwd(PY, 0, PX, PW, PZ, 1, dx, dW, 0, db, 4, 8, 64, 1 << 20, 1 << 20, None)
+        assert lin() == 0
+        for at in (PX, PY, PZ, PW):
+            assert lin(dx=at) == EINVAL and lin(dW=at) == EINVAL and lin(db=at) == EINVAL
+
+
+def test_sizes_beyond_a_launch(B):
+    """No launch has 2^32 threads or more, no query of a workspace runs over, and no size loses its upper bits on the way to the C call."""
+    L, top = B.lib(), 2 ** 31 - 1
+    with B.dry_run():
+        assert lin_fwd(L, M=1 << 28) == EUNSUPPORTED and lin_fwd(L, M=(1 << 28) - 1) == 0 and lin_fwd(L, N=1 << 22) == EUNSUPPORTED
+        # 256 + 256 heads of eight pairs of single elements and more: a token for a workgroup
+        many = dict(D=16, pairs=(7,), layout=1, hq=256, hk=256, ldq=4096, ldk=4096, ldyq=4096, ldyk=4096, Bn=1)
+        assert rope(B, T=(1 << 24) - 1, **many) == 0 and rope(B, T=1 << 24, **many) == EUNSUPPORTED
+        assert rope(B, T=top, Bn=1, hq=1, hk=1) == EUNSUPPORTED and rope(B, T=1 << 28, Bn=1, hq=1, hk=1) == 0
+    assert L.sd_linear_bwd_workspace_bytes(top, top, top) == 256 and L.sd_linear_bwd_workspace_bytes((1 << 28) - 1, 8, 8) > 1 << 32
+    assert L.sd_layernorm_bwd_workspace_bytes(top, 16384) > 0
+    B._sizes(0, top)
+    with pytest.raises(ValueError, match="2\\^31"):
+        B._sizes(4, top + 1)
+
+
 def test_linear_bwd_launches(B):
     """Which launches a choice of gradients takes: nothing sums the parts of a product that is not wanted."""
     L = B.lib()
