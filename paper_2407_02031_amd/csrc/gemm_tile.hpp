@@ -466,6 +466,9 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
     // a wavefront that read its second K segment without the producer's flag stores NaN: what it
     // computed from a stale or half-written down-projection must not look like a result
     const float alpha = timed_out ? __builtin_nanf("") : P.alpha;
+    // A large z goes past the caches, which y, that the next call reads, then has to itself: z waits for the backward pass.  (us, the layers of a feed-forward, layer norm and both products, 8192 x 1280
+    // to 5120 287 / 278, 6144 198 / 193, 16384 x 640 to 2560 180 / 175; but 4096 x 1280 to 5120 156 / 174, where the caches hold z too.)
+    const bool z_past = Ext::act && (int64_t)Mp * P.ldy > (24ll << 20);
     int32_t* const sig = std::is_same_v<Ext, GemmPlain> ? P.signal : nullptr;
     // (opaque to the optimiser, which would otherwise widen right after the loads and wait for them there)
 #pragma unroll
@@ -507,20 +510,26 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                 if (bias && P.bias_on_rows) {
                     float br[NPASS];
 #pragma unroll
-                    for (int pass = 0; pass < NPASS; ++pass) br[pass] = bf16_to_f32(bias[p0 + pass * RPP]);
+                    for (int pass = 0; pass < NPASS; ++pass) br[pass] = bf16_to_f32(*as_global(bias + p0 + pass * RPP));
 #pragma unroll
                     for (int pass = 0; pass < NPASS; ++pass) val[pass] += br[pass];
                 }
                 if constexpr (Ext::act) {
                     if (P.z) {
                         uint16_t* const zp = P.z + (int64_t)p0 * P.ldy + q4;
+                        bf16x4 o[NPASS];
 #pragma unroll
-                        for (int pass = 0; pass < NPASS; ++pass) {
-                            bf16x4 o;
+                        for (int pass = 0; pass < NPASS; ++pass)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e] = (__bf16)val[pass][e];
-                            *reinterpret_cast<bf16x4*>(zp + (int64_t)(pass * RPP) * P.ldy) = o;
-                        }
+                            for (int e = 0; e < 4; ++e) o[pass][e] = (__bf16)val[pass][e];
+                        if (z_past) {
+                            asm volatile("");       // (or the two kinds of store are merged into one)
+#pragma unroll
+                            for (int pass = 0; pass < NPASS; ++pass) __builtin_nontemporal_store(o[pass], as_global(reinterpret_cast<bf16x4*>(zp + (int64_t)(pass * RPP) * P.ldy)));
+                            asm volatile("");
+                        } else
+#pragma unroll
+                            for (int pass = 0; pass < NPASS; ++pass) *as_global(reinterpret_cast<bf16x4*>(zp + (int64_t)(pass * RPP) * P.ldy)) = o[pass];
                     }
                     apply_act(P.act - 1, val);
                 }
@@ -532,14 +541,14 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                         const float* rf = static_cast<const float*>(P.res) + (int64_t)p0 * P.ldr + q4;
                         f32x4 r[NPASS];
 #pragma unroll
-                        for (int pass = 0; pass < NPASS; ++pass) r[pass] = *reinterpret_cast<const f32x4*>(rf + (int64_t)(pass * RPP) * P.ldr);
+                        for (int pass = 0; pass < NPASS; ++pass) r[pass] = *as_global(reinterpret_cast<const f32x4*>(rf + (int64_t)(pass * RPP) * P.ldr));
 #pragma unroll
                         for (int pass = 0; pass < NPASS; ++pass) val[pass] += r[pass];
                     } else {
                         const uint16_t* rb = static_cast<const uint16_t*>(P.res) + (int64_t)p0 * P.ldr + q4;
                         u32x2 r[NPASS];
 #pragma unroll
-                        for (int pass = 0; pass < NPASS; ++pass) r[pass] = *reinterpret_cast<const u32x2*>(rb + (int64_t)(pass * RPP) * P.ldr);
+                        for (int pass = 0; pass < NPASS; ++pass) r[pass] = *as_global(reinterpret_cast<const u32x2*>(rb + (int64_t)(pass * RPP) * P.ldr));
 #pragma unroll
                         for (int pass = 0; pass < NPASS; ++pass) {
                             val[pass][0] += bf16lo_to_f32(r[pass][0]); val[pass][1] += bf16hi_to_f32(r[pass][0]);
@@ -550,7 +559,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                 if (y_f32) {
                     float* yp = static_cast<float*>(P.y) + (int64_t)p0 * P.ldy + q4;
 #pragma unroll
-                    for (int pass = 0; pass < NPASS; ++pass) *reinterpret_cast<f32x4*>(yp + (int64_t)(pass * RPP) * P.ldy) = val[pass];
+                    for (int pass = 0; pass < NPASS; ++pass) *as_global(reinterpret_cast<f32x4*>(yp + (int64_t)(pass * RPP) * P.ldy)) = val[pass];
                 } else {
                     uint16_t* yp = static_cast<uint16_t*>(P.y) + (int64_t)p0 * P.ldy + q4;
 #pragma unroll
@@ -563,7 +572,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                             __hip_atomic_store(reinterpret_cast<uint64_t*>(yq), __builtin_bit_cast(uint64_t, o), __ATOMIC_RELAXED,
                                                __HIP_MEMORY_SCOPE_AGENT);
                         else
-                            *reinterpret_cast<bf16x4*>(yq) = o;
+                            *as_global(reinterpret_cast<bf16x4*>(yq)) = o;
                     }
                 }
             } else {
@@ -574,12 +583,12 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                     const int p = m0 + wm + mi * 32 + rr;
                     if (p < Mp && q4 < N) {
                         f32x4 val = *reinterpret_cast<const f32x4*>(stage + rr * EPI_STRIDE + lcol);
-                        if (bias && P.bias_on_rows) val += bf16_to_f32(bias[p]);
+                        if (bias && P.bias_on_rows) val += bf16_to_f32(*as_global(bias + p));
                         if constexpr (Ext::act) {
                             if (P.z)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
-                                    if (q4 + e < N) P.z[(int64_t)p * P.ldy + q4 + e] = __builtin_bit_cast(uint16_t, (__bf16)val[e]);
+                                    if (q4 + e < N) *as_global(P.z + (int64_t)p * P.ldy + q4 + e) = __builtin_bit_cast(uint16_t, (__bf16)val[e]);
                             f32x4 one[1] = {val};
                             apply_act(P.act - 1, one);
                             val = one[0];
@@ -591,12 +600,12 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                             const float* rp = static_cast<const float*>(P.res);
                             if (vec_ok) {
                                 if (RES32 && res_pre) val += rpre[RES32 ? mi : 0][RES32 ? cc : 0][RES32 ? pass : 0];
-                                else if (rp) val += *reinterpret_cast<const f32x4*>(rp + ri);
-                                *reinterpret_cast<f32x4*>(yp) = val;
+                                else if (rp) val += *as_global(reinterpret_cast<const f32x4*>(rp + ri));
+                                *as_global(reinterpret_cast<f32x4*>(yp)) = val;
                             } else {
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
-                                    if (q4 + e < N) yp[e] = val[e] + (rp ? rp[ri + e] : 0.f);
+                                    if (q4 + e < N) *as_global(yp + e) = val[e] + (rp ? *as_global(rp + ri + e) : 0.f);
                             }
                         } else {
                             uint16_t* yp = static_cast<uint16_t*>(P.y) + oi;
@@ -604,16 +613,16 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                             if (P.res_f32 && rp) {      // fp32 residual stream into a bf16 output
                                 const float* rf = static_cast<const float*>(P.res);
                                 if (RES32 && res_pre) val += rpre[RES32 ? mi : 0][RES32 ? cc : 0][RES32 ? pass : 0];
-                                else if (vec_ok) val += *reinterpret_cast<const f32x4*>(rf + ri);
+                                else if (vec_ok) val += *as_global(reinterpret_cast<const f32x4*>(rf + ri));
                                 else
 #pragma unroll
                                     for (int e = 0; e < 4; ++e)
-                                        if (q4 + e < N) val[e] += rf[ri + e];
+                                        if (q4 + e < N) val[e] += *as_global(rf + ri + e);
                                 rp = nullptr;
                             }
                             if (vec_ok) {
                                 if (rp) {
-                                    const u32x2 rv = *reinterpret_cast<const u32x2*>(rp + ri);
+                                    const u32x2 rv = *as_global(reinterpret_cast<const u32x2*>(rp + ri));
                                     val[0] += bf16lo_to_f32(rv[0]); val[1] += bf16hi_to_f32(rv[0]);
                                     val[2] += bf16lo_to_f32(rv[1]); val[3] += bf16hi_to_f32(rv[1]);
                                 }
@@ -624,13 +633,13 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                                     __hip_atomic_store(reinterpret_cast<uint64_t*>(yp), __builtin_bit_cast(uint64_t, o), __ATOMIC_RELAXED,
                                                        __HIP_MEMORY_SCOPE_AGENT);
                                 else
-                                    *reinterpret_cast<bf16x4*>(yp) = o;
+                                    *as_global(reinterpret_cast<bf16x4*>(yp)) = o;
                             } else {
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
                                     if (q4 + e < N) {
-                                        const float f = val[e] + (rp ? bf16_to_f32(rp[ri + e]) : 0.f);
-                                        yp[e] = __builtin_bit_cast(uint16_t, (__bf16)f);
+                                        const float f = val[e] + (rp ? bf16_to_f32(*as_global(rp + ri + e)) : 0.f);
+                                        *as_global(yp + e) = __builtin_bit_cast(uint16_t, (__bf16)f);
                                     }
                             }
                         }

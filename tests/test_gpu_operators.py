@@ -341,7 +341,7 @@ def test_linear_fwd(B, M, N, K, yt):
     assert torch.equal(B.linear_fwd(x, W, bias, 3, residual=res, out=res), ref)
 
 
-@pytest.mark.parametrize("M,N,K", [(4133, 640, 320), (2048, 1280, 648), (8192, 640, 1280), (1976, 1280, 1280), (700, 5120, 640), (4096, 5120, 2056), (9000, 321, 128)])
+@pytest.mark.parametrize("M,N,K", [(4133, 640, 320), (2048, 1280, 648), (8192, 640, 1280), (1976, 1280, 1280), (700, 5120, 640), (4096, 5120, 2056), (9000, 321, 128), (5003, 5160, 64)])
 def test_linear_fwd_large(B, M, N, K):
     import torch
     x, W, bias, g = lin_inputs(M, N, K, M)
