@@ -129,13 +129,14 @@ __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const 
     }
 }
 // How dz is cut.  Few rows: 16 columns and all rows a workgroup, so that no sums of row blocks are left.  Else 512 or 2048 columns, and as many rows as leave two
-// workgroups a CU, 8 to 32.
+// workgroups a CU, 8 to 32.  (us, a whole backward pass to K = 640, few rows / else: 128 x 640 11.0 / 12.4, 300 x 317 12.9 / 13.3, 500 x 1280 17.2 / 19.0, 1003 x 640 17.2 / 17.5, and a launch less; of rows
+// at odd addresses, whose pieces lie in two lines each, 500 x 317 15.7 / 14.5, 1003 x 317 21.6 / 18.0.)
 struct DzCut {
     int ct, nt, rows;
     int64_t col_wgs, blocks;
     DzCut(int64_t M, int64_t N) {
         const int64_t Np = (N + 7) & ~7ll;
-        const bool few = M <= 256 || (M <= 1024 && M * N <= (1 << 20));
+        const bool few = M <= 256 || (M <= (N % 8 ? 384 : 1024) && M * N <= (1 << 20));
         ct = few ? 2 : N > 1024 ? 256 : 64;
         nt = few ? 1024 : 256;
         col_wgs = (Np + ct * 8 - 1) / (ct * 8);
