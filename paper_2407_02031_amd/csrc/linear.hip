@@ -24,7 +24,7 @@ template <class D, bool STORE, bool SUMS, int CT, int NT>
 __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
     constexpr int SUB = NT / CT, BATCH = 4;
     constexpr int PARTS = CT < 64 ? NT / 64 : SUB;          // sums of a column that meet in LDS
-    __shared__ f32x8 sh[PARTS > 1 ? (PARTS - 1) * CT : 1];
+    __shared__ f32x8 sh[(PARTS - 1) * CT];
     const int t = threadIdx.x % CT, sub = threadIdx.x / CT;
     const int cols = (int)blockIdx.x / blocks, block = (int)blockIdx.x - cols * blocks;
     const int c = (cols * CT + t) * 8;
@@ -106,15 +106,13 @@ __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const 
                 }
             part = threadIdx.x >> 6;
         }
-        if constexpr (PARTS > 1) {
-            if (part && (CT >= 64 || (threadIdx.x & 63) < CT)) sh[(part - 1) * CT + t] = sum;
-            __syncthreads();
-            if (threadIdx.x >= CT) return;
+        if (part && (CT >= 64 || (threadIdx.x & 63) < CT)) sh[(part - 1) * CT + t] = sum;
+        __syncthreads();
+        if (threadIdx.x >= CT) return;
 #pragma unroll
-            for (int w = 0; w < PARTS - 1; ++w) {
-                sum.lo += sh[w * CT + t].lo;
-                sum.hi += sh[w * CT + t].hi;
-            }
+        for (int w = 0; w < PARTS - 1; ++w) {
+            sum.lo += sh[w * CT + t].lo;
+            sum.hi += sh[w * CT + t].hi;
         }
         float* const to = sums + (int64_t)block * N + c;
         if (whole) {
@@ -128,8 +126,8 @@ __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const 
         }
     }
 }
-// How dz is cut.  Few rows: 16 columns and all rows a workgroup, so that no sums of row blocks are left.  Else 512 or 2048 columns, and as many rows as leave two
-// workgroups a CU, 8 to 32.  (us, a whole backward pass to K = 640, few rows / else: 128 x 640 11.0 / 12.4, 300 x 317 12.9 / 13.3, 500 x 1280 17.2 / 19.0, 1003 x 640 17.2 / 17.5, and a launch less; of rows
+// How dz is cut.  Few rows: 16 columns and all rows a workgroup, so that no sums of row blocks are left.  Else 512 columns (of 2048 a row's end leaves more idle: dz and a product
+// of 8 columns, 8192 x 2560 54.7 / 47.9 us, 8192 x 1280 33.9 / 30.3) and as many rows as leave two workgroups a CU, 8 to 32.  (us, a whole backward pass to K = 640, few rows / else: 128 x 640 11.0 / 12.4, 300 x 317 12.9 / 13.3, 500 x 1280 17.2 / 19.0, 1003 x 640 17.2 / 17.5, and a launch less; of rows
 // at odd addresses, whose pieces lie in two lines each, 500 x 317 15.7 / 14.5, 1003 x 317 21.6 / 18.0.)
 struct DzCut {
     int ct, nt, rows;
@@ -137,7 +135,7 @@ struct DzCut {
     DzCut(int64_t M, int64_t N) {
         const int64_t Np = (N + 7) & ~7ll;
         const bool few = M <= 256 || (M <= (N % 8 ? 384 : 1024) && M * N <= (1 << 20));
-        ct = few ? 2 : N > 1024 ? 256 : 64;
+        ct = few ? 2 : 64;
         nt = few ? 1024 : 256;
         col_wgs = (Np + ct * 8 - 1) / (ct * 8);
         const int64_t r = M * col_wgs / 512;
@@ -625,8 +623,7 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
         };
         auto by_cut = [&](auto* t) {
             if (cut.ct == 2) run(t, std::integral_constant<int, 2>(), std::integral_constant<int, 1024>());
-            else if (cut.ct == 64) run(t, std::integral_constant<int, 64>(), std::integral_constant<int, 256>());
-            else run(t, std::integral_constant<int, 256>(), std::integral_constant<int, 256>());
+            else run(t, std::integral_constant<int, 64>(), std::integral_constant<int, 256>());
         };
         if (y_dtype == SD_F32) by_cut(static_cast<float*>(nullptr));
         else by_cut(static_cast<__bf16*>(nullptr));
