@@ -10,6 +10,10 @@
 // registers: a mean, then the sums of the deviations and of their squares, of which the first corrects the mean's own
 // rounding.  (One pass over sums and squares loses the variance's digits where a row has a large offset, or one
 // element far from all others.)
+//
+// Measured, 8192 x 1280 fp32 to bf16: forward 13.3 us, 4.7 TB/s, 18.2 from cold inputs (a copy of the same 63 MB, cold: 14.0); backward with
+// gradients of the weights 20.6 and 3.9 for the sums, cold 29.1 in all (a copy of 105 MB 22.3); 2777 x 1155 bf16 11.2 + 3.5.  Stores past the caches
+// make the forward pass 16.4 cold, and the projection behind it slower by more than that.
 #include "rows.hpp"
 
 #include <algorithm>
