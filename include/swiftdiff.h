@@ -330,7 +330,8 @@ int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_d
  *              4-byte aligned; fractions are fine, whole numbers are exact up to 2^24
  *   q, k       device [Bn * T] rows of heads x head_dim elements, ld elements apart (the queries and keys of packed
  *              rows, for instance); heads_k = 0: queries alone (k, yk NULL)
- *   yq, yk     rows like those; may be the same rows as q and k (in place), else they do not overlap them
+ *   yq, yk     rows like those; may be the same rows as q and k (in place, at the same distance: SD_EINVAL at
+ *              another), else they do not overlap them
  * head_dim is a multiple of 8, at most 256, and Bn * T below 2^29, or 2^24 where a token has many heads
  * (SD_EUNSUPPORTED otherwise); ld are multiples of 8. */
 #define SD_ROPE_INTERLEAVED 0

@@ -229,6 +229,8 @@ static int rope(const char* who, float sign, const sd_rope* r, const float* pos,
                "%s: keys need 16-byte aligned pointers and rows of a multiple of 8 elements, %lld at least", who, (long long)wk);
     SD_REQUIRE(heads_q == 0 || heads_k == 0 || (yq != yk && yq != k && yk != q), SD_EINVAL, "%s: a result in the other's place", who);
     a.rows = (int64_t)Bn * T;
+    // (workgroups take their tokens in any order: at another distance a token would be written over one that is still to be read)
+    SD_REQUIRE(a.rows == 1 || ((heads_q == 0 || yq != q || ldyq == ldq) && (heads_k == 0 || yk != k || ldyk == ldk)), SD_EINVAL, "%s: in place with rows at another distance", who);
     SD_REQUIRE(a.rows <= 0x7fffffff, SD_EUNSUPPORTED, "%s: %lld tokens", who, (long long)a.rows);
     a.pos = pos; a.pos_stride = pos_stride; a.q = q; a.k = k; a.yq = yq; a.yk = yk;
     a.ldq = ldq; a.ldk = ldk; a.ldyq = ldyq; a.ldyk = ldyk;

@@ -167,3 +167,18 @@ def test_binding_refuses_what_the_c_call_cannot_see(B):
     for bad in (q.transpose(1, 2), q[:, :4], q[:, ::2][:, :2], q[..., ::2]):
         with pytest.raises(ValueError):
             B._token_rows("q", bad, bad.shape[-1])
+
+
+@pytest.mark.parametrize("bwd", [False, True])
+def test_rope_in_place_keeps_its_distance(B, bwd):
+    """A result in its own argument's place has the argument's distance between tokens, or tokens are overwritten that others have still to read."""
+    f = lambda **kw: rope(B, bwd=bwd, **kw)
+    with B.dry_run():
+        # out of packed rows into dense ones at the same address, and the other way
+        assert f(yq=PX, ldq=1920) == EINVAL and f(yq=PX, ldyq=1920) == EINVAL and b"place" in B.lib().sd_last_error()
+        assert f(yk=PZ, ldk=1920) == EINVAL and f(yk=PZ, ldyk=1920) == EINVAL
+        assert f(Bn=2, T=1, yq=PX, ldq=1920) == EINVAL and f(Bn=1, T=2, yk=PZ, ldk=1920) == EINVAL
+        # at one distance; with one token, which has none; without heads
+        assert f(yq=PX, ldq=1920, ldyq=1920, yk=PZ, ldk=1280, ldyk=1280) == 0
+        assert f(Bn=1, T=1, yq=PX, ldq=1920, yk=PZ, ldk=1920) == 0
+        assert f(hk=0, yk=PZ, ldk=1920) == 0 and f(hq=0, yq=PX, ldq=1920) == 0
