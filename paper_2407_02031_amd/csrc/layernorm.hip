@@ -316,11 +316,11 @@ int launch_sum_partials(const float* partials, int G, float* out0, int n0, float
 // 17.0 / 14.4, but of 256 19.7 / 25.3, 320 25.8 / 27.8: a thread's sums of columns take the registers of the wavefronts that would hide its loads).
 template <int TPR_, int J_, int JW_>
 struct LnShape { static constexpr int TPR = TPR_, J = J_, JW = JW_; };
-template <class F>
-static int ln_by_length(int C, bool backward, F f) {
+template <bool BACKWARD, class F>
+static int ln_by_length(int C, F f) {
     if (C <= 16 * 4) return f(LnShape<16, 1, 0>());
     if (C <= 16 * 4 * 2) return f(LnShape<16, 2, 1>());
-    if (backward) {
+    if constexpr (BACKWARD) {
         if (C <= 64 * 4) return f(LnShape<64, 1, 0>());
     } else {
         if (C <= 16 * 4 * 5) return f(LnShape<16, 5, 2>());
@@ -383,7 +383,7 @@ extern "C" int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* 
     hipStream_t s = static_cast<hipStream_t>(stream);
     return by_type(x_dtype, [&](auto* xt) {
         return by_type(y_dtype, [&](auto* yt) {
-            return ln_by_length(C, false, [&](auto shape) {
+            return ln_by_length<false>(C, [&](auto shape) {
                 using X = std::remove_pointer_t<decltype(xt)>;
                 using Y = std::remove_pointer_t<decltype(yt)>;
                 using S = decltype(shape);
@@ -426,7 +426,7 @@ extern "C" int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, 
     if (!SD_DRY_RUN("layernorm bwd%s; ", few ? " few" : "")) {
         rc = by_type(x_dtype, [&](auto* xt) {
             return by_type(y_dtype, [&](auto* yt) {
-                return ln_by_length(C, true, [&](auto shape) {
+                return ln_by_length<true>(C, [&](auto shape) {
                     using X = std::remove_pointer_t<decltype(xt)>;
                     using D = std::remove_pointer_t<decltype(yt)>;
                     using S = decltype(shape);

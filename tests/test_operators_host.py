@@ -182,3 +182,18 @@ def test_rope_in_place_keeps_its_distance(B, bwd):
         assert f(yq=PX, ldq=1920, ldyq=1920, yk=PZ, ldk=1280, ldyk=1280) == 0
         assert f(Bn=1, T=1, yq=PX, ldq=1920, yk=PZ, ldk=1920) == 0
         assert f(hk=0, yk=PZ, ldk=1920) == 0 and f(hq=0, yq=PX, ldq=1920) == 0
+
+
+def kernel_shapes(name):
+    """(threads a row, chunks, whole chunks) of every instance of a layer norm kernel in the built library"""
+    import re
+    text = open(LIB, "rb").read()
+    # their mangled names: types, then three integers
+    return {tuple(map(int, m)) for m in re.findall(rb"_ZN2sd\d+" + name + rb"I[^E]*?Li(\d+)ELi(\d+)ELi(\d+)E", text)}
+
+
+def test_layernorm_kernels_are_all_launched(B):
+    """Each direction is built for the row lengths that it takes, and for no others."""
+    short, long = {(16, 1, 0), (16, 2, 1)}, {(64, 3, 1), (64, 5, 3), (64, 8, 5), (256, 4, 2), (256, 8, 4), (1024, 4, 2)}
+    assert kernel_shapes(b"ln_fwd_kernel") == short | {(16, 5, 2), (16, 8, 5)} | long
+    assert kernel_shapes(b"ln_bwd_kernel") == kernel_shapes(b"ln_bwd_few_kernel") == short | {(64, 1, 0)} | long
