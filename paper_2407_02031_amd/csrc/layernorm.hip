@@ -89,7 +89,9 @@ __global__ __launch_bounds__(ln_block<TPR>()) void ln_fwd_kernel(const X* x, con
     const int t = threadIdx.x % TPR;
     int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
     const int64_t stride = (int64_t)gridDim.x * RPB;
-    if (row >= M) return;      // (whole wavefronts; a block of one row is never past the end)
+    // Rows leave here and in the loop below at times of their own.  Of 256 threads and more a row, the workgroup is the row, and its barriers are met by all; of 64 a wavefront leaves; of
+    // 16 a quarter of one, and row_sums reads no lane outside it (a wider exchange would read lanes that have left).
+    if (row >= M) return;
     const __bf16* const gb = reinterpret_cast<const __bf16*>(gamma);
     const __bf16* const bb = reinterpret_cast<const __bf16*>(beta);
     f32x4 next[J], v[J], g[J], b[J];
