@@ -131,7 +131,7 @@ struct GemmProblem {
     int64_t ldp0, ldq0, ldp1, ldq1, ldr, ldy;
     int32_t Mp, N;                             // output rows, output columns
     int32_t K0, K1;
-    int32_t geglu_F;                           // > 0: Q has 2F rows (value, gate); N == F
+    int32_t geglu_F;                           // > 0: Q has 2F rows (value, gate); N == F.  < 0: a linear layer (linear, below)
     int32_t y_f32;                             // output dtype: 1 fp32, 0 bf16
     int32_t res_f32;                           // residual dtype (an fp32 stream may be added into a bf16 output)
     int32_t bias_on_rows;                      // 1: bias per row; 2 (launch_gemm16): per column, and y is stored transposed, y[n * ldy + m]
@@ -142,7 +142,7 @@ struct GemmProblem {
     // signal[row-tile index]; its y is bf16 without residual.  wait: before loading K segment 1
     // a tile waits until wait[i] >= wait_need for every row-tile i of the producer that covers
     // its P rows (or its Q rows if wait_cols).  Flags are zero when the launch starts.
-    // (of a linear layer, which neither signals nor waits: where z goes, or null)
+    // (of a linear layer, which neither signals nor waits and which launch_gemm_group refuses: where z goes, or null)
     union { int32_t* signal; uint16_t* z; };
     const int32_t* wait;
     int32_t wait_need;                         // filled by the launcher
@@ -150,11 +150,14 @@ struct GemmProblem {
     // The in-tile form of an adapter (launch_gemm16): p1 is A [K1, K0], q1 is B, and the tile forms
     // t = t_scale * x A^T by itself.
     float t_scale;
-    // filled by the launcher: tiles that wait for one row block.  Of a linear layer (launch_gemm16): its activation, SD_ACT_* + 1; y = act(z) + residual
-    union { int32_t readers; int32_t act; };
+    int32_t readers;                           // filled by the launcher: tiles that wait for one row block
     // nonce != 0: signal and wait are dependency records (dep_record.hpp), one per row-tile index, that need
     // not be zero when the launch starts; at most DEP_PRODUCERS column tiles of producers, wait_cols 0.
     uint64_t nonce;
+    // A linear layer: y = act(z) + residual, act one of SD_ACT_*.  No launcher writes where this is kept.
+    __host__ __device__ bool linear() const { return geglu_F < 0; }
+    __host__ __device__ int act() const { return -1 - geglu_F; }
+    void set_act(int a) { geglu_F = -1 - a; }
 };
 
 constexpr int GEMM_MAX_PROBLEMS = 16;

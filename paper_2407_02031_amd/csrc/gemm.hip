@@ -132,6 +132,7 @@ int launch_gemm_group(GemmGroup& g, hipStream_t stream) {
     for (int i = 0; i < g.n; ++i) geglu = geglu || g.p[i].geglu_F > 0;
     for (int i = 0; i < g.n; ++i) {
         const GemmProblem& P = g.p[i];
+        SD_REQUIRE(!P.linear(), SD_EINVAL, "gemm problem %d: a linear layer", i);
         SD_REQUIRE((P.geglu_F > 0) == geglu || P.signal, SD_EINVAL, "gemm group mixes GEGLU and plain problems");
         SD_REQUIRE(P.Mp >= 0 && P.N >= 0 && P.K0 > 0 && P.K0 % 8 == 0 && P.K1 >= 0 && P.K1 % 8 == 0, SD_EINVAL,
                    "gemm problem %d: bad sizes M=%d N=%d K0=%d K1=%d", i, P.Mp, P.N, P.K0, P.K1);

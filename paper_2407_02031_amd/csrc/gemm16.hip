@@ -378,7 +378,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * WGK, 2) void gemm16_kernel(const G
         }
     }
     // A linear layer: z is kept and its activation takes the product's place, and there is no bias left to add.
-    if (NRB == 0 && P.act) {
+    if (NRB == 0 && P.linear()) {
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) {
             f32x4 v[ME];
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * WGK, 2) void gemm16_kernel(const G
                     *as_global(reinterpret_cast<bf16x4*>(P.z + (int64_t)(mrow + mi * 16) * ldy + ncol + ni * 16)) = o;
                 }
             }
-            apply_act(P.act - 1, v);
+            apply_act(P.act(), v);
 #pragma unroll
             for (int mi = 0; mi < ME; ++mi) fin[mi][ni] = v[mi];
             bias[ni] = u32x2{0u, 0u};
@@ -519,7 +519,7 @@ static int tile16(const GemmGroup& g) {
         lead += (long)((P.Mp + 127) / 128) * ((P.K1 + 63) / 64);
         for (int i = 0; i < 2; ++i) thin[i] += (long)((P.Mp + 31) / 32) * (P.N / (32 << i));
         thin[2] += (long)((P.Mp + 63) / 64) * P.N;             // (columns: how many a tile has is up to the largest rank)
-        thin_ok = thin_ok && P.N % 64 == 0 && (!P.bias || P.res || P.y_f32 || P.act);
+        thin_ok = thin_ok && P.N % 64 == 0 && (!P.bias || P.res || P.y_f32 || P.linear());
         rmax = P.K1 > rmax ? P.K1 : rmax;
         kmax = P.K0 > kmax ? P.K0 : kmax;
         nmax = P.N > nmax ? P.N : nmax;
@@ -542,6 +542,8 @@ int launch_gemm16(GemmGroup& g, hipStream_t stream) {
     for (int i = 0; i < g.n; ++i) {
         rmax = g.p[i].K1 > rmax ? g.p[i].K1 : rmax;
         kmax = g.p[i].K0 > kmax ? g.p[i].K0 : kmax;
+        // (an activation is in the kernels without adapter, and z is in a signal's place)
+        SD_REQUIRE(!g.p[i].linear() || (g.n == 1 && g.p[i].K1 == 0 && !g.p[i].wait && !g.p[i].nonce), SD_EINVAL, "gemm16: a linear layer beside another problem or with an adapter");
     }
     const int tile = tile16(g);
     switch (tile) {

@@ -201,7 +201,7 @@ __global__ __launch_bounds__(512, 2) void gemm_thin_kernel(const GemmGroup g) {
         v[1] = P.alpha * v[1] + bf16hi_to_f32(bias[i][0]);
         v[2] = P.alpha * v[2] + bf16lo_to_f32(bias[i][1]);
         v[3] = P.alpha * v[3] + bf16hi_to_f32(bias[i][1]);
-        if (RT == 0 && P.act) {       // a linear layer's activation, and z kept
+        if (RT == 0 && P.linear()) {       // a linear layer's activation, and z kept
             if (P.z && mrow < Mp && ncol < N) {
                 bf16x4 o;
 #pragma unroll
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(512, 2) void gemm_thin_kernel(const GemmGroup g) {
                 *as_global(reinterpret_cast<bf16x4*>(P.z + (int64_t)mrow * P.ldy + ncol)) = o;
             }
             f32x4 one[1] = {v};
-            apply_act(P.act - 1, one);
+            apply_act(P.act(), one);
             v = one[0];
         }
         if (RES == THIN_F32) v += resf[i];

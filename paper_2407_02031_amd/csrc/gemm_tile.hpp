@@ -531,7 +531,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
 #pragma unroll
                             for (int pass = 0; pass < NPASS; ++pass) *as_global(reinterpret_cast<bf16x4*>(zp + (int64_t)(pass * RPP) * P.ldy)) = o[pass];
                     }
-                    apply_act(P.act - 1, val);
+                    apply_act(P.act(), val);
                 }
                 if (P.res) {
                     if (RES32 && res_pre) {
@@ -590,7 +590,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
                                 for (int e = 0; e < 4; ++e)
                                     if (q4 + e < N) *as_global(P.z + (int64_t)p * P.ldy + q4 + e) = __builtin_bit_cast(uint16_t, (__bf16)val[e]);
                             f32x4 one[1] = {val};
-                            apply_act(P.act - 1, one);
+                            apply_act(P.act(), one);
                             val = one[0];
                         }
                         const int64_t oi = (int64_t)p * P.ldy + q4;

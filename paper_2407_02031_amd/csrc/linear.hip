@@ -561,7 +561,7 @@ extern "C" int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_
     // 17.9 / 14.8.)
     const int f32 = y_dtype == SD_F32;
     if (M <= 16) return launch_rows<1, 1, 6>(x, W, bias, act, residual, y, f32, z, M, N, K, s);
-    P.act = act + 1;
+    P.set_act(act);
     P.z = z;
     if (gemm16_takes(g)) return launch_gemm16(g, s);
     const int64_t r32 = (M + 31) / 32, r64 = (M + 63) / 64, c16 = (N + 15) / 16, c32 = (N + 31) / 32;

@@ -197,3 +197,37 @@ def test_layernorm_kernels_are_all_launched(B):
     short, long = {(16, 1, 0), (16, 2, 1)}, {(64, 3, 1), (64, 5, 3), (64, 8, 5), (256, 4, 2), (256, 8, 4), (1024, 4, 2)}
     assert kernel_shapes(b"ln_fwd_kernel") == short | {(16, 5, 2), (16, 8, 5)} | long
     assert kernel_shapes(b"ln_bwd_kernel") == kernel_shapes(b"ln_bwd_few_kernel") == short | {(64, 1, 0)} | long
+
+
+class GemmProblem(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("p0", "q0", "p1", "q1", "bias", "res", "y")] + [(n, C.c_int64) for n in ("ldp0", "ldq0", "ldp1", "ldq1", "ldr", "ldy")] +
+                [(n, C.c_int32) for n in ("Mp", "N", "K0", "K1", "geglu_F", "y_f32", "res_f32", "bias_on_rows")] + [("alpha", C.c_float)] +
+                [(n, C.c_int32) for n in ("tile_begin", "tiles_m", "tiles_n")] + [(n, C.c_void_p) for n in ("signal_or_z", "wait")] +
+                [(n, C.c_int32) for n in ("wait_need", "wait_cols")] + [("t_scale", C.c_float), ("readers", C.c_int32), ("nonce", C.c_uint64)])
+
+
+class GemmGroup(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "total_tiles", "n_lead", "zero_n")] + [("zero_ptr", C.c_void_p), ("first_tile", C.c_int32 * 16), ("p", GemmProblem * 16)]
+
+
+def test_linear_layers_and_projections_keep_apart(B):
+    """A linear layer keeps z where a projection keeps its signal: neither is launched as the other, whatever a launcher has written into the group."""
+    L = B.lib()
+    assert C.sizeof(GemmProblem) == 192
+
+    def launch(name, *problems):
+        g = GemmGroup(n=len(problems))
+        for i, kw in enumerate(problems):
+            for k, v in dict(dict(p0=PX, q0=PW, y=PY, ldp0=640, ldq0=640, ldy=320, Mp=256, N=320, K0=640, alpha=1.0), **kw).items():
+                setattr(g.p[i], k, v)
+        with B.dry_run() as names:
+            rc = getattr(L, name)(C.byref(g), None)
+        return rc, names
+    group, g16 = "_ZN2sd17launch_gemm_groupERNS_9GemmGroupEP12ihipStream_t", "_ZN2sd13launch_gemm16ERNS_9GemmGroupEP12ihipStream_t"
+    gelu = dict(geglu_F=-2, signal_or_z=PZ)
+    assert launch(g16, gelu)[0] == 0 and launch(g16, {})[0] == 0 and launch(group, {})[0] == 0
+    assert launch(group, gelu)[0] == EINVAL and b"linear layer" in L.sd_last_error()
+    adapter = dict(p1=PA, q1=PB, ldp1=16, ldq1=16, K1=16)
+    assert launch(g16, adapter)[0] == 0 and launch(g16, dict(gelu, **adapter))[0] == EINVAL and launch(g16, gelu, adapter)[0] == EINVAL
+    # a projection that the general launcher has been through: readers and tiles written, still no activation
+    assert launch(g16, dict(readers=3, tiles_m=2, tiles_n=3)) == launch(g16, {})
