@@ -366,7 +366,8 @@ int sd_rope_bwd(const sd_rope* r, const float* pos, int64_t pos_stride, const vo
  *             aliases an input.
  *   The products multiply dz in bf16 (rounded once) and sum in fp32; dbias sums dz as it was before.  All sums
  *   are in a fixed order.
- * K is a multiple of 8, M below 2^28, N and K below 2^22 (SD_EUNSUPPORTED otherwise). */
+ * K is a multiple of 8, M below 2^28, N and K below 2^22; with M = 0 or N = 0, dx and dW (cleared) together below 2^34
+ * elements (SD_EUNSUPPORTED otherwise). */
 int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int32_t act, const void* residual, void* y, int32_t y_dtype, uint16_t* z,
                   int32_t M, int32_t N, int32_t K, void* stream);
 size_t sd_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K);

@@ -199,6 +199,7 @@ __global__ __launch_bounds__(256) void part_sums_kernel(const PartSums a) {
 static Parts parts_of(const float* parts, void* out, bool f32, int64_t n, int count) { return Parts{parts, out, n, count, f32, (int32_t)((n / 4 + 255) / 256)}; }
 static int launch_part_sums(PartSums& a, hipStream_t stream) {
     const int64_t wgs = (int64_t)a.m[0].wgs + a.m[1].wgs + (a.dbias ? (a.N + 15) / 16 : 0);
+    SD_REQUIRE(wgs < (1 << 24), SD_EUNSUPPORTED, "linear_bwd: gradients of 2^34 elements and more in parts, or of nothing");      // (threads of a launch stay below 2^32)
     if (wgs == 0 || SD_DRY_RUN("part sums; ")) return SD_OK;
     hipLaunchKernelGGL(part_sums_kernel, dim3((unsigned)wgs), dim3(256), 0, stream, a);
     SD_HIP_CHECK(hipGetLastError());

@@ -231,3 +231,13 @@ def test_linear_layers_and_projections_keep_apart(B):
     assert launch(g16, adapter)[0] == 0 and launch(g16, dict(gelu, **adapter))[0] == EINVAL and launch(g16, gelu, adapter)[0] == EINVAL
     # a projection that the general launcher has been through: readers and tiles written, still no activation
     assert launch(g16, dict(readers=3, tiles_m=2, tiles_n=3)) == launch(g16, {})
+
+
+def test_sums_over_nothing_beyond_a_launch(B):
+    """Gradients without a row to sum over are cleared by as many threads as a launch has, or refused."""
+    L = B.lib()
+    zeros = lambda M, N, K, **kw: L.sd_linear_bwd(None, 0, None, None, None, 0, kw.get("dx"), kw.get("dW"), 0, None, M, N, K, None, 0, None)
+    with B.dry_run() as names:
+        assert zeros((1 << 24) - 1, 0, 1024, dx=PA) == 0 and zeros(1 << 24, 0, 1024, dx=PA) == EUNSUPPORTED
+        assert zeros(0, (1 << 22) - 1, 4096, dW=PA) == 0 and zeros(0, (1 << 22) - 1, 4104, dW=PA) == EUNSUPPORTED
+    assert names == ["part sums"] * 2
