@@ -699,3 +699,75 @@ def test_two_streams_at_once(B):
     for o, w in zip(got, want):
         for r in o:
             assert all(torch.equal(a, b) for a, b in zip(r, w))
+
+
+# ---- every shape and loop of the row kernels -------------------------------------------------------------------------------
+# both sides of every length at which a kernel ends, and lengths inside that four elements do not divide
+BORDERS = [64, 65, 66, 100, 127, 128, 129, 254, 258, 319, 320, 321, 333, 511, 512, 513, 767, 769, 1279, 1281, 2047, 4094, 4097, 8190]
+TYPES = [("float32", "bfloat16"), ("bfloat16", "bfloat16"), ("float32", "float32"), ("bfloat16", "float32")]
+
+
+@pytest.mark.parametrize("C", BORDERS)
+def test_layernorm_borders(B, C):
+    for xt, yt in TYPES:
+        test_layernorm_fwd(B, C, xt, yt)
+        test_layernorm_bwd(B, C, xt, yt)
+
+
+@pytest.mark.parametrize("M,C", [(40003, 64), (33001, 63), (33001, 128), (40003, 100), (20001, 320), (33001, 319), (20001, 512), (16385, 333), (8195, 768), (4101, 515), (8195, 1280), (4097, 1155),
+                                 (8195, 1283), (5003, 2048), (2051, 4096), (1030, 4095), (2051, 8192), (1030, 5001), (1030, 8193), (2051, 10001), (1030, 16384)])
+def test_layernorm_fwd_rows_in_turn(B, M, C):
+    """More rows than a launch has places for (1024 workgroups of 16, 4 or 1 rows): two rounds and more, of which the last is not full."""
+    import torch
+    for xt, yt in (TYPES[0], TYPES[1]) if C != 1280 else TYPES:
+        x, ga, be, _ = ln_inputs(M, C, getattr(torch, xt), C + M)
+        check_ln_fwd(B, x, ga, be, getattr(torch, yt))
+
+
+@pytest.mark.parametrize("M,C", [(40003, 64), (33001, 63), (40003, 128), (33001, 101), (9001, 256), (8201, 131), (9001, 768), (8201, 515), (5003, 1280), (4101, 1283), (5003, 2048), (1100, 4096), (1031, 5000),
+                                 (2051, 8192), (1100, 8193), (600, 16384)])
+def test_layernorm_bwd_rows_in_turn(B, M, C):
+    """The same backwards, with gradients of the weights (256 or 512 workgroups) and without (512 or 1024)."""
+    import torch
+    for xt, yt in (TYPES[0], TYPES[1]) if C != 1280 else TYPES:
+        x, ga, be, g = ln_inputs(M, C, getattr(torch, xt), C + M)
+        dy = torch.randn(M, C, generator=g, device="cuda").to(getattr(torch, yt))
+        _, mean, rstd = B.layernorm_fwd(x, ga, be, stats=True)
+        check_ln_bwd(B, x, dy, ga, mean, rstd)
+
+
+@pytest.mark.parametrize("dt", ["bfloat16", "float32"])
+@pytest.mark.parametrize("layout", [0, 1, 2])
+@pytest.mark.parametrize("Bn,T,Hq,Hk,D,pairs", [(4500, 1, 1, 0, 64, (16, 8)), (5003, 3, 1, 1, 24, (3, 4)), (1, 33001, 1, 0, 8, (4,)), (1, 40009, 1, 0, 8, (1, 2)), (1, 5003, 2, 1, 40, (3, 7)), (3, 701, 2, 2, 128, (16, 24)),
+                                                (700, 7, 3, 1, 64, (13, 18))])
+def test_rope_tokens_of_a_workgroup(B, Bn, T, Hq, Hk, D, pairs, layout, dt):
+    """Several tokens a workgroup, from 2 to 32, of one sample or of many; one unit a token; heads with a rest that is not turned; single elements."""
+    rope_case(B, Bn, T, Hq, Hk, D, pairs, layout, dt=dt, seed=D + T)
+
+
+@pytest.mark.parametrize("M,N,K", [(129, 317, 648), (300, 512, 1024), (2100, 320, 136), (4133, 645, 320)])
+def test_linear_bwd_rounds_dz_once_and_nothing_else(B, M, N, K):
+    """Where dz needs no rounding the products have none but their sums'; where it does, theirs is the product of the rounded dz."""
+    import torch
+    x, W, bias, g = lin_inputs(M, N, K, M + N)
+    xd, wd = x.double(), W.double()
+    dy = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    z = (1.5 * torch.randn(M, N, generator=g, device="cuda")).bfloat16()
+    # relu's slope is 0 or 1; fp32 gradients that bf16 holds
+    for d, act, dz in ((dy, 4, torch.where(z > 0, dy, 0).double()), (dy.float(), 4, torch.where(z > 0, dy, 0).double()), (dy.float(), 0, dy.double()), (dy, 0, dy.double())):
+        dx, dW, db = B.linear_bwd(d, x, W, z if act else None, act, dw_dtype=torch.float32)
+        within(dx, dz @ wd, (N + 8) * U * (dz.abs() @ wd.abs()))
+        within(dW, dz.T @ xd, (M + 8) * U * (dz.abs().T @ xd.abs()))
+        within(db, dz.sum(0), (M / 64 + 40) * U * dz.abs().sum(0))
+        # every addition is off by U of the sum so far, whose norm over all elements is no more than the whole's
+        assert float((dW.double() - dz.T @ xd).norm() / (dz.T @ xd).norm()) <= (M + 8) * U
+    for d, act in ((torch.randn(M, N, generator=g, device="cuda"), 0), (dy, 1), (dy, 2), (dy.float(), 3)):
+        zz = z.double().requires_grad_(True)
+        dz = torch.autograd.grad(act64(zz, act), zz, d.double())[0] if act else d.double()
+        r = dz.bfloat16().double()
+        dW = B.linear_bwd(d, x, W, z if act else None, act, dw_dtype=torch.float32)[1].double()
+        # fp32's error e <= (1e-6 or U) |dy| takes dz over a tie, and so one step (2^-7 |dz| at most) the other way, with probability 2 e / step: the mean square of that is
+        # below 2 e 2^-7 |dz|.  x is independent of it, so that the product's error has the same ratio to the product; twice that.  The sums as above.
+        flips = math.sqrt(float((2 * (1e-6 if act else U) * 2.0 ** -7 * d.double().abs() * dz.abs()).sum())) / float(dz.norm())
+        off = float((dW - r.T @ xd).norm() / (dz.T @ xd).norm())
+        assert off <= 2 * flips + (M + 8) * U < 2.0 ** -10, (act, off, flips)
