@@ -86,6 +86,14 @@ constexpr int gemm_min_waves() {
     return gemm_lds_chunks<BM, BN, BK, WGM, WGN, STAGES>() * 16 <= 80 * 1024 ? 2 : 1;
 }
 
+// 16-column blocks of a wavefront that the epilogue stages and stores at a time, of `nout` that it has
+constexpr int gemm_pass_blocks(int nout) { return nout % 4 == 0 ? 4 : nout % 2 == 0 ? 2 : 1; }
+// A linear layer's large z goes past the caches, which y, that the next call reads, then has to itself: z waits for the backward pass.  (us, the layers of a feed-forward, layer norm and both products,
+// 8192 x 1280 to 5120 287 / 278, 6144 198 / 193, 16384 x 640 to 2560 180 / 175; but 4096 x 1280 to 5120 156 / 174, where the caches hold z too.)  Passes of 64 columns write whole lines
+// of it; those of 16, which the 128x160 tiles' wavefronts have, do not, and then the caches have to join them (past / through them: 42496x960x320 131 / 82, 88576x320x1280 149 / 125).
+template <int NOUT>
+__host__ __device__ constexpr bool gemm_z_past(int64_t rows, int64_t ldy) { return gemm_pass_blocks(NOUT) == 4 && rows * ldy > (24ll << 20); }
+
 template <int BM, int BN, int BK, int WGM, int WGN, int STAGES, bool GEGLU, bool GUARD, bool RES32, class Ext>
 __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, u32x4* const lds, const Ext) {
     constexpr int NW = WGM * WGN;
@@ -393,7 +401,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
     // whole row pieces: lane handles 4 consecutive columns (lcol) of row lr, lr + RPP, ... of the piece.  (Stored from where they are, 32 or 64 bytes
     // of a row at a time: 8192x1920x640 + 64 39 -> 44 us, 2048x1280x1280 + 64 with an fp32 residual 20.1 -> 21.9.)
     constexpr int NOUT = GEGLU ? NI / 2 : NI;   // 16-column output blocks per wave
-    constexpr int CB = NOUT % 4 == 0 ? 4 : NOUT % 2 == 0 ? 2 : 1;   // ... staged per pass (<= 64 columns)
+    constexpr int CB = gemm_pass_blocks(NOUT);  // ... staged per pass (<= 64 columns)
     constexpr int CCOLS = CB * 16;              // staged columns
     constexpr int LPR = CCOLS / 4;              // lanes per staged row (4 columns each)
     constexpr int RPP = 64 / LPR;               // rows per pass
@@ -466,9 +474,7 @@ __device__ __forceinline__ void gemm_tile(const GemmProblem& P, const int tile, 
     // a wavefront that read its second K segment without the producer's flag stores NaN: what it
     // computed from a stale or half-written down-projection must not look like a result
     const float alpha = timed_out ? __builtin_nanf("") : P.alpha;
-    // A large z goes past the caches, which y, that the next call reads, then has to itself: z waits for the backward pass.  (us, the layers of a feed-forward, layer norm and both products, 8192 x 1280
-    // to 5120 287 / 278, 6144 198 / 193, 16384 x 640 to 2560 180 / 175; but 4096 x 1280 to 5120 156 / 174, where the caches hold z too.)
-    const bool z_past = Ext::act && (int64_t)Mp * P.ldy > (24ll << 20);
+    const bool z_past = Ext::act && gemm_z_past<NOUT>(Mp, P.ldy);
     int32_t* const sig = std::is_same_v<Ext, GemmPlain> ? P.signal : nullptr;
     // (opaque to the optimiser, which would otherwise widen right after the loads and wait for them there)
 #pragma unroll

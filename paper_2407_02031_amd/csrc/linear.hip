@@ -216,7 +216,8 @@ static int launch_act(GemmGroup& g, hipStream_t stream) {
     P.tiles_n = (P.N + BN - 1) / BN;
     g.total_tiles = P.tiles_m * P.tiles_n;
     const bool guard = P.K0 % 64 != 0;
-    if (SD_DRY_RUN("gemm act %dx%d/%d waves/%d stages%s; ", BM, BN, WGM * WGN, STAGES, guard ? " guard" : "")) return SD_OK;
+    if (SD_DRY_RUN("gemm act %dx%d/%d waves/%d stages%s%s; ", BM, BN, WGM * WGN, STAGES, guard ? " guard" : "", P.z && gemm_z_past<BN / WGN / 16>(P.Mp, P.ldy) ? dry_detail(", z past the caches") : ""))
+        return SD_OK;
     const dim3 grid((g.total_tiles + 7) & ~7), block(64 * WGM * WGN);
     if (guard) hipLaunchKernelGGL((gemm_kernel<BM, BN, 64, WGM, WGN, STAGES, false, true, false, GemmAct>), grid, block, 0, stream, g, GemmAct{});
     else hipLaunchKernelGGL((gemm_kernel<BM, BN, 64, WGM, WGN, STAGES, false, false, false, GemmAct>), grid, block, 0, stream, g, GemmAct{});

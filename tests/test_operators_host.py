@@ -241,3 +241,18 @@ def test_sums_over_nothing_beyond_a_launch(B):
         assert zeros((1 << 24) - 1, 0, 1024, dx=PA) == 0 and zeros(1 << 24, 0, 1024, dx=PA) == EUNSUPPORTED
         assert zeros(0, (1 << 22) - 1, 4096, dW=PA) == 0 and zeros(0, (1 << 22) - 1, 4104, dW=PA) == EUNSUPPORTED
     assert names == ["part sums"] * 2
+
+
+def test_z_past_the_caches(B):
+    """A z above 24 Mi elements, and only from tiles that store whole lines of it."""
+    L = B.lib()
+
+    def name(M, N, K, z=PZ):
+        with B.dry_run(True) as n:
+            assert lin_fwd(L, M=M, N=N, K=K, z=z) == 0
+        return n[0]
+    past = ", z past the caches"
+    assert name(8192, 5120, 1280) == "gemm act 128x256/8 waves/3 stages" + past and name(49152, 640, 2560) == "gemm act 256x128/8 waves/3 stages" + past
+    assert name(8192, 5120, 1280, None) == "gemm act 128x256/8 waves/3 stages" and past not in name(4096, 3840, 1280)
+    for M, N, K in ((42496, 960, 320), (42496, 960, 1280), (88576, 320, 320), (88576, 320, 1280)):
+        assert M * N > 24 << 20 and name(M, N, K) == "gemm act 128x160/4 waves/2 stages"
