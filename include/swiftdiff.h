@@ -364,8 +364,9 @@ int sd_rope_bwd(const sd_rope* r, const float* pos, int64_t pos_stride, const vo
  *   dx        device [M, K] bf16, dW device [N, K] bf16 or fp32 (dw_dtype), dbias device [N] fp32; each
  *             overwritten, or NULL: not wanted (x and W may be NULL where nothing needs them).  None of them
  *             aliases an input.
- *   The products multiply dz in bf16 (rounded once) and sum in fp32; dbias sums dz as it was before.  All sums
- *   are in a fixed order.
+ *   The products multiply dz in bf16 and sum in fp32; dbias sums dz as it was before.  That one rounding, 2^-8 of a
+ *   term at most, is there whatever the types of dy and dW (of an fp32 dW it is the larger part of the error), but
+ *   not where bf16 holds dz as it is.  All sums are in a fixed order.
  * K is a multiple of 8, M below 2^28, N and K below 2^22; with M = 0 or N = 0, dx and dW (cleared) together below 2^34
  * elements (SD_EUNSUPPORTED otherwise). */
 int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int32_t act, const void* residual, void* y, int32_t y_dtype, uint16_t* z,

@@ -397,7 +397,8 @@ def _scratch(x: torch.Tensor, nbytes: int, ws: Optional[torch.Tensor], dev: int)
 
 
 def layernorm_fwd(x: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, out_dtype=torch.bfloat16, stats: bool = False, out=None):
-    """Layer norm over the last axis of x [..., C], bf16 or fp32; y, or with `stats` (y, mean, rstd) for layernorm_bwd."""
+    """Layer norm over the last axis of x [..., C], bf16 or fp32; y, or with `stats` (y, mean, rstd) for layernorm_bwd.  (As of all
+    calls here, autograd records nothing of it: a gradient is the caller's call of layernorm_bwd.)"""
     dev, shape = _on(x), x.shape
     Cc = shape[-1]
     M = x.numel() // Cc if Cc else 0
@@ -502,7 +503,8 @@ def _rope(fn, rope: Rope, pos: torch.Tensor, q: torch.Tensor, k, q_out, k_out):
 
 def rope_fwd(rope: Rope, pos: torch.Tensor, q: torch.Tensor, k=None, q_out=None, k_out=None):
     """Queries and keys [Bn, T, heads, head_dim] turned by their positions [T, axes], [1, T, axes] or [Bn, T, axes].  They may be
-    views into the rows of a packed projection; the results may be given, the arguments themselves among them."""
+    views into the rows of a packed projection; the results may be given, the arguments themselves among them, but not other rows
+    that overlap them.  Autograd records nothing."""
     return _rope(_lib.sd_rope_fwd, rope, pos, q, k, q_out, k_out)
 
 
@@ -512,7 +514,7 @@ def rope_bwd(rope: Rope, pos: torch.Tensor, dq: torch.Tensor, dk=None, q_out=Non
 
 
 def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_NONE, residual=None, out_dtype=torch.bfloat16, save_z: bool = False, out=None):
-    """act(x W^T + bias) + residual for x [M, K]; with `save_z` (y, z), z for linear_bwd."""
+    """act(x W^T + bias) + residual for x [M, K]; with `save_z` (y, z), z for linear_bwd.  Autograd records nothing."""
     dev = _on(x)
     M, K = x.shape
     N = W.shape[0]
@@ -533,7 +535,7 @@ def linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_NO
 
 def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: int = SD_ACT_NONE, grads: Sequence[bool] = (True, True, True),
                dw_dtype=torch.bfloat16, ws=None):
-    """(dx, dW, dbias) of linear_fwd, each None where `grads` does not ask for it."""
+    """(dx, dW, dbias) of linear_fwd, each None where `grads` does not ask for it.  dx and dW are products of dy act'(z) rounded to bf16."""
     dev = _on(x)
     M, K = x.shape
     N = W.shape[0]

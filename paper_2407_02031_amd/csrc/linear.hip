@@ -7,9 +7,11 @@
 // whose rows are the reduction's, which the transposing LDS read turns on the way into the registers, so that nothing is
 // transposed in memory.  dz is formed once, in front of the products, by a kernel that sums its columns in fp32 too.
 //
-// Measured, 8192 rows, N = 5120, K = 1280: forward with GELU and z kept 121 to 130 us, 820 to 890 TFLOP/s; backward dz 48 us (252 MB, 5.3 TB/s), both products 193
-// (215 GFLOP, 1110 TFLOP/s), what they left in parts 5.  1976 rows, N = 1280, K = 5120, fp32 with residual 36 us, 710 TFLOP/s: bound by what a CU
-// draws of its one tile's operands.  One row, N = 5120, K = 1280 5.6 us, 2.3 TB/s: a launch and one trip to HBM.
+// Measured (kernels alone, three sets of inputs in turn; least and mean), 8192 rows, N = 5120, K = 1280: forward with GELU and z kept 115 to 121 us, 890 to 940 TFLOP/s; backward dz 47 to
+// 50 us (252 MB, 5.0 to 5.4 TB/s), both products 192 to 208 (215 GFLOP, 1030 to 1120 TFLOP/s), what they left in parts 5.  1976 rows, N = 1280, K = 5120, fp32 with residual 37 to 39 us,
+// 660 to 690 TFLOP/s: bound by what a CU draws of its one tile's operands.  One row, N = 5120, K = 1280 5.6 to 5.9 us, 2.2 to 2.3 TB/s: a launch and one trip to HBM.
+// Backward of few rows, N = 5120, K = 1280, cold: 1 row 21.4 us (dx alone 13.8), 16 22.1, 64 24.0, 128 26.9: the weights come in and their gradient goes out at 1.1 to 1.2 TB/s, behind dz and
+// ahead of the sum of dx's parts.
 #include "gemm_tile.hpp"
 #include "rows.hpp"
 
@@ -21,8 +23,9 @@ namespace sd {
 // ---------------------------------------------------------------------------------------
 // dz and its column sums.  Bound by HBM (dy and z in, dz out).  CT threads have eight columns each; the NT / CT groups of them take rows in turn, four at
 // a time in flight.  The sums of a workgroup's rows go to sums[row block] (where there is one row block, to the result itself).
-// dz is rounded to bf16, which is what the matrix cores multiply (the sums are of what it was before); its rows are Np elements
-// long, N rounded up to a multiple of 8, with zeros behind N.
+// dz is rounded to bf16, once, whatever the types of dy and of dW (the sums are of what it was before): that is what the matrix cores multiply with x and W, which are bf16 themselves.  It
+// is off by up to 2^-8 of each term; against 64 bits a bf16 gradient's error grows from 0.0017 of it, its own rounding, to 0.0023, and an fp32 dW has 0.0017 of it.  Two bf16 halves of dz would
+// take both products twice (192 us more for 8192 x 5120 x 1280).  Its rows are Np elements long, N rounded up to a multiple of 8, with zeros behind N.
 // ---------------------------------------------------------------------------------------
 template <class D, bool STORE, bool SUMS, int CT, int NT>
 __global__ __launch_bounds__(NT) void dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
@@ -224,9 +227,12 @@ static int launch_act(GemmGroup& g, hipStream_t stream) {
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }
-// Tiles of a linear layer with more of them than one round of small ones: what the launch takes is its rounds times what a round takes, us, from fits of 49
-// launches of 1000 to 16384 rows (within 10 %, cold; each of the five is the fastest of some by 10 % or more: 2960x1280x5120 in 64x128 74, 128x128 88, 128x256 80; 6100x1920x640 36,
-// 37, 39; 8192x1280x5120 in 128x160 131, 128x256 165; 4096x1280x5120 103, 88; 8192x1920x640 in 256x128 40, 128x128 44, 128x256 51).
+// Tiles of a linear layer with more of them than one round of small ones: the launch is taken to last its rounds times what a round takes, us, a first part and a part for every step of 64.
+// Each of the five is the fastest of some launches (us, z kept, cold, it / the next: 64x128 4096x640x2560 44.0 / 50.3, 128x128 16384x1920x640 67.4 / 73.3, 128x160 8192x1280x5120 130 /
+// 164, 256x128 8192x1920x640 40.2 / 43.7, 128x256 2960x5120x1280 52.6 / 56.5).  Of 49 launches of 1000 to 16384 rows 38 get the fastest or one within 3 % of it; the mean of all is 2 %
+// above.  The others are those that the model knows too little of: it has no term for the bytes of y and z, which count where K is short, and takes 128x256 and 256x128 for nearly the
+// same (taken / fastest: 8192x1920x640 128x256 50.6 / 40.2, 16384x1920x640 128x256 80.8 / 67.4, 2960x1920x640 128x256 23.7 / 21.1, 8192x5120x1280 128x256 138 / 130, 16384x1280x1280 128x160
+// 85.8 / 80.2).
 static int launch_large(GemmGroup& g, hipStream_t stream) {
     struct Tile { int bm, bn, slots; float step, rest; };
     static const Tile tiles[5] = {{64, 128, 512, 0.85f, 4.f}, {128, 128, 512, 1.12f, 7.f}, {128, 160, 512, 1.45f, 9.f}, {256, 128, 256, 1.02f, 6.f}, {128, 256, 256, 1.0f, 6.f}};

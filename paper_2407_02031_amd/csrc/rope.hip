@@ -9,8 +9,9 @@
 // them.  Angles are reduced in 64 bits, as turns, whose whole part falls away exactly: in fp32 position 10^5 would be off by
 // 2^-24 10^5 = 6e-3 turns' radians and more.
 //
-// Measured: 12844 tokens of 32 heads x 128 fp32 75.4 us, 5.6 TB/s; 8192 tokens of 40 heads x 64 bf16 in packed rows 16.5 us, 5.1 TB/s, 22.9 from
-// cold inputs for 84 MB (copies of 63 and 105 MB, cold: 14.0 and 22.3).
+// Measured (three sets of inputs in turn): 12844 tokens of 32 heads x 128 fp32 76.0 us, 5.5 TB/s; 8192 tokens of 40 heads x 64 bf16 in packed rows 18.2 us, 4.6 TB/s.  From cold inputs
+// into cold results 77.4 and 22.0, the latter for 84 MB (copies of 63 and 105 MB: 14.0 and 22.3).  Axes that no access but a single element's divides take twice that: 8192 tokens of 40 x 64
+// bf16, cold, 16 + 16 pairs in halves 21.2, 13 + 18 40.1, the same as neighbours (accesses of two) 32.3; fp32 34.1 and 46.3.
 #include "common.hpp"
 
 #include <math.h>
@@ -152,7 +153,7 @@ static int launch_rope(RopeArgs& a, hipStream_t stream) {
     a.units = INTER ? a.D / V : a.D / (2 * V);
     a.rot_units = INTER ? 2 * a.R / V : a.R / V;
     const int per = a.heads * a.units;
-    // So many tokens that a thread has up to four units, but no fewer workgroups than four a CU while there are tokens.  (us at 4 / 8 units: 12844 tokens of 32 heads x 128 fp32 79.7 /
+    // So many tokens that a thread has up to four units, but no fewer workgroups than four a CU while there are tokens.  (us, cold inputs and results, at 4 / 8 units: 12844 tokens of 32 heads x 128 fp32 79.7 /
     // 83.4, 8192 of 40 x 64 bf16 22.8 / 23.0; as few workgroups as eight units take / four a CU: 40 tokens of 4 x 88 6.0 / 2.9, 54 of 24 x 32 5.7 / 3.5)
     const int64_t most = (a.rows + 1023) / 1024;
     int tokens = 4 * ROPE_THREADS / per;
