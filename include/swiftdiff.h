@@ -309,7 +309,8 @@ int sd_groupnorm_silu_fwd(const uint16_t* x, uint16_t* y, const uint16_t* gamma,
  *                are the same
  *   dgamma, dbeta device [C] fp32, overwritten (zeros for M = 0); NULL: not wanted.  With neither of
  *                them ws may be NULL.
- * 4 <= C <= 16384, any C (SD_EUNSUPPORTED outside).  A row that holds an infinity or NaN gives NaN in that row. */
+ * 4 <= C <= 16384, any C (SD_EUNSUPPORTED outside).  A row that holds an infinity or NaN gives NaN in that row;
+ * the squares of the deviations from the mean are summed in fp32 (deviations up to 1e17 at any C). */
 int sd_layernorm_fwd(const void* x, int32_t x_dtype, const uint16_t* gamma, const uint16_t* beta, float eps, void* y, int32_t y_dtype,
                      float* mean, float* rstd, int32_t M, int32_t C, void* stream);
 size_t sd_layernorm_bwd_workspace_bytes(int32_t M, int32_t C);

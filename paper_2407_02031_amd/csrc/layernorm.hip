@@ -15,7 +15,8 @@
 // bf16 11.5 + 3.6.  From cold inputs into cold results 17.6 (a copy of the same 63 MB: 14.0) and 27.8 in all (a copy of 105 MB 22.3).  Stores past the caches make the forward pass 16.4
 // cold, and the projection behind it slower by more than that.
 // Other rows, cold (forward / backward with gradients of the weights / without): 8192 x 1280 bf16 13.9 / 20.6 / 16.5, 8192 x 1155 bf16 14.1 / 21.4 / 16.4, 32768 x 320 fp32 to bf16 16.4 /
-// 27.1 / 26.3; few long ones, whose backward kernels keep 4 to 14 registers in scratch beyond C = 4096: 1024 x 8192 fp32 to bf16 18.0 / 39.2 / 24.7, 1024 x 16384 34.4 / 60.2 / 39.0.
+// 27.1 / 26.3; few long ones 1024 x 8192 fp32 to bf16 18.0 / 39.2 / 24.7, 1024 x 16384 34.4 / 60.2 / 39.0 (of the eight backward kernels beyond C = 4096 with gradients of the weights four
+// keep 4 to 14 registers in scratch).
 #include "rows.hpp"
 
 #include <algorithm>
