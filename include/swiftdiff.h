@@ -42,6 +42,7 @@ extern "C" {
 
 #define SD_BF16 0
 #define SD_F32 1
+#define SD_FP8 2            /* e4m3 values, a scale for every block of 128 of a row */
 
 #define SD_EPI_NONE 0
 #define SD_EPI_GEGLU 1
@@ -317,6 +318,42 @@ size_t sd_layernorm_bwd_workspace_bytes(int32_t M, int32_t C);
 int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_dtype, const float* mean, const float* rstd, const uint16_t* gamma,
                      void* dx, float* dgamma, float* dbeta, int32_t M, int32_t C, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- rows in 8 bits: quantize_fp8 --------------------------------------------------------
+ * e4m3 values q and, for every block of 128 elements of a row (the last may be shorter), a scale 2^(s - 127), s a byte (e8m0):
+ * an element stands for q 2^(s - 127).  s is the least with amax <= 448 * 2^(s - 127), amax the largest magnitude
+ * of the block's finite elements, and at least 1; q is the element times 2^(127 - s), which is exact, rounded to nearest, ties to
+ * even.  A NaN or an infinity becomes NaN, and its block's other elements are as they would be without it.
+ * The scales of a matrix of M rows of K elements lie block by block: s of row m and block b is scales[b * lds + m], lds a
+ * multiple of 4, at least M (device, (ceil(K / 128) - 1) * lds + M rounded up to a multiple of 4 bytes; of what lies behind a block's M
+ * at most three bytes are read, whose values do not matter, and nothing is written).  Rows are K bytes, K a multiple of 16 below 2^22; M below 2^27.
+ *   x          device [M, K] of x_dtype (bf16 or fp32) */
+int sd_quantize_fp8(const void* x, int32_t x_dtype, uint8_t* q, uint8_t* scales, int64_t lds, int32_t M, int32_t K, void* stream);
+
+/* ---- rmsnorm_fwd / rmsnorm_bwd -----------------------------------------------------------
+ * Root-mean-square norm with the addition of a branch's result to the residual stream ahead of it.
+ *   h = x + residual,  rstd = 1 / sqrt(sum_c h^2 / C + eps),  y = h rstd gamma
+ *   x          device [M, C] of x_dtype (bf16 or fp32)
+ *   residual   device [M, C] of res_dtype, or NULL: h = x.  bf16 or fp32; an fp32 x onto a bf16 residual is
+ *              SD_EUNSUPPORTED
+ *   gamma      device [C] bf16; NULL: ones
+ *   y          device [M, C] of y_dtype: bf16, fp32, or SD_FP8, rows in 8 bits as above with their scales and lds (C a multiple of
+ *              16 then); may alias x or the residual if the types are the same
+ *   h          device [M, C] of res_dtype, or NULL: not wanted; may alias the residual, or x if the types are the same.
+ *              The norm is of the sum in fp32, before it is rounded to h's type.
+ *   rstd       device [M] fp32 or NULL: kept for the backward pass
+ * Backward: n = h rstd, g = dy gamma;  dh = rstd (g - n sum_c (g n) / C) + dres,  dgamma = sum_m dy n, added up in an order
+ *   that the sizes fix (and, for few rows, whether dh is one of the inputs).  dh is the gradient of x and of the residual.
+ *   dy         device [M, C] of y_dtype (bf16 or fp32);  h device [M, C] of h_dtype, x itself where there was no residual
+ *   dres       device [M, C] of h_dtype: the gradient that reaches h on its own way, or NULL
+ *   dh         device [M, C] of h_dtype; may alias h or dres, or dy if the types are the same
+ *   dgamma     device [C] fp32, overwritten (zeros for M = 0); NULL: not wanted, and ws may be NULL
+ * 4 <= C <= 16384, any C (SD_EUNSUPPORTED outside).  Squares are summed in fp32 (elements up to 1e17 at any C). */
+int sd_rmsnorm_fwd(const void* x, int32_t x_dtype, const void* residual, int32_t res_dtype, const uint16_t* gamma, float eps, void* y, int32_t y_dtype, uint8_t* scales, int64_t lds,
+                   void* h, float* rstd, int32_t M, int32_t C, void* stream);
+size_t sd_rmsnorm_bwd_workspace_bytes(int32_t M, int32_t C);
+int sd_rmsnorm_bwd(const void* dy, int32_t y_dtype, const void* h, int32_t h_dtype, const float* rstd, const uint16_t* gamma, const void* dres, void* dh, float* dgamma, int32_t M, int32_t C,
+                   void* ws, size_t ws_bytes, void* stream);
+
 /* ---- rope_fwd / rope_bwd -------------------------------------------------------------------
  * Rotary positions with several axes, height and width of an image's latent or time, height and
  * width of a video's, on the queries and keys that sd_attention_fwd reads.  A head's first 2 R elements are R pairs
@@ -375,6 +412,38 @@ int sd_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, in
 size_t sd_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K);
 int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, const uint16_t* W, const uint16_t* z, int32_t act, uint16_t* dx, void* dW, int32_t dw_dtype,
                   float* dbias, int32_t M, int32_t N, int32_t K, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- gated_linear_fwd / gated_linear_bwd -------------------------------------------------
+ * The gated projection of a feed-forward, both halves, the activation and the product in one launch:
+ *   v = x Wv^T + bv,  g = x Wg^T + bg,  y = v act(g)        (SD_ACT_NONE: v g)
+ *   x          device [M, K] bf16;  W device [2 N, K] bf16, the rows of Wv first, then those of Wg (as SD_EPI_GEGLU has
+ *              them);  bias device [2 N] bf16 or NULL
+ *   y          device [M, N] of y_dtype, bf16 or fp32;  z device [M, 2 N] bf16 or NULL: v and g of every row, which the
+ *              backward pass needs.  Neither aliases an input or the other.
+ * Backward: dv = dy act(g), dg = dy v act'(g), dz = [dv, dg];  dx = dz W,  dW = dz^T x,  dbias = sum_m dz
+ *   with the arguments, the rounding of dz to bf16 and the order of sums of sd_linear_bwd, of 2 N columns.  z is always read.
+ * K is a multiple of 8, M below 2^27 (2^28 backward), N below 2^21, K below 2^22, and less than 2^22 tiles forward
+ * (SD_EUNSUPPORTED otherwise). */
+int sd_gated_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int32_t act, void* y, int32_t y_dtype, uint16_t* z, int32_t M, int32_t N, int32_t K, void* stream);
+size_t sd_gated_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, const uint16_t* W, const uint16_t* z, int32_t act, uint16_t* dx, void* dW, int32_t dw_dtype,
+                        float* dbias, int32_t M, int32_t N, int32_t K, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- linear_fp8_fwd / gated_linear_fp8_fwd -----------------------------------------------
+ * The linear and the gated linear layer of rows in 8 bits (above), for serving: products of e4m3 values with both
+ * blocks' scales, sums in fp32.
+ *   y = act(x W^T + bias) + residual;       gated: y = (x Wv^T + bv) act(x Wg^T + bg)
+ *   x          device [M, K] in 8 bits with x_scales, x_lds;  W device [N, K], gated [2 N, K] (Wv first), with w_scales, w_lds
+ *   bias       device [N] or [2 N] bf16, or NULL;  residual device [M, N] of y_dtype, or NULL; may alias y
+ *   y          device [M, N] of y_dtype: bf16, fp32, or, gated, SD_FP8 with y_scales, y_lds, for the next product; aliases no input
+ *              but the residual
+ * K is a multiple of 16 below 2^22, M below 2^27, N below 2^22, gated a multiple of 16 below 2^21, and less than 2^22
+ * tiles (SD_EUNSUPPORTED otherwise).  ws is used where y is SD_FP8 and M is small, and may be NULL elsewhere. */
+int sd_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int64_t x_lds, const uint8_t* W, const uint8_t* w_scales, int64_t w_lds, const uint16_t* bias, int32_t act, const void* residual,
+                      void* y, int32_t y_dtype, int32_t M, int32_t N, int32_t K, void* stream);
+size_t sd_gated_linear_fp8_workspace_bytes(int32_t M, int32_t N, int32_t K);
+int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int64_t x_lds, const uint8_t* W, const uint8_t* w_scales, int64_t w_lds, const uint16_t* bias, int32_t act,
+                            void* y, int32_t y_dtype, uint8_t* y_scales, int64_t y_lds, int32_t M, int32_t N, int32_t K, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- spatial_transformer_fwd ----------------------------------------------------------
  * The whole hot path on the guidance pair (Section 3.3: both latents in one batch):

@@ -11,7 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -19,7 +19,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("SWIFTDIFF_LIB") or os.path.join(_HERE, "libswiftdiff.so")
 
-SD_BF16, SD_F32 = 0, 1
+SD_BF16, SD_F32, SD_FP8 = 0, 1, 2
 SD_EPI_NONE, SD_EPI_GEGLU = 0, 1
 SD_ACT_NONE, SD_ACT_GELU, SD_ACT_GELU_TANH, SD_ACT_SILU, SD_ACT_RELU = range(5)
 SD_ROPE_INTERLEAVED, SD_ROPE_HALVES, SD_ROPE_AXIS_HALVES = range(3)
@@ -117,6 +117,16 @@ def _load() -> C.CDLL:
         "sd_linear_fwd": (C.c_int, [vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp]),
         "sd_linear_bwd_workspace_bytes": (sz, [i32, i32, i32]),
         "sd_linear_bwd": (C.c_int, [vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, sz, vp]),
+        "sd_quantize_fp8": (C.c_int, [vp, i32, vp, vp, i64, i32, i32, vp]),
+        "sd_rmsnorm_fwd": (C.c_int, [vp, i32, vp, i32, vp, f32, vp, i32, vp, i64, vp, vp, i32, i32, vp]),
+        "sd_rmsnorm_bwd_workspace_bytes": (sz, [i32, i32]),
+        "sd_rmsnorm_bwd": (C.c_int, [vp, i32, vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, sz, vp]),
+        "sd_gated_linear_fwd": (C.c_int, [vp, vp, vp, i32, vp, i32, vp, i32, i32, i32, vp]),
+        "sd_gated_linear_bwd_workspace_bytes": (sz, [i32, i32, i32]),
+        "sd_gated_linear_bwd": (C.c_int, [vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, i32, i32, i32, vp, sz, vp]),
+        "sd_linear_fp8_fwd": (C.c_int, [vp, vp, i64, vp, vp, i64, vp, i32, vp, vp, i32, i32, i32, i32, vp]),
+        "sd_gated_linear_fp8_workspace_bytes": (sz, [i32, i32, i32]),
+        "sd_gated_linear_fp8_fwd": (C.c_int, [vp, vp, i64, vp, vp, i64, vp, i32, vp, i32, vp, i64, i32, i32, i32, vp, sz, vp]),
         "sd_spatial_transformer_workspace_bytes": (sz, [i32, i32, i32, i32, i32, i32]),
         "sd_spatial_transformer_fwd": (C.c_int, [vp, vp, P(sd_stack_params), vp, i32, i32, i32, i32, i32, i32, vp, sz, vp]),
         "sd_multi_lora_linear_workspace_bytes": (sz, [i32, i32]),
@@ -154,6 +164,8 @@ EXPORTS = ["sd_last_error", "sd_version", "sd_dry_run", "sd_dry_run_text", "sd_g
            "sd_ff_block_fwd", "sd_groupnorm_workspace_bytes", "sd_groupnorm_fwd", "sd_groupnorm_silu_fwd",
            "sd_layernorm_fwd", "sd_layernorm_bwd_workspace_bytes", "sd_layernorm_bwd", "sd_rope_fwd", "sd_rope_bwd",
            "sd_linear_fwd", "sd_linear_bwd_workspace_bytes", "sd_linear_bwd",
+           "sd_quantize_fp8", "sd_rmsnorm_fwd", "sd_rmsnorm_bwd_workspace_bytes", "sd_rmsnorm_bwd", "sd_gated_linear_fwd", "sd_gated_linear_bwd_workspace_bytes", "sd_gated_linear_bwd",
+           "sd_linear_fp8_fwd", "sd_gated_linear_fp8_workspace_bytes", "sd_gated_linear_fp8_fwd",
            "sd_spatial_transformer_workspace_bytes", "sd_spatial_transformer_fwd",
            "sd_multi_lora_linear_workspace_bytes", "sd_multi_lora_linear_fwd", "sd_patch_plan_bytes",
            "sd_patch_plan_build", "sd_lora_patch", "sd_lora_unpatch", "sd_patch_multi_plan_bytes",
@@ -551,6 +563,201 @@ def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: 
     _check(_lib.sd_linear_bwd(pd, _dt(dy), px, pw, pz, act, dx.data_ptr() if grads[0] else None, dW.data_ptr() if grads[1] else None,
                               _dt(dW) if grads[1] else SD_BF16, db.data_ptr() if grads[2] else None, M, N, K, pws, nws, _raw_stream(dev)))
     return dx, dW, db
+
+
+class Fp8Rows(NamedTuple):
+    """Rows in 8 bits: values q [M, K] (torch.float8_e4m3fn) and scales [ceil(K / 128), M] (torch.float8_e8m0fnu), one for every 128 elements of a row.  Element
+    [m, k] stands for q[m, k] * scales[k // 128, m].  The scales of a block are dense, and blocks a multiple of 4 apart (so a view [:, :M], where M is none)."""
+    q: torch.Tensor
+    scales: torch.Tensor
+
+
+_E4M3, _E8M0 = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu,)
+
+
+def _new_fp8(x: torch.Tensor, M: int, K: int):
+    """Room for rows in 8 bits, its two addresses and the distance of its blocks' scales."""
+    q = x.new_empty((M, K), dtype=torch.float8_e4m3fn)
+    ld = (M + 3) & ~3
+    s = x.new_empty(((K + 127) // 128, ld), dtype=torch.float8_e8m0fnu)
+    return Fp8Rows(q, s if ld == M else s[:, :M]), q.data_ptr(), s.data_ptr(), ld
+
+
+def _expect_fp8(name: str, x: Fp8Rows, M: int, K: int, dev: int):
+    """Addresses of values and scales, and the distance of the blocks' scales."""
+    s, blocks = x.scales, (K + 127) // 128
+    pq = _expect(name + ".q", x.q, (M, K), _E4M3, dev)
+    ps = _expect(name + ".scales", s, (blocks, M), _E8M0, dev, dense=False)
+    if s.is_contiguous() and M % 4 == 0:
+        return pq, ps, M
+    ld = s.stride(0) if blocks > 1 else (M + 3) & ~3
+    if s.numel():
+        if (M > 1 and s.stride(1) != 1) or ld % 4 or ld < M:
+            raise ValueError(f"{name}.scales: strides {s.stride()}: dense rows a multiple of 4 apart, please")
+        if s.storage_offset() + (blocks - 1) * ld + ((M + 3) & ~3) > s.untyped_storage().nbytes():
+            raise ValueError(f"{name}.scales: the last block's row ends before a multiple of 4 scales")
+    return pq, ps, ld
+
+
+def quantize_fp8(x: torch.Tensor, out: Optional[Fp8Rows] = None) -> Fp8Rows:
+    """x [M, K], bf16 or fp32, in 8 bits.  K is a multiple of 16."""
+    dev = _on(x)
+    M, K = x.shape
+    _sizes(M, K)
+    px = _expect("x", x, (M, K), _FLOATS, dev)
+    if out is None:
+        out, pq, ps, ld = _new_fp8(x, M, K)
+    else:
+        pq, ps, ld = _expect_fp8("out", out, M, K, dev)
+    _check(_lib.sd_quantize_fp8(px, _dt(x), pq, ps, ld, M, K, _raw_stream(dev)))
+    return out
+
+
+def rmsnorm_fwd(x: torch.Tensor, gamma=None, eps: float = 1e-6, residual=None, out_dtype=torch.bfloat16, stats: bool = False, out=None, h_out=None):
+    """Root-mean-square norm over the last axis of x [..., C], bf16 or fp32, or of h = x + residual: y, with a residual (y, h), h of its type; with `stats` rstd
+    behind them, for rmsnorm_bwd.  With out_dtype torch.float8_e4m3fn y is Fp8Rows, of x [M, C] then.  out and h_out may be given; h_out may be the residual itself.
+    Autograd records nothing."""
+    dev, shape = _on(x), x.shape
+    Cc = shape[-1]
+    M = x.numel() // Cc if Cc else 0
+    _sizes(M, Cc)
+    px = _expect("x", x, shape, _FLOATS, dev)
+    pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
+    pr = ph = h = prs = ps = None
+    rt = ld = 0
+    if residual is not None:
+        pr, rt = _expect("residual", residual, shape, _FLOATS, dev), _dt(residual)
+        h = h_out if h_out is not None else torch.empty_like(residual)
+        ph = _expect("h_out", h, shape, (residual.dtype,), dev)
+    elif h_out is not None:
+        raise ValueError("h_out: without a residual h is x")
+    if isinstance(out, Fp8Rows) or (out is None and out_dtype == torch.float8_e4m3fn):
+        if len(shape) != 2:
+            raise ValueError(f"x: shape {tuple(shape)}: [M, C] where y is in 8 bits")
+        yt = SD_FP8
+        if out is None:
+            y, py, ps, ld = _new_fp8(x, M, Cc)
+        else:
+            y, (py, ps, ld) = out, _expect_fp8("out", out, M, Cc, dev)
+    else:
+        y = out if out is not None else torch.empty_like(x, dtype=out_dtype)
+        py, yt = _expect("out", y, shape, _FLOATS, dev), _dt(y)
+    if stats:
+        rstd = x.new_empty(shape[:-1], dtype=torch.float32)
+        prs = rstd.data_ptr()
+    _check(_lib.sd_rmsnorm_fwd(px, _dt(x), pr, rt, pg, eps, py, yt, ps, ld, ph, prs, M, Cc, _raw_stream(dev)))
+    if residual is None:
+        return (y, rstd) if stats else y
+    return (y, h, rstd) if stats else (y, h)
+
+
+def rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, gamma=None, dres=None, weight_grad: bool = True, out=None, ws=None):
+    """(dh, dgamma) of rmsnorm_fwd: dh, of h's type, the gradient of x and of the residual; dgamma fp32, or None without `weight_grad`.  h is x where there was no
+    residual; dres the gradient that reaches h on its own way."""
+    dev, shape = _on(h), h.shape
+    Cc = shape[-1]
+    M = h.numel() // Cc if Cc else 0
+    _sizes(M, Cc)
+    ph = _expect("h", h, shape, _FLOATS, dev)
+    pd = _expect("dy", dy, shape, _FLOATS, dev)
+    pr = _expect("rstd", rstd, shape[:-1], _F32, dev)
+    pg = _expect("gamma", gamma, (Cc,), _BF16, dev)
+    pa = _expect("dres", dres, shape, (h.dtype,), dev)
+    if out is None:
+        dh = torch.empty_like(h)
+        po = dh.data_ptr()
+    else:
+        dh, po = out, _expect("out", out, shape, (h.dtype,), dev)
+    dg = pdg = pw = None
+    nw = 0
+    if weight_grad:
+        dg = h.new_empty((Cc,), dtype=torch.float32)
+        pdg = dg.data_ptr()
+        w, pw, nw = _scratch(h, _lib.sd_rmsnorm_bwd_workspace_bytes(M, Cc), ws, dev)
+    _check(_lib.sd_rmsnorm_bwd(pd, _dt(dy), ph, _dt(h), pr, pg, pa, po, pdg, M, Cc, pw, nw, _raw_stream(dev)))
+    return dh, dg
+
+
+def gated_linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_ACT_SILU, out_dtype=torch.bfloat16, save_z: bool = False, out=None):
+    """v act(g) for x [M, K], [v, g] = x W^T + bias, W [2 N, K] the value's rows first; with `save_z` (y, z), z = [v, g] for gated_linear_bwd.  Autograd records
+    nothing."""
+    dev = _on(x)
+    M, K = x.shape
+    N = W.shape[0] // 2
+    _sizes(M, N, K)
+    px = _expect("x", x, (M, K), _BF16, dev)
+    pw = _expect("W", W, (2 * N, K), _BF16, dev)
+    pb = _expect("bias", bias, (2 * N,), _BF16, dev)
+    if out is None:
+        y = x.new_empty((M, N), dtype=out_dtype)
+    else:
+        y = out
+    py = _expect("out", y, (M, N), _FLOATS, dev)
+    z = x.new_empty((M, 2 * N)) if save_z else None
+    _check(_lib.sd_gated_linear_fwd(px, pw, pb, act, py, _dt(y), z.data_ptr() if save_z else None, M, N, K, _raw_stream(dev)))
+    return (y, z) if save_z else y
+
+
+def gated_linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z: torch.Tensor, act: int = SD_ACT_SILU, grads: Sequence[bool] = (True, True, True),
+                     dw_dtype=torch.bfloat16, ws=None):
+    """(dx, dW, dbias) of gated_linear_fwd, each None where `grads` does not ask for it.  dx and dW are products of dz rounded to bf16."""
+    dev = _on(x)
+    M, K = x.shape
+    N = W.shape[0] // 2
+    _sizes(M, N, K)
+    px = _expect("x", x, (M, K), _BF16, dev)
+    pw = _expect("W", W, (2 * N, K), _BF16, dev)
+    pd = _expect("dy", dy, (M, N), _FLOATS, dev)
+    pz = _expect("z", z, (M, 2 * N), _BF16, dev)
+    dx = torch.empty_like(x) if grads[0] else None
+    dW = torch.empty_like(W, dtype=dw_dtype) if grads[1] else None
+    db = x.new_empty((2 * N,), dtype=torch.float32) if grads[2] else None
+    w, pws, nws = _scratch(x, _lib.sd_gated_linear_bwd_workspace_bytes(M, N, K), ws, dev)
+    _check(_lib.sd_gated_linear_bwd(pd, _dt(dy), px, pw, pz, act, dx.data_ptr() if grads[0] else None, dW.data_ptr() if grads[1] else None,
+                                    _dt(dW) if grads[1] else SD_BF16, db.data_ptr() if grads[2] else None, M, N, K, pws, nws, _raw_stream(dev)))
+    return dx, dW, db
+
+
+def linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_NONE, residual=None, out_dtype=torch.bfloat16, out=None) -> torch.Tensor:
+    """act(x W^T + bias) + residual for x [M, K] and W [N, K] in 8 bits."""
+    dev = _on(x.q)
+    M, K = x.q.shape
+    N = W.q.shape[0]
+    _sizes(M, N, K)
+    px, pxs, ldx = _expect_fp8("x", x, M, K, dev)
+    pw, pws, ldw = _expect_fp8("W", W, N, K, dev)
+    pb = _expect("bias", bias, (N,), _BF16, dev)
+    y = out if out is not None else x.q.new_empty((M, N), dtype=out_dtype)
+    py = _expect("out", y, (M, N), _FLOATS, dev)
+    pr = _expect("residual", residual, (M, N), (y.dtype,), dev)
+    _check(_lib.sd_linear_fp8_fwd(px, pxs, ldx, pw, pws, ldw, pb, act, pr, py, _dt(y), M, N, K, _raw_stream(dev)))
+    return y
+
+
+def gated_linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_SILU, out_dtype=torch.bfloat16, out=None, ws=None):
+    """v act(g) for x [M, K] and W [2 N, K] in 8 bits, [v, g] = x W^T + bias; with out_dtype torch.float8_e4m3fn as Fp8Rows, for linear_fp8_fwd.  N is a multiple
+    of 16."""
+    dev = _on(x.q)
+    M, K = x.q.shape
+    N = W.q.shape[0] // 2
+    _sizes(M, N, K)
+    px, pxs, ldx = _expect_fp8("x", x, M, K, dev)
+    pw, pws, ldw = _expect_fp8("W", W, 2 * N, K, dev)
+    pb = _expect("bias", bias, (2 * N,), _BF16, dev)
+    if isinstance(out, Fp8Rows) or (out is None and out_dtype == torch.float8_e4m3fn):
+        yt = SD_FP8
+        if out is None:
+            y, py, pys, ldy = _new_fp8(x.q, M, N)
+        else:
+            y, (py, pys, ldy) = out, _expect_fp8("out", out, M, N, dev)
+        w, pwk, nwk = _scratch(x.q, _lib.sd_gated_linear_fp8_workspace_bytes(M, N, K), ws, dev)
+    else:
+        y = out if out is not None else x.q.new_empty((M, N), dtype=out_dtype)
+        py, yt = _expect("out", y, (M, N), _FLOATS, dev), _dt(y)
+        pys = pwk = None
+        ldy = nwk = 0
+    _check(_lib.sd_gated_linear_fp8_fwd(px, pxs, ldx, pw, pws, ldw, pb, act, py, yt, pys, ldy, M, N, K, pwk, nwk, _raw_stream(dev)))
+    return y
 
 
 def spatial_transformer_workspace_bytes(Bn, T, Cc, Tc, Dc, r_max) -> int:

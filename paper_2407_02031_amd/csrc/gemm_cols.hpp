@@ -1,0 +1,625 @@
+// Products of rows, D[m][n] = sum_k P[m][k] Q[n][k], both operands in bf16 or both in 8 bits with scales (fp8.hpp), for epilogues that need several columns of a row in one lane: a gate
+// beside its value, a block's largest element.
+//
+// Tiling and loads as in gemm_tile.hpp: BM x BN tiles of WGM x WGN wavefronts, operands straight into LDS in steps of 128 bytes of K, a ring of STAGES such steps, 16-byte chunks swizzled.
+// What differs:
+//   - A step is 64 elements of bf16, two MFMAs 16x16x32 deep, or 128 of 8 bits, one scaled MFMA 16x16x128.  The scales of a step's rows ride along in LDS, a byte a row, and the
+//     MFMA multiplies by them: both operands' blocks are 128 long, so all four 32-element pieces of a lane's row have the same one.
+//   - The 16 rows of an MFMA operand are not neighbours: of 32 (64) rows of Q, block b takes every second (fourth), so that a lane, which holds elements 4 quad .. 4 quad + 3 of
+//     each block's result, has 8 (16) neighbouring columns of one row of D in all.  Epilogues work in registers and store 16 bytes a lane, without a detour through LDS.  The
+//     rows are sorted where they are loaded: which row of memory goes into which row of LDS costs nothing.  The same for P, four blocks to 64 rows, whose four scales are then one word.
+//   - Gated: half of a wavefront's Q blocks are rows of the value, half rows of the gate, of the same columns.
+#pragma once
+#include "gemm_dma.hpp"
+#include "fp8.hpp"
+
+namespace sd {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+struct ColsProblem {
+    const uint8_t *p, *q;              // [M, Kb], [N or 2 N, Kb] bytes: values first, then gates
+    const uint8_t *ps, *qs;            // scales (8 bits)
+    int64_t ldps, ldqs;
+    const uint16_t* bias;              // [N or 2 N] or null
+    const void* res;                   // [M, N] of y's type or null
+    void* y;                           // [M, N]
+    uint16_t* z;                       // gated: [M, 2 N] bf16 or null
+    uint8_t* ys;                       // y in 8 bits: its scales
+    int64_t ldys;
+    int32_t M, N, Kb;                  // Kb: bytes of a row of P or Q, a multiple of 16
+    int32_t act, y_f32;
+    int32_t tiles_m, tiles_n;
+};
+
+// Which row of 16 B rows is row i of block b: every B-th
+template <int B>
+__device__ __forceinline__ constexpr int spread(int b, int i) { return b / B * (16 * B) + B * i + b % B; }
+
+template <bool FP8, int BM, int BN, int STAGES>
+constexpr int cols_scale_words() { return FP8 ? ((BM + BN + 255) / 256) * 64 : 0; }      // of a stage
+template <bool FP8, int BM, int BN, int WGN, int STAGES, bool OUT8>
+constexpr int cols_lds_chunks() {
+    const int ring = STAGES * ((BM + BN) * 8 + cols_scale_words<FP8, BM, BN, STAGES>() / 4);
+    return ring + (OUT8 ? WGN * BM / 4 : 0);
+}
+
+__device__ __forceinline__ void dma4(const void* gptr, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds_base)), "v"(gptr) : "memory", "m0");
+}
+
+// What the operands are, and how they are multiplied.  The scaled MFMA takes 128 of 8 bits in the time of 64 of bf16, but it adds products eight at a time, and of those eight it keeps what is worth 2^-13 of
+// the largest and more (measured: with one of 2^16, another of 2^2 is gone; in another eight, and of the sums of eights, nothing is): off by 1.5e-5 of a sum of random terms, where
+// 8 bits were off by 2^-5 in each.  That is far below the rounding of y to bf16 or to 8 bits, but not of y in fp32: there, and where the rows are few and the
+// operands' bytes all that counts, they are widened to bf16, exactly and with their scales, and multiplied as those.
+enum ColsMode { COLS_BF16, COLS_FP8, COLS_FP8_WIDE };
+
+// 32 e4m3 elements times 2^(s - 127), s a byte: a multiple of it has the same 8 exponent bits
+__device__ __forceinline__ void widen32(const u32x4 (&w)[2], uint32_t s, bf16x8 (&o)[4]) {
+    const float scale = __uint_as_float(s << 23);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        union { bf16x8 v; bf16x2 p[4]; } u;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t x = w[i / 2][i % 2 * 2 + j];
+            u.p[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
+            u.p[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+        }
+        o[i] = u.v;
+    }
+}
+__device__ __forceinline__ f32x4 mfma_bf16(bf16x8 q, bf16x8 p, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, p, c, 0, 0, 0); }
+// c + (Q block) (P block)^T, scales bytes QB of qs and PB of ps
+template <int QB, int PB>
+__device__ __forceinline__ f32x4 mfma_fp8(const u32x4 (&q)[2], const u32x4 (&p)[2], f32x4 c, uint32_t qs, uint32_t ps) {
+    const i32x8 a = {(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[1][0], (int)q[1][1], (int)q[1][2], (int)q[1][3]};
+    const i32x8 b = {(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[1][0], (int)p[1][1], (int)p[1][2], (int)p[1][3]};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, QB, (int)qs, PB, (int)ps);
+}
+// f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>)
+template <int N, class F, int I = 0>
+__device__ __forceinline__ void each(F f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each<N, F, I + 1>(f);
+    }
+}
+
+template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8, bool GUARD>
+__device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, u32x4* const lds) {
+    constexpr bool FP8 = MODE != COLS_BF16, WIDE = MODE == COLS_FP8_WIDE;
+    constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NI = WN / 16;
+    constexpr int LPT = (BM + BN) / 8 / NW;            // 1 KB loads a wavefront and step: eight rows each
+    constexpr int JP = BM / 8 / NW;                    // ... of them of P
+    constexpr int SW = cols_scale_words<FP8, BM, BN, STAGES>();
+    constexpr int STAGE = (BM + BN) * 8 + SW / 4;      // 16-byte chunks
+    constexpr int PIECES = SW / 64;
+    constexpr int LOADS = LPT + (FP8 ? 1 : 0);
+    constexpr int RING = NI >= 4 ? NI / 2 : NI;
+    constexpr int NV = GATED ? NI / 2 : NI;            // blocks of columns of the result
+    constexpr int BP = MI % 4 == 0 ? 4 : 2, BQ = OUT8 ? 4 : 2;
+    constexpr int BN_OUT = GATED ? BN / 2 : BN, WN_OUT = GATED ? WN / 2 : WN;
+    static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && MI % BP == 0 && NV % BQ == 0 && NI % RING == 0 && STAGES >= 2 && STAGES <= 4, "tile");
+    static_assert(!FP8 || PIECES <= NW, "scales");
+    static_assert(!OUT8 || (GATED && FP8 && BN_OUT == FP8_BLOCK), "a tile's columns are one block of y");
+
+    const int band_tiles = 8 * P.tiles_n;
+    const int band = tile / band_tiles, rem = tile - band * band_tiles;
+    const int band_rows = min(8, P.tiles_m - band * 8);
+    const int tn = rem / band_rows, tm = band * 8 + rem % band_rows;
+    const int m0 = tm * BM, n0 = tn * BN_OUT;
+    const int M = P.M, N = P.N, Kb = P.Kb;
+    const int nk = (Kb + 127) / 128;
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, quad = lane >> 4;
+    const int wm = (wave / WGN) * WM, wn = (wave % WGN) * WN, wn_out = (wave % WGN) * WN_OUT;
+
+    // ---- loads: load j of a wavefront fills rows 8 (j NW + wave) .. + 8 of a stage, lane l the chunk at position l % 8 of row l / 8.  They lie in one block of 16, so what
+    // differs between value and gate is the wavefront's base.
+    uint32_t off[LPT];
+    const uint8_t* base[LPT];
+    const uint8_t* const pb = P.p + (int64_t)m0 * Kb;
+    const uint8_t* const qb = P.q + (int64_t)n0 * Kb;
+#pragma unroll
+    for (int j = 0; j < LPT; ++j) {
+        const int first = (j * NW + wave) * 8, row = first + (lane >> 3);
+        const int c = swz<8>(row, lane & 7) * 16;
+        if (j < JP) {
+            const int w = first / WM, b = first % WM / 16;
+            const int r = min(m0 + w * WM + spread<BP>(b, row % 16), M - 1) - m0;
+            base[j] = pb;
+            off[j] = (uint32_t)r * (uint32_t)Kb + c;
+        } else {
+            const int w = (first - BM) / WN, b = (first - BM) % WN / 16;
+            const bool gate = GATED && b >= NV;
+            const int r = min(n0 + w * WN_OUT + spread<BQ>(gate ? b - NV : b, row % 16), N - 1) - n0;
+            base[j] = gate ? qb + (int64_t)N * Kb : qb;
+            off[j] = (uint32_t)r * (uint32_t)Kb + c;
+        }
+    }
+    // scales: word a of a stage has those of rows 4 a .. 4 a + 3 of P's, then of Q's (values, gates); past the last row, the last word that there is
+    const uint8_t* sp = nullptr;
+    int64_t sp_step = 0;
+    if constexpr (FP8) {
+        const int a = (wave % PIECES) * 64 + lane, j = a * 4 - BM;
+        if (j < 0 || j >= BN) {
+            sp = P.ps + min(m0 + (j < 0 ? a * 4 : 0), (M - 1) & ~3);
+            sp_step = P.ldps;
+        } else {
+            sp = P.qs + min(n0 + (GATED && j >= BN_OUT ? N + j - BN_OUT : j), ((GATED ? 2 * N : N) - 1) & ~3);
+            sp_step = P.ldqs;
+        }
+    }
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+    const uint32_t wave_base = lds_base + (uint32_t)wave * 1024;
+    const uint32_t scale_base = lds_base + (uint32_t)((BM + BN) * 128 + (PIECES ? wave % (PIECES ? PIECES : 1) : 0) * 256);
+    // load j of step t; steps are loaded in order, each once
+    auto load = [&](int j, int t, int stg, auto partial) {
+        const uint32_t to = wave_base + (uint32_t)stg * (STAGE * 16) + (uint32_t)j * (NW * 1024);
+        const int kb = t * 128;
+        if (decltype(partial)::value && kb + 128 > Kb) {
+            const uint8_t* const src = base[j] + kb + off[j];
+            dma16(kb + (int)(swz<8>((j * NW + wave) * 8 + (lane >> 3), lane & 7) * 16) < Kb ? src : reinterpret_cast<const uint8_t*>(g_gemm_zeros), to);
+        } else {
+            dma16_so(base[j] + kb, off[j], to);
+        }
+        if (FP8 && j == 0) {
+            dma4(sp, scale_base + (uint32_t)stg * (STAGE * 16));
+            sp += sp_step;
+        }
+    };
+
+    f32x4 acc[MI][NI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // ---- operands in registers: P's blocks, and a ring of Q's
+    u32x4 pr[MI][2], qr[RING][2];
+    uint32_t ps[FP8 ? MI / BP : 1], qs[FP8 ? NI / BQ : 1];     // scales of the step being multiplied
+    const int lsw = (l16 >> 1) & 7;
+    const u32x4* const frag = lds + l16 * 8;
+    auto fetch_p = [&](int st, int mi) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) pr[mi][h] = frag[st * STAGE + (wm + mi * 16) * 8 + ((h * 4 + quad) ^ lsw)];
+    };
+    auto fetch_q = [&](int st, int ni) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) qr[ni % RING][h] = frag[st * STAGE + (BM + wn + ni * 16) * 8 + ((h * 4 + quad) ^ lsw)];
+    };
+    auto fetch_scales = [&](int st, auto& p, auto& q) {
+        if constexpr (FP8) {
+            const uint8_t* const sc = reinterpret_cast<const uint8_t*>(lds) + st * (STAGE * 16) + (BM + BN) * 128;
+#pragma unroll
+            for (int i = 0; i < MI / BP; ++i) {
+                const uint8_t* const at = sc + wm + i * 16 * BP + BP * l16;
+                p[i] = BP == 4 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+            }
+#pragma unroll
+            for (int i = 0; i < NI / BQ; ++i) {
+                const bool gate = GATED && i >= NV / BQ;
+                const uint8_t* const at = sc + BM + wn_out + (gate ? BN_OUT + (i - NV / BQ) * 16 * BQ : i * 16 * BQ) + BQ * l16;
+                q[i] = BQ == 4 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
+            }
+        }
+    };
+    bf16x8 pw[WIDE ? MI : 1][4], qw[4];
+    // Slot s: Q block s by all of P's, then `load`'s share of another step's loads, dealt over the slots from the edge on.  (No branches in here: the compiler would move the MFMAs past them, all
+    // to the end of the step.)
+    auto slot = [&](auto sc, auto refill_qc, auto refill_pc, int st_q, auto load) {
+        constexpr int s = decltype(sc)::value;
+        constexpr bool refill_q = decltype(refill_qc)::value, refill_p = decltype(refill_pc)::value;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (WIDE) {
+            if constexpr (s == 0) each<MI>([&](auto mi) { widen32(pr[mi], (ps[mi / BP] >> (mi % BP * 8)) & 255u, pw[mi]); });
+            widen32(qr[s % RING], (qs[s / BQ] >> (s % BQ * 8)) & 255u, qw);
+        }
+        each<MI>([&](auto mic) {
+            constexpr int mi = decltype(mic)::value;
+            f32x4& c = acc[mi][s];
+            if constexpr (MODE == COLS_FP8) {
+                c = mfma_fp8<s % BQ, mi % BP>(qr[s % RING], pr[mi], c, qs[s / BQ], ps[mi / BP]);
+            } else if constexpr (WIDE) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c = mfma_bf16(qw[i], pw[mi][i], c);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) c = mfma_bf16(__builtin_bit_cast(bf16x8, qr[s % RING][h]), __builtin_bit_cast(bf16x8, pr[mi][h]), c);
+            }
+            if constexpr (refill_p) {
+                __builtin_amdgcn_sched_barrier(0);
+                fetch_p(st_q, mi);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (refill_q) fetch_q(st_q, (s + RING) % NI);
+        constexpr int i = (s + RING) % NI;
+#pragma unroll
+        for (int j = i * LPT / NI; j < (i + 1) * LPT / NI; ++j) load(j);
+    };
+    // A step: its first NI - RING slots (`head`), then, when the next step has landed everywhere and this one's stage is free (what is left of it is in registers), the last RING
+    // (`edge`), which bring in the next step's first blocks and, P's as they are done with, all of P.
+    uint32_t ps_next[FP8 ? MI / BP : 1], qs_next[FP8 ? NI / BQ : 1];
+    auto head = [&](int st, auto load) {
+        each<NI - RING>([&](auto s) { slot(s, std::true_type(), std::false_type(), st, load); });
+    };
+    auto edge = [&](int sn, auto load) {
+        fetch_scales(sn, ps_next, qs_next);
+        each<RING>([&](auto i) {
+            constexpr int s = NI - RING + decltype(i)::value;
+            slot(std::integral_constant<int, s>(), std::true_type(), std::integral_constant<bool, s == NI - 1>(), sn, load);
+        });
+        if constexpr (FP8) {
+#pragma unroll
+            for (int i = 0; i < MI / BP; ++i) ps[i] = ps_next[i];
+#pragma unroll
+            for (int i = 0; i < NI / BQ; ++i) qs[i] = qs_next[i];
+        }
+    };
+    auto none = [](int) {};
+    auto wait_steps = [&](int newer) {      // `newer` steps may stay in flight
+        if (STAGES >= 4 && newer >= 3) wait_vmcnt<3 * LOADS>();
+        else if (STAGES >= 3 && newer >= 2) wait_vmcnt<2 * LOADS>();
+        else if (newer >= 1) wait_vmcnt<LOADS>();
+        else wait_vmcnt<0>();
+    };
+
+#pragma unroll
+    for (int d = 0; d < STAGES; ++d)
+        if (d < nk)
+#pragma unroll
+            for (int j = 0; j < LPT; ++j) load(j, d, d, std::integral_constant<bool, GUARD>());
+    wait_steps(nk - 1 < STAGES - 1 ? nk - 1 : STAGES - 1);
+    __syncthreads();
+    fetch_scales(0, ps, qs);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) fetch_p(0, mi);
+#pragma unroll
+    for (int s = 0; s < RING; ++s) fetch_q(0, s);
+    head(0, none);
+    int st = 0, t = 0;
+    const int nfull = GUARD ? Kb / 128 : nk;     // whole steps
+#pragma unroll 1
+    for (; t + STAGES < nfull; ++t) {
+        wait_vmcnt<(STAGES - 2) * LOADS>();
+        __syncthreads();
+        const int sn = st + 1 == STAGES ? 0 : st + 1;
+        auto next = [&](int j) { load(j, t + STAGES, st, std::false_type()); };
+        edge(sn, next);
+        head(sn, next);
+        st = sn;
+    }
+    // the last steps, which have nothing left to load but one that may be partial
+#pragma unroll 1
+    for (; t + 1 < nk; ++t) {
+        wait_steps(nk - 2 - t < STAGES - 2 ? nk - 2 - t : STAGES - 2);
+        __syncthreads();
+        const int sn = st + 1 == STAGES ? 0 : st + 1;
+        if (t + STAGES < nk)
+#pragma unroll
+            for (int j = 0; j < LPT; ++j) load(j, t + STAGES, st, std::integral_constant<bool, GUARD>());
+        edge(sn, none);
+        head(sn, none);
+        st = sn;
+    }
+    each<RING>([&](auto i) { slot(std::integral_constant<int, NI - RING + decltype(i)::value>(), std::false_type(), std::false_type(), 0, none); });
+
+    // ---- epilogue.  A lane has rows spread<BP>(mi, l16) of its wavefront's, and of each 16 BQ columns the 4 BQ from 4 BQ quad on.
+    constexpr int NG = NV / BQ, W4 = BQ;               // groups of 16 BQ columns; pieces of four columns of a lane in one
+    const uint16_t* const bias = P.bias;
+    auto column = [&](int g) { return n0 + wn_out + g * 16 * BQ + quad * 4 * BQ; };
+    // piece c of group g: columns 4 c .. 4 c + 3 of the lane's: element x is block (4 c + x) % BQ's, entry (4 c + x) / BQ
+    auto piece = [&](int mi, int first, int g, int c) {
+        f32x4 v;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) v[x] = acc[mi][first + g * BQ + (4 * c + x) % BQ][(4 * c + x) / BQ];
+        return v;
+    };
+    auto bias4 = [&](const uint16_t* b, int col) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (!b) return v;
+        if (col + 4 <= N) return load4(reinterpret_cast<const __bf16*>(b) + col);
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+            if (col + x < N) v[x] = bf16_to_f32(b[col + x]);
+        return v;
+    };
+    auto store = [&](auto* p, int64_t at, int col, f32x4 v) {
+        using T = std::remove_pointer_t<decltype(p)>;
+        if (col + 4 <= N) store4(p + at, v);
+        else
+#pragma unroll
+            for (int x = 0; x < 3; ++x)
+                if (col + x < N) p[at + x] = (T)v[x];
+    };
+    auto residual4 = [&](auto* p, int64_t at, int col) {
+        if (col + 4 <= N) return load4(p + at);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 3; ++x)
+            if (col + x < N) v[x] = (float)p[at + x];
+        return v;
+    };
+    __bf16* const zb = reinterpret_cast<__bf16*>(P.z);
+    uint32_t top[OUT8 ? MI : 1];
+#pragma unroll
+    for (int mi = 0; mi < (OUT8 ? MI : 1); ++mi) top[mi] = 0;
+#pragma unroll
+    for (int gr = 0; gr < NG; ++gr) {
+        const int col = column(gr);
+        f32x4 bv[W4], bg[W4];
+#pragma unroll
+        for (int c = 0; c < W4; ++c) {
+            bv[c] = bias4(bias, col + 4 * c);
+            if (GATED) bg[c] = bias4(bias ? bias + N : nullptr, col + 4 * c);
+        }
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int m = m0 + wm + spread<BP>(mi, l16);
+            f32x4 v[W4], g[W4];
+#pragma unroll
+            for (int c = 0; c < W4; ++c) {
+                v[c] = piece(mi, 0, gr, c) + bv[c];
+                if (GATED) g[c] = piece(mi, GATED ? NV : 0, gr, c) + bg[c];
+            }
+            if constexpr (GATED) {
+                if (!OUT8 && P.z && m < M)
+#pragma unroll
+                    for (int c = 0; c < W4; ++c) {
+                        store(zb, (int64_t)m * 2 * N + col + 4 * c, col + 4 * c, v[c]);
+                        store(zb, (int64_t)m * 2 * N + N + col + 4 * c, col + 4 * c, g[c]);
+                    }
+                apply_act(P.act, g);
+#pragma unroll
+                for (int c = 0; c < W4; ++c) v[c] *= g[c];
+            } else {
+                apply_act(P.act, v);
+                if (P.res && m < M)
+#pragma unroll
+                    for (int c = 0; c < W4; ++c) {
+                        const int64_t at = (int64_t)m * N + col + 4 * c;
+                        v[c] += P.y_f32 ? residual4(static_cast<const float*>(P.res), at, col + 4 * c) : residual4(static_cast<const __bf16*>(P.res), at, col + 4 * c);
+                    }
+            }
+            if constexpr (OUT8) {
+                // kept where the value's sums were, until the block's largest is known
+#pragma unroll
+                for (int c = 0; c < W4; ++c) {
+                    if (col + 4 * c < N) top[mi] = fp8_magnitude(top[mi], v[c]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) acc[mi][gr * BQ + (4 * c + x) % BQ][(4 * c + x) / BQ] = v[c][x];
+                }
+            } else if (m < M) {
+#pragma unroll
+                for (int c = 0; c < W4; ++c) {
+                    const int64_t at = (int64_t)m * N + col + 4 * c;
+                    if (P.y_f32) store(static_cast<float*>(P.y), at, col + 4 * c, v[c]);
+                    else store(static_cast<__bf16*>(P.y), at, col + 4 * c, v[c]);
+                }
+            }
+        }
+    }
+    if constexpr (OUT8) {
+        uint32_t* const meet = reinterpret_cast<uint32_t*>(lds + STAGES * STAGE);      // [WGN][BM]
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            uint32_t u = max(top[mi], (uint32_t)__shfl_xor((int)top[mi], 16));
+            u = max(u, (uint32_t)__shfl_xor((int)u, 32));
+            if (quad == 0) meet[(wave % WGN) * BM + wm + spread<BP>(mi, l16)] = u;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            const int r = wm + spread<BP>(mi, l16), m = m0 + r;
+            uint32_t u = 0;
+#pragma unroll
+            for (int w = 0; w < WGN; ++w) u = max(u, meet[w * BM + r]);
+            const int sc = fp8_scale(u);
+            const float inv = fp8_inverse(sc);
+            if (m < M) {
+                if (wave % WGN == 0 && quad == 0) P.ys[(int64_t)tn * P.ldys + m] = (uint8_t)sc;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    u32x4 w;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) w[c] = fp8_pack(piece(mi, 0, g, c), inv);
+                    const int col = column(g);         // (N is a multiple of 16)
+                    if (col < N) *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(P.y) + (int64_t)m * N + col) = w;
+                }
+            }
+        }
+    }
+}
+
+template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8, bool GUARD>
+__global__ __launch_bounds__(64 * WGM * WGN, (cols_lds_chunks<MODE != COLS_BF16, BM, BN, WGN, STAGES, OUT8>() * 16 <= 80 * 1024 ? 2 : 1)) void cols_kernel(const ColsProblem P) {
+    __shared__ u32x4 lds[cols_lds_chunks<MODE != COLS_BF16, BM, BN, WGN, STAGES, OUT8>()];
+    const int total = P.tiles_m * P.tiles_n, per = (total + 7) >> 3;
+    const int tile = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+    if (tile >= total) return;
+    cols_tile<MODE, BM, BN, WGM, WGN, STAGES, GATED, OUT8, GUARD>(P, tile, lds);
+}
+
+// Few rows (one token's, a guidance pair's, a short text's).  A workgroup has 16 MB rows and 16 NB columns (of a gated product of value and gate each); its eight wavefronts take every eighth
+// step of 128 bytes and bring the rows of P and Q straight into the registers as MFMA operands, U steps at once, and meet in LDS when they are done.  Bound by Q, which comes in once per
+// 16 MB rows, and one trip to HBM.
+constexpr int FEW_NW = 8;
+template <bool FP8, bool GATED, int MB, int NB, int U>
+__global__ __launch_bounds__(64 * FEW_NW) void few_rows_kernel(const ColsProblem P) {
+    constexpr int NW = FEW_NW, QB = GATED ? 2 * NB : NB, BLOCKS = MB * QB, OUT = MB * NB, PER = (OUT + NW - 1) / NW;
+    __shared__ f32x4 sh[NW * BLOCKS * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l16 = lane & 15, quad = lane >> 4;
+    const int M = P.M, N = P.N, Kb = P.Kb;
+    const int n0 = blockIdx.x * (16 * NB), m0 = blockIdx.y * (16 * MB);
+    const uint8_t *qr[QB], *pr[MB], *qsr[QB], *psr[MB];
+    f32x4 acc[MB][QB];
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+        const int64_t r = min(n0 + n % NB * 16 + l16, N - 1) + (n >= NB ? (int64_t)N : 0);
+        qr[n] = P.q + r * Kb + quad * 16;
+        if (FP8) qsr[n] = P.qs + r;
+    }
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+        const int64_t r = min(m0 + m * 16 + l16, M - 1);
+        pr[m] = P.p + r * Kb + quad * 16;
+        if (FP8) psr[m] = P.ps + r;
+#pragma unroll
+        for (int n = 0; n < QB; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int steps = (Kb + 127) / 128;
+    const u32x4 none = {0u, 0u, 0u, 0u};
+    u32x4 qf[U][QB][2], pf[U][MB][2];
+    uint32_t qsc[U][QB], psc[U][MB];
+    auto fetch = [&](int s0) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int s = s0 + i * NW, k = s * 128;
+            const bool lo = k + quad * 16 < Kb, hi = k + quad * 16 + 64 < Kb;      // (a chunk of 16 bytes is whole or not there)
+#pragma unroll
+            for (int n = 0; n < QB; ++n) {
+                qf[i][n][0] = lo ? *reinterpret_cast<const u32x4*>(qr[n] + k) : none;
+                qf[i][n][1] = hi ? *reinterpret_cast<const u32x4*>(qr[n] + k + 64) : none;
+                if (FP8) qsc[i][n] = s < steps ? qsr[n][s * P.ldqs] : 127u;
+            }
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+                pf[i][m][0] = lo ? *reinterpret_cast<const u32x4*>(pr[m] + k) : none;
+                pf[i][m][1] = hi ? *reinterpret_cast<const u32x4*>(pr[m] + k + 64) : none;
+                if (FP8) psc[i][m] = s < steps ? psr[m][s * P.ldps] : 127u;
+            }
+        }
+    };
+    fetch(wave);
+    // what the epilogue adds, behind the first loads: wavefront w finishes blocks w, w + 8, ..., a lane has four columns of one row
+    f32x4 bv[PER], bg[GATED ? PER : 1], rv[PER];
+    auto place = [&](int i, int& row, int& col) {
+        const int b = wave + i * NW;
+        row = m0 + b / NB * 16 + l16;
+        col = n0 + b % NB * 16 + quad * 4;
+        return b < OUT && row < M && col < N;
+    };
+    auto read4 = [&](auto* p, int col) {
+        if (col + 4 <= N) return load4(p);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (col + e < N) v[e] = (float)p[e];
+        return v;
+    };
+    auto write4 = [&](auto* p, int col, f32x4 v) {
+        using T = std::remove_pointer_t<decltype(p)>;
+        if (col + 4 <= N) store4(p, v);
+        else
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if (col + e < N) p[e] = (T)v[e];
+    };
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        bv[i] = rv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (GATED) bg[GATED ? i : 0] = bv[i];
+        int row, col;
+        if (!place(i, row, col)) continue;
+        const int64_t at = (int64_t)row * N + col;
+        const __bf16* const bb = reinterpret_cast<const __bf16*>(P.bias) + col;
+        if (P.bias) {
+            bv[i] = read4(bb, col);
+            if (GATED) bg[GATED ? i : 0] = read4(bb + N, col);
+        }
+        if (!GATED && P.res) rv[i] = P.y_f32 ? read4(static_cast<const float*>(P.res) + at, col) : read4(static_cast<const __bf16*>(P.res) + at, col);
+    }
+    for (int s0 = wave;;) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if constexpr (FP8) {
+                bf16x8 qw[QB][4];
+#pragma unroll
+                for (int n = 0; n < QB; ++n) widen32(qf[i][n], qsc[i][n], qw[n]);
+#pragma unroll
+                for (int m = 0; m < MB; ++m) {
+                    bf16x8 pw[4];
+                    widen32(pf[i][m], psc[i][m], pw);
+#pragma unroll
+                    for (int n = 0; n < QB; ++n)
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) acc[m][n] = mfma_bf16(qw[n][h], pw[h], acc[m][n]);
+                }
+            } else {
+#pragma unroll
+                for (int m = 0; m < MB; ++m)
+#pragma unroll
+                    for (int n = 0; n < QB; ++n)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) acc[m][n] = mfma_bf16(__builtin_bit_cast(bf16x8, qf[i][n][h]), __builtin_bit_cast(bf16x8, pf[i][m][h]), acc[m][n]);
+            }
+        }
+        s0 += NW * U;
+        if (s0 >= steps) break;
+        fetch(s0);
+    }
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) sh[(wave * BLOCKS + b) * 64 + lane] = acc[b / QB][b % QB];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        int row, col;
+        if (!place(i, row, col)) continue;
+        const int b = (wave + i * NW) / NB * QB + (wave + i * NW) % NB;
+        auto total = [&](int blk) {
+            f32x4 v = sh[blk * 64 + lane];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) v += sh[(w * BLOCKS + blk) * 64 + lane];
+            return v;
+        };
+        f32x4 v[1] = {total(b) + bv[i]};
+        const int64_t at = (int64_t)row * N + col;
+        if constexpr (GATED) {
+            f32x4 g[1] = {total(b + NB) + bg[i]};
+            if (P.z) {
+                __bf16* const zp = reinterpret_cast<__bf16*>(P.z) + (int64_t)row * 2 * N + col;
+                write4(zp, col, v[0]);
+                write4(zp + N, col, g[0]);
+            }
+            apply_act(P.act, g);
+            v[0] *= g[0];
+        } else {
+            apply_act(P.act, v);
+            v[0] += rv[i];
+        }
+        if (P.y_f32) write4(static_cast<float*>(P.y) + at, col, v[0]);
+        else write4(static_cast<__bf16*>(P.y) + at, col, v[0]);
+    }
+}
+
+// ---- launches
+template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8>
+static int launch_cols(ColsProblem& P, hipStream_t stream) {
+    constexpr int BN_OUT = GATED ? BN / 2 : BN;
+    P.tiles_m = (P.M + BM - 1) / BM;
+    P.tiles_n = (P.N + BN_OUT - 1) / BN_OUT;
+    const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n;
+    SD_REQUIRE(tiles < (1 << 22), SD_EUNSUPPORTED, "linear: M=%d N=%d: 2^22 tiles and more", P.M, P.N);        // (threads of a launch stay below 2^32)
+    const bool guard = P.Kb % 128 != 0;
+    if (SD_DRY_RUN("gemm cols%s%s%s %dx%d/%d waves/%d stages%s; ", MODE == COLS_BF16 ? "" : MODE == COLS_FP8 ? " 8 bits" : " 8 bits wide", GATED ? " gated" : "", OUT8 ? " to 8 bits" : "", BM, BN, WGM * WGN, STAGES, guard ? " guard" : "")) return SD_OK;
+    const dim3 grid((unsigned)((tiles + 7) & ~7ll)), block(64 * WGM * WGN);
+    if (guard) hipLaunchKernelGGL((cols_kernel<MODE, BM, BN, WGM, WGN, STAGES, GATED, OUT8, true>), grid, block, 0, stream, P);
+    else hipLaunchKernelGGL((cols_kernel<MODE, BM, BN, WGM, WGN, STAGES, GATED, OUT8, false>), grid, block, 0, stream, P);
+    SD_HIP_CHECK(hipGetLastError());
+    return SD_OK;
+}
+template <bool FP8, bool GATED, int MB, int NB, int U>
+static int launch_few(const ColsProblem& P, hipStream_t stream) {
+    if (SD_DRY_RUN("few rows%s%s %dx%d; ", FP8 ? " 8 bits" : "", GATED ? " gated" : "", 16 * MB, 16 * NB)) return SD_OK;
+    hipLaunchKernelGGL((few_rows_kernel<FP8, GATED, MB, NB, U>), dim3((P.N + 16 * NB - 1) / (16 * NB), (P.M + 16 * MB - 1) / (16 * MB)), dim3(64 * FEW_NW), 0, stream, P);
+    SD_HIP_CHECK(hipGetLastError());
+    return SD_OK;
+}
+
+}  // namespace sd

@@ -151,6 +151,133 @@ struct DzCut {
     }
 };
 
+// The same of a gated layer: dy [M, N] and z = [v, g] [M, 2 N] in, dz = [dy act(g), dy v act'(g)] [M, Np] out, Np 2 N rounded up to a multiple of 8; its column sums are 2 N.  Where N is
+// no multiple of eight, accesses to the gate's half are aligned to an element alone.
+template <class D, bool STORE, bool SUMS, int CT, int NT>
+__global__ __launch_bounds__(NT) void gated_dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
+    constexpr int SUB = NT / CT, BATCH = 2;
+    constexpr int PARTS = CT < 64 ? NT / 64 : SUB;          // sums of a column that meet in LDS
+    __shared__ f32x8 sh[2 * (PARTS - 1) * CT];
+    const int t = threadIdx.x % CT, sub = threadIdx.x / CT;
+    const int cols = (int)blockIdx.x / blocks, block = (int)blockIdx.x - cols * blocks;
+    const int c = (cols * CT + t) * 8;
+    const int64_t r0 = (int64_t)block * rows + sub;
+    const int64_t r1 = min((int64_t)M, ((int64_t)block + 1) * rows);
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    f32x8 sv = {zero, zero}, sg = sv;
+    const __bf16* const zb = reinterpret_cast<const __bf16*>(z);
+    __bf16* const out = reinterpret_cast<__bf16*>(dz);
+    const int at = c + 8 <= N ? c : N - 8;        // (as in dz_kernel)
+    auto all = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        auto one = [&](f32x4& d, f32x4& v, const f32x4& g) {        // d <- dy act(g), v <- dy v act'(g)
+            f32x4 a[1] = {g};
+            apply_act(KIND, a);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] *= d[e] * act_slope<KIND>(g[e]);
+                d[e] *= a[0][e];
+            }
+        };
+        auto both = [&](f32x8& d, f32x8& v, const f32x8& g) {
+            one(d.lo, v.lo, g.lo);
+            one(d.hi, v.hi, g.hi);
+            if (SUMS) {
+                sv.lo += d.lo;
+                sv.hi += d.hi;
+                sg.lo += v.lo;
+                sg.hi += v.hi;
+            }
+        };
+        if (N >= 8 && c < N) {
+            for (int64_t r = r0; r < r1; r += SUB * BATCH) {
+                f32x8 d[BATCH], v[BATCH], g[BATCH];
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i) {
+                    const int64_t row = min(r + i * SUB, r1 - 1);
+                    d[i] = load8(dy + row * N + at);
+                    v[i] = load8(zb + row * 2 * N + at);
+                    g[i] = load8(zb + row * 2 * N + N + at);
+                }
+#pragma unroll
+                for (int i = 0; i < BATCH; ++i)
+                    if (r + i * SUB < r1) {
+                        both(d[i], v[i], g[i]);
+                        if (STORE) {
+                            store8(out + (r + i * SUB) * Np + at, d[i]);
+                            store8(out + (r + i * SUB) * Np + N + at, v[i]);
+                        }
+                    }
+            }
+        } else if (c < N) {
+            for (int64_t r = r0; r < r1; r += SUB) {
+                f32x8 d = {zero, zero}, v = d, g = d;
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < N) {
+                        const float dd = (float)dy[r * N + e], vv = (float)zb[r * 2 * N + e], gg = (float)zb[r * 2 * N + N + e];
+                        if (e < 4) d.lo[e & 3] = dd, v.lo[e & 3] = vv, g.lo[e & 3] = gg;
+                        else d.hi[e & 3] = dd, v.hi[e & 3] = vv, g.hi[e & 3] = gg;
+                    }
+                both(d, v, g);
+                if (STORE)
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < N) {
+                            out[r * Np + e] = (__bf16)(e < 4 ? d.lo[e & 3] : d.hi[e & 3]);
+                            out[r * Np + N + e] = (__bf16)(e < 4 ? v.lo[e & 3] : v.hi[e & 3]);
+                        }
+            }
+        }
+    };
+    switch (act) {
+    case SD_ACT_GELU: all(std::integral_constant<int, SD_ACT_GELU>()); break;
+    case SD_ACT_GELU_TANH: all(std::integral_constant<int, SD_ACT_GELU_TANH>()); break;
+    case SD_ACT_SILU: all(std::integral_constant<int, SD_ACT_SILU>()); break;
+    case SD_ACT_RELU: all(std::integral_constant<int, SD_ACT_RELU>()); break;
+    default: all(std::integral_constant<int, SD_ACT_NONE>());
+    }
+    if (STORE && c < N && c + 8 >= N)
+        for (int64_t r = r0; r < r1; r += SUB)
+            for (int e = 2 * N; e < Np; ++e) dz[r * Np + e] = 0;
+    if (SUMS) {
+        int part = sub;
+        if constexpr (CT < 64) {       // the rows of a wavefront
+#pragma unroll
+            for (int o = CT; o < 64; o *= 2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sv.lo[e] += __shfl_xor(sv.lo[e], o);
+                    sv.hi[e] += __shfl_xor(sv.hi[e], o);
+                    sg.lo[e] += __shfl_xor(sg.lo[e], o);
+                    sg.hi[e] += __shfl_xor(sg.hi[e], o);
+                }
+            part = threadIdx.x >> 6;
+        }
+        if (part && (CT >= 64 || (threadIdx.x & 63) < CT)) {
+            sh[(part - 1) * 2 * CT + t] = sv;
+            sh[(part - 1) * 2 * CT + CT + t] = sg;
+        }
+        __syncthreads();
+        if (threadIdx.x >= CT || c >= N) return;
+#pragma unroll
+        for (int w = 0; w < PARTS - 1; ++w) {
+            sv.lo += sh[w * 2 * CT + t].lo;
+            sv.hi += sh[w * 2 * CT + t].hi;
+            sg.lo += sh[w * 2 * CT + CT + t].lo;
+            sg.hi += sh[w * 2 * CT + CT + t].hi;
+        }
+        const int first = c + 8 <= N ? c : N >= 8 ? N - 8 : 0;
+        float* const to = sums + (int64_t)block * 2 * N + first;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (first + e >= c && first + e < N) {
+                to[e] = e < 4 ? sv.lo[e & 3] : sv.hi[e & 3];
+                to[N + e] = e < 4 ? sg.lo[e & 3] : sg.hi[e & 3];
+            }
+    }
+}
+
 // ---------------------------------------------------------------------------------------
 // What is left in parts: dx, dW (as many fp32 matrices as their reductions were cut into) and dbias (a row for every
 // row block of dz), each added up in order, in one launch.  256 threads: 1024 elements of a matrix, or 16 columns of dbias.
@@ -542,6 +669,47 @@ struct BwdWs {
     size_t total() const { return round_up(dz, 256) + round_up(sums, 256) + round_up(dx_parts, 256) + round_up(dw_parts, 256) + 256; }
 };
 
+// dx = dz W and dW = dz^T x, dz with rows of Np elements, and what `left` holds besides of what is in parts
+static int launch_products(const uint16_t* dz, int Np, const uint16_t* x, const uint16_t* W, uint16_t* dx, void* dW, int dw_dtype, float* dx_parts, float* dw_parts, PartSums& left, int M, int N, int K,
+                           const BwdPlan& plan, hipStream_t s) {
+    if (dx || dW) {
+        GemmGroup g;
+        memset(&g, 0, sizeof(g));
+        const bool dw_first = dW && (!dx || plan.w_first);
+        auto push_dw = [&] {
+            if (dW) push_product(g, true, dz, Np, x, K, dW, dw_dtype == SD_F32, plan.w, M, dw_parts);
+        };
+        if (dw_first) push_dw();
+        const int dx_from = g.n;
+        if (dx) push_product(g, false, dz, Np, W, K, dx, false, plan.x, N, dx_parts);
+        const int dx_to = g.n;
+        if (!dw_first) push_dw();
+        const bool guard = (dW && M % 64 != 0) || (dx && N % 64 != 0);
+        const int dw_from = dw_first ? 0 : dx_to, dw_to = dw_first ? dx_from : g.n;
+        const int rc = plan.small ? launch_bwd<BWD_SMALL_BM, BWD_BN, 2, 2, 3>(g, dw_from, dw_to, guard, s) : launch_bwd<BWD_BM, BWD_BN, 4, 2, 3>(g, dw_from, dw_to, guard, s);
+        if (rc) return rc;
+        auto rest = [&](const BwdCut& c, const float* parts, void* out, bool f32) {
+            return parts_of(parts, static_cast<char*>(out) + c.whole * c.cols * (f32 ? 4 : 2), f32, (c.rows - c.whole) * c.cols, c.parts);
+        };
+        if (dx && plan.x.parts > 1) left.m[0] = rest(plan.x, dx_parts, dx, false);
+        if (dW && plan.w.parts > 1) left.m[1] = rest(plan.w, dw_parts, dW, dw_dtype == SD_F32);
+    }
+    return launch_part_sums(left, s);
+}
+// what sd_gated_linear_bwd carves out of its workspace
+struct GatedBwdWs {
+    size_t dz, sums, dx_parts, dw_parts;
+    GatedBwdWs(int64_t M, int64_t N, int64_t K) {
+        dz = (size_t)M * ((2 * N + 7) & ~7ll) * 2;
+        sums = (size_t)DzCut(M, N).blocks * 2 * N * 4;
+        const BwdPlan p(M, 2 * N, K);
+        dx_parts = p.x.bytes();
+        dw_parts = p.w.bytes();
+    }
+    size_t total() const { return round_up(dz, 256) + round_up(sums, 256) + round_up(dx_parts, 256) + round_up(dw_parts, 256) + 256; }
+};
+constexpr int GATED_MAX_N = LINEAR_MAX_NK / 2;
+
 }  // namespace sd
 
 using namespace sd;
@@ -647,28 +815,72 @@ extern "C" int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x,
         left.blocks = blocks;
         left.N = N;
     }
-    if (dx || dW) {
-        const uint16_t* const dz = plain ? static_cast<const uint16_t*>(dy) : dzbuf;
-        GemmGroup g;
-        memset(&g, 0, sizeof(g));
-        const bool dw_first = dW && (!dx || plan.w_first);
-        auto push_dw = [&] {
-            if (dW) push_product(g, true, dz, Np, x, K, dW, dw_dtype == SD_F32, plan.w, M, dw_parts);
-        };
-        if (dw_first) push_dw();
-        const int dx_from = g.n;
-        if (dx) push_product(g, false, dz, Np, W, K, dx, false, plan.x, N, dx_parts);
-        const int dx_to = g.n;
-        if (!dw_first) push_dw();
-        const bool guard = (dW && M % 64 != 0) || (dx && N % 64 != 0);
-        const int dw_from = dw_first ? 0 : dx_to, dw_to = dw_first ? dx_from : g.n;
-        rc = plan.small ? launch_bwd<BWD_SMALL_BM, BWD_BN, 2, 2, 3>(g, dw_from, dw_to, guard, s) : launch_bwd<BWD_BM, BWD_BN, 4, 2, 3>(g, dw_from, dw_to, guard, s);
-        if (rc) return rc;
-        auto rest = [&](const BwdCut& c, const float* parts, void* out, bool f32) {
-            return parts_of(parts, static_cast<char*>(out) + c.whole * c.cols * (f32 ? 4 : 2), f32, (c.rows - c.whole) * c.cols, c.parts);
-        };
-        if (dx && plan.x.parts > 1) left.m[0] = rest(plan.x, dx_parts, dx, false);
-        if (dW && plan.w.parts > 1) left.m[1] = rest(plan.w, dw_parts, dW, dw_dtype == SD_F32);
+    return launch_products(plain ? static_cast<const uint16_t*>(dy) : dzbuf, Np, x, W, dx, dW, dw_dtype, dx_parts, dw_parts, left, M, N, K, plan, s);
+}
+
+extern "C" size_t sd_gated_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K) {
+    if (M <= 0 || N <= 0 || K <= 0 || M >= LINEAR_MAX_M || N >= GATED_MAX_N || K >= LINEAR_MAX_NK) return 256;      // (nothing to do, or refused)
+    return GatedBwdWs(M, N, K).total();
+}
+
+extern "C" int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, const uint16_t* W, const uint16_t* z, int32_t act, uint16_t* dx, void* dW, int32_t dw_dtype,
+                                   float* dbias, int32_t M, int32_t N, int32_t K, void* ws, size_t ws_bytes, void* stream) {
+    SD_REQUIRE(N < GATED_MAX_N, SD_EUNSUPPORTED, "gated_linear_bwd: N=%d (below 2^21)", N);
+    int rc = linear_sizes("gated_linear_bwd", M, N < 0 ? N : 2 * N, K, act, y_dtype);
+    if (rc) return rc;
+    SD_REQUIRE(dw_dtype == SD_BF16 || dw_dtype == SD_F32, SD_EINVAL, "gated_linear_bwd: dw_dtype=%d", dw_dtype);
+    SD_REQUIRE(aligned16(dy) && aligned16(x) && aligned16(W) && aligned16(z) && aligned16(dx) && aligned16(dW) && aligned16(dbias), SD_EINVAL,
+               "gated_linear_bwd: pointers must be 16-byte aligned");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    PartSums left;
+    memset(&left, 0, sizeof(left));
+    if (M == 0 || N == 0) {        // sums over nothing
+        if (dx) left.m[0] = parts_of(nullptr, dx, false, (int64_t)M * K, 0);
+        if (dW) left.m[1] = parts_of(nullptr, dW, dw_dtype == SD_F32, 2ll * N * K, 0);
+        left.dbias = dbias;
+        left.N = 2 * N;
+        return launch_part_sums(left, s);
     }
-    return launch_part_sums(left, s);
+    SD_REQUIRE(dy && z && (!dW || x) && (!dx || W), SD_EINVAL, "gated_linear_bwd: dy, z, x or W is null");
+    for (const void* const out : {static_cast<const void*>(dx), static_cast<const void*>(dW), static_cast<const void*>(dbias)})
+        SD_REQUIRE(!out || (out != dy && out != x && out != W && out != z), SD_EINVAL, "gated_linear_bwd: a gradient in an input's place");
+    if (!dx && !dW && !dbias) return SD_OK;
+    const size_t need = sd_gated_linear_bwd_workspace_bytes(M, N, K);
+    SD_REQUIRE(ws && ws_bytes >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SD_EWORKSPACE, "gated_linear_bwd: workspace of %zu bytes, need %zu, 256-byte aligned", ws_bytes, need);
+    const GatedBwdWs b(M, N, K);
+    Workspace w(ws, ws_bytes);
+    uint16_t* const dz = static_cast<uint16_t*>(w.take(b.dz));
+    float* const sums = static_cast<float*>(w.take(b.sums));
+    float* const dx_parts = static_cast<float*>(w.take(b.dx_parts));
+    float* const dw_parts = static_cast<float*>(w.take(b.dw_parts));
+    const int Np = (2 * N + 7) & ~7;
+    const DzCut cut(M, N);
+    const int blocks = (int)cut.blocks;
+    const bool store = dx || dW;
+    if (!SD_DRY_RUN("gated dz%s%s; ", store ? "" : " sums only", dbias ? "" : " no sums")) {
+        const dim3 grid((unsigned)(cut.blocks * cut.col_wgs));
+        float* const to = blocks == 1 ? dbias : sums;
+        auto run = [&](auto* t, auto ct, auto nt) {
+            using D = std::remove_pointer_t<decltype(t)>;
+            constexpr int CT = decltype(ct)::value, NT = decltype(nt)::value;
+            const D* const d = static_cast<const D*>(dy);
+            if (store && dbias) hipLaunchKernelGGL((gated_dz_kernel<D, true, true, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
+            else if (store) hipLaunchKernelGGL((gated_dz_kernel<D, true, false, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
+            else hipLaunchKernelGGL((gated_dz_kernel<D, false, true, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
+        };
+        auto by_cut = [&](auto* t) {
+            if (cut.ct == 2) run(t, std::integral_constant<int, 2>(), std::integral_constant<int, 1024>());
+            else run(t, std::integral_constant<int, 64>(), std::integral_constant<int, 256>());
+        };
+        if (y_dtype == SD_F32) by_cut(static_cast<float*>(nullptr));
+        else by_cut(static_cast<__bf16*>(nullptr));
+        SD_HIP_CHECK(hipGetLastError());
+    }
+    if (dbias && blocks > 1) {
+        left.sums = sums;
+        left.dbias = dbias;
+        left.blocks = blocks;
+        left.N = 2 * N;
+    }
+    return launch_products(dz, Np, x, W, dx, dW, dw_dtype, dx_parts, dw_parts, left, M, 2 * N, K, BwdPlan(M, 2 * N, K), s);
 }
