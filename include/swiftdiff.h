@@ -422,7 +422,7 @@ int sd_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, const uint
  *              backward pass needs.  Neither aliases an input or the other.
  * Backward: dv = dy act(g), dg = dy v act'(g), dz = [dv, dg];  dx = dz W,  dW = dz^T x,  dbias = sum_m dz
  *   with the arguments, the rounding of dz to bf16 and the order of sums of sd_linear_bwd, of 2 N columns.  z is always read.
- * K is a multiple of 8, M below 2^27 (2^28 backward), N below 2^21, K below 2^22, and less than 2^22 tiles forward
+ * K is a multiple of 8, M below 2^27 (2^28 backward), N below 2^21, K below 2^22, and M / 64 times N / 32, rounded up, below 2^22 forward
  * (SD_EUNSUPPORTED otherwise). */
 int sd_gated_linear_fwd(const uint16_t* x, const uint16_t* W, const uint16_t* bias, int32_t act, void* y, int32_t y_dtype, uint16_t* z, int32_t M, int32_t N, int32_t K, void* stream);
 size_t sd_gated_linear_bwd_workspace_bytes(int32_t M, int32_t N, int32_t K);
@@ -437,8 +437,9 @@ int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, cons
  *   bias       device [N] or [2 N] bf16, or NULL;  residual device [M, N] of y_dtype, or NULL; may alias y
  *   y          device [M, N] of y_dtype: bf16, fp32, or, gated, SD_FP8 with y_scales, y_lds, for the next product; aliases no input
  *              but the residual
- * K is a multiple of 16 below 2^22, M below 2^27, N below 2^22, gated a multiple of 16 below 2^21, and less than 2^22
- * tiles (SD_EUNSUPPORTED otherwise).  ws is used where y is SD_FP8 and M is small, and may be NULL elsewhere. */
+ * K is a multiple of 16 below 2^22, M below 2^27, N below 2^22, gated a multiple of 16 below 2^21, and M / 64 times the
+ * rows of W / 64, both rounded up, below 2^22 (SD_EUNSUPPORTED otherwise).  ws is used for some sizes where y is SD_FP8, and may
+ * be NULL elsewhere (the query says 0). */
 int sd_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int64_t x_lds, const uint8_t* W, const uint8_t* w_scales, int64_t w_lds, const uint16_t* bias, int32_t act, const void* residual,
                       void* y, int32_t y_dtype, int32_t M, int32_t N, int32_t K, void* stream);
 size_t sd_gated_linear_fp8_workspace_bytes(int32_t M, int32_t N, int32_t K);

@@ -580,7 +580,7 @@ def _new_fp8(x: torch.Tensor, M: int, K: int):
     q = x.new_empty((M, K), dtype=torch.float8_e4m3fn)
     ld = (M + 3) & ~3
     s = x.new_empty(((K + 127) // 128, ld), dtype=torch.float8_e8m0fnu)
-    return Fp8Rows(q, s if ld == M else s[:, :M]), q.data_ptr(), s.data_ptr(), ld
+    return Fp8Rows(q, s if ld == M else s.narrow(1, 0, M)), q.data_ptr(), s.data_ptr(), ld
 
 
 def _expect_fp8(name: str, x: Fp8Rows, M: int, K: int, dev: int):
@@ -750,7 +750,10 @@ def gated_linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_SI
             y, py, pys, ldy = _new_fp8(x.q, M, N)
         else:
             y, (py, pys, ldy) = out, _expect_fp8("out", out, M, N, dev)
-        w, pwk, nwk = _scratch(x.q, _lib.sd_gated_linear_fp8_workspace_bytes(M, N, K), ws, dev)
+        nwk = _lib.sd_gated_linear_fp8_workspace_bytes(M, N, K)
+        pwk = None
+        if nwk or ws is not None:
+            w, pwk, nwk = _scratch(x.q, nwk, ws, dev)
     else:
         y = out if out is not None else x.q.new_empty((M, N), dtype=out_dtype)
         py, yt = _expect("out", y, (M, N), _FLOATS, dev), _dt(y)

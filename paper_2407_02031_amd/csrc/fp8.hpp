@@ -24,6 +24,12 @@ __device__ __forceinline__ uint32_t fp8_magnitude(float v) {
     return u >= 0x7f800000u ? 0u : u;
 }
 __device__ __forceinline__ uint32_t fp8_magnitude(uint32_t m, f32x4 v) { return max(max(max(m, fp8_magnitude(v[0])), max(fp8_magnitude(v[1]), fp8_magnitude(v[2]))), fp8_magnitude(v[3])); }
+// max(m, |v[0]|, ..., |v[3]|), NaN apart: infinite where one of them is
+__device__ __forceinline__ float fp8_top(float m, f32x4 v) {
+    asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(m) : "v"(v[0]), "v"(v[1]));
+    asm("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(m) : "v"(v[2]), "v"(v[3]));
+    return m;
+}
 // The largest over the 16 lanes of a DPP row, in all of them
 __device__ __forceinline__ uint32_t max16(uint32_t m) {
     m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xf, 0xf, false));
@@ -47,6 +53,11 @@ __device__ __forceinline__ uint32_t fp8_pack(f32x4 v, float inv) {
     auto in = [&](float f) { return fmaf(f, 0.f, f * inv); };
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(in(v[0]), in(v[1]), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(in(v[2]), in(v[3]), w, true);
+}
+// ... of finite ones, or NaN
+__device__ __forceinline__ uint32_t fp8_pack_finite(f32x4 v, float inv) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, w, true);
 }
 
 }  // namespace sd

@@ -36,12 +36,12 @@ struct ColsProblem {
 template <int B>
 __device__ __forceinline__ constexpr int spread(int b, int i) { return b / B * (16 * B) + B * i + b % B; }
 
-template <bool FP8, int BM, int BN, int STAGES>
+template <bool FP8, int BM, int BN>
 constexpr int cols_scale_words() { return FP8 ? ((BM + BN + 255) / 256) * 64 : 0; }      // of a stage
 template <bool FP8, int BM, int BN, int WGN, int STAGES, bool OUT8>
 constexpr int cols_lds_chunks() {
-    const int ring = STAGES * ((BM + BN) * 8 + cols_scale_words<FP8, BM, BN, STAGES>() / 4);
-    return ring + (OUT8 ? WGN * BM / 4 : 0);
+    const int ring = STAGES * ((BM + BN) * 8 + cols_scale_words<FP8, BM, BN>() / 4);
+    return ring + BN / 4 + (OUT8 ? WGN * BM / 4 : 0);
 }
 
 __device__ __forceinline__ void dma4(const void* gptr, uint32_t lds_base) {
@@ -54,28 +54,32 @@ __device__ __forceinline__ void dma4(const void* gptr, uint32_t lds_base) {
 // operands' bytes all that counts, they are widened to bf16, exactly and with their scales, and multiplied as those.
 enum ColsMode { COLS_BF16, COLS_FP8, COLS_FP8_WIDE };
 
-// 32 e4m3 elements times 2^(s - 127), s a byte: a multiple of it has the same 8 exponent bits
-__device__ __forceinline__ void widen32(const u32x4 (&w)[2], uint32_t s, bf16x8 (&o)[4]) {
+// 16 e4m3 elements times 2^(s - 127), s a byte, which is what the conversion looks at of an fp32 scale
+__device__ __forceinline__ void widen16(const u32x4& w, uint32_t s, bf16x8 (&o)[2]) {
     const float scale = __uint_as_float(s << 23);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
         union { bf16x8 v; bf16x2 p[4]; } u;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const uint32_t x = w[i / 2][i % 2 * 2 + j];
-            u.p[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
-            u.p[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+            u.p[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i * 2 + j], scale, false);
+            u.p[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i * 2 + j], scale, true);
         }
         o[i] = u.v;
     }
 }
+__device__ __forceinline__ void widen32(const u32x4 (&w)[2], uint32_t s, bf16x8 (&o)[4]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) widen16(w[h], s, reinterpret_cast<bf16x8(&)[2]>(o[2 * h]));
+}
 __device__ __forceinline__ f32x4 mfma_bf16(bf16x8 q, bf16x8 p, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, p, c, 0, 0, 0); }
+__device__ __forceinline__ i32x8 words8(const u32x4 (&w)[2]) {
+    return i32x8{(int)w[0][0], (int)w[0][1], (int)w[0][2], (int)w[0][3], (int)w[1][0], (int)w[1][1], (int)w[1][2], (int)w[1][3]};
+}
 // c + (Q block) (P block)^T, scales bytes QB of qs and PB of ps
 template <int QB, int PB>
 __device__ __forceinline__ f32x4 mfma_fp8(const u32x4 (&q)[2], const u32x4 (&p)[2], f32x4 c, uint32_t qs, uint32_t ps) {
-    const i32x8 a = {(int)q[0][0], (int)q[0][1], (int)q[0][2], (int)q[0][3], (int)q[1][0], (int)q[1][1], (int)q[1][2], (int)q[1][3]};
-    const i32x8 b = {(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[1][0], (int)p[1][1], (int)p[1][2], (int)p[1][3]};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, QB, (int)qs, PB, (int)ps);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(words8(q), words8(p), c, 0, 0, QB, (int)qs, PB, (int)ps);
 }
 // f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>)
 template <int N, class F, int I = 0>
@@ -90,9 +94,9 @@ template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bo
 __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, u32x4* const lds) {
     constexpr bool FP8 = MODE != COLS_BF16, WIDE = MODE == COLS_FP8_WIDE;
     constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NI = WN / 16;
-    constexpr int LPT = (BM + BN) / 8 / NW;            // 1 KB loads a wavefront and step: eight rows each
+    constexpr int LPT = (BM + BN) / 8 / NW;            // loads of a wavefront and step
     constexpr int JP = BM / 8 / NW;                    // ... of them of P
-    constexpr int SW = cols_scale_words<FP8, BM, BN, STAGES>();
+    constexpr int SW = cols_scale_words<FP8, BM, BN>();
     constexpr int STAGE = (BM + BN) * 8 + SW / 4;      // 16-byte chunks
     constexpr int PIECES = SW / 64;
     constexpr int LOADS = LPT + (FP8 ? 1 : 0);
@@ -102,6 +106,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     constexpr int BN_OUT = GATED ? BN / 2 : BN, WN_OUT = GATED ? WN / 2 : WN;
     static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && MI % BP == 0 && NV % BQ == 0 && NI % RING == 0 && STAGES >= 2 && STAGES <= 4, "tile");
     static_assert(!FP8 || PIECES <= NW, "scales");
+    static_assert(NW * 64 >= BN, "bias");
     static_assert(!OUT8 || (GATED && FP8 && BN_OUT == FP8_BLOCK), "a tile's columns are one block of y");
 
     const int band_tiles = 8 * P.tiles_n;
@@ -117,28 +122,34 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     const int l16 = lane & 15, quad = lane >> 4;
     const int wm = (wave / WGN) * WM, wn = (wave % WGN) * WN, wn_out = (wave % WGN) * WN_OUT;
 
-    // ---- loads: load j of a wavefront fills rows 8 (j NW + wave) .. + 8 of a stage, lane l the chunk at position l % 8 of row l / 8.  They lie in one block of 16, so what
+    // ---- loads: load j of a wavefront fills rows 8 (j NW + wave) .. + 8 of a stage, lane l the chunk at position l % 8 of row l / 8.  They lie in one block, so what
     // differs between value and gate is the wavefront's base.
     uint32_t off[LPT];
     const uint8_t* base[LPT];
     const uint8_t* const pb = P.p + (int64_t)m0 * Kb;
     const uint8_t* const qb = P.q + (int64_t)n0 * Kb;
+    auto chunk = [&](int j) { return swz<8>((j * NW + wave) * 8 + (lane >> 3), lane & 7) * 16; };
 #pragma unroll
     for (int j = 0; j < LPT; ++j) {
         const int first = (j * NW + wave) * 8, row = first + (lane >> 3);
-        const int c = swz<8>(row, lane & 7) * 16;
         if (j < JP) {
             const int w = first / WM, b = first % WM / 16;
             const int r = min(m0 + w * WM + spread<BP>(b, row % 16), M - 1) - m0;
             base[j] = pb;
-            off[j] = (uint32_t)r * (uint32_t)Kb + c;
+            off[j] = (uint32_t)r * (uint32_t)Kb + chunk(j);
         } else {
             const int w = (first - BM) / WN, b = (first - BM) % WN / 16;
             const bool gate = GATED && b >= NV;
             const int r = min(n0 + w * WN_OUT + spread<BQ>(gate ? b - NV : b, row % 16), N - 1) - n0;
             base[j] = gate ? qb + (int64_t)N * Kb : qb;
-            off[j] = (uint32_t)r * (uint32_t)Kb + c;
+            off[j] = (uint32_t)r * (uint32_t)Kb + chunk(j);
         }
+    }
+    // what the epilogue adds to columns: thread j has that of the tile's j-th (of the value's, then of the gate's)
+    uint16_t bias_raw = 0;
+    if (P.bias && tid < BN) {
+        const int j = GATED && tid >= BN_OUT ? tid - BN_OUT : tid;
+        if (n0 + j < N) bias_raw = P.bias[n0 + j + (GATED && tid >= BN_OUT ? N : 0)];
     }
     // scales: word a of a stage has those of rows 4 a .. 4 a + 3 of P's, then of Q's (values, gates); past the last row, the last word that there is
     const uint8_t* sp = nullptr;
@@ -162,7 +173,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         const int kb = t * 128;
         if (decltype(partial)::value && kb + 128 > Kb) {
             const uint8_t* const src = base[j] + kb + off[j];
-            dma16(kb + (int)(swz<8>((j * NW + wave) * 8 + (lane >> 3), lane & 7) * 16) < Kb ? src : reinterpret_cast<const uint8_t*>(g_gemm_zeros), to);
+            dma16(kb + (int)chunk(j) < Kb ? src : reinterpret_cast<const uint8_t*>(g_gemm_zeros), to);
         } else {
             dma16_so(base[j] + kb, off[j], to);
         }
@@ -178,10 +189,10 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // ---- operands in registers: P's blocks, and a ring of Q's
+    // ---- operands in registers: P's blocks, and a ring of Q's.  A lane has chunks quad and quad + 4 of a row, of either operand: which k an MFMA's lane has does not matter, if it is the same ones.
     u32x4 pr[MI][2], qr[RING][2];
     uint32_t ps[FP8 ? MI / BP : 1], qs[FP8 ? NI / BQ : 1];     // scales of the step being multiplied
-    const int lsw = (l16 >> 1) & 7;
+    const int lsw = swz<8>(l16, 0);
     const u32x4* const frag = lds + l16 * 8;
     auto fetch_p = [&](int st, int mi) {
 #pragma unroll
@@ -202,7 +213,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
 #pragma unroll
             for (int i = 0; i < NI / BQ; ++i) {
                 const bool gate = GATED && i >= NV / BQ;
-                const uint8_t* const at = sc + BM + wn_out + (gate ? BN_OUT + (i - NV / BQ) * 16 * BQ : i * 16 * BQ) + BQ * l16;
+                const uint8_t* const at = sc + BM + wn_out + (gate ? BN_OUT : 0) + (gate ? i - NV / BQ : i) * 16 * BQ + BQ * l16;
                 q[i] = BQ == 4 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
             }
         }
@@ -218,29 +229,37 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
             if constexpr (s == 0) each<MI>([&](auto mi) { widen32(pr[mi], (ps[mi / BP] >> (mi % BP * 8)) & 255u, pw[mi]); });
             widen32(qr[s % RING], (qs[s / BQ] >> (s % BQ * 8)) & 255u, qw);
         }
-        each<MI>([&](auto mic) {
-            constexpr int mi = decltype(mic)::value;
-            f32x4& c = acc[mi][s];
-            if constexpr (MODE == COLS_FP8) {
-                c = mfma_fp8<s % BQ, mi % BP>(qr[s % RING], pr[mi], c, qs[s / BQ], ps[mi / BP]);
-            } else if constexpr (WIDE) {
+        if constexpr (WIDE) {
+            // (P's raw blocks are done with since they were widened)
+            if constexpr (refill_p)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) c = mfma_bf16(qw[i], pw[mi][i], c);
-            } else {
+                for (int mi = 0; mi < MI; ++mi) fetch_p(st_q, mi);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) c = mfma_bf16(__builtin_bit_cast(bf16x8, qr[s % RING][h]), __builtin_bit_cast(bf16x8, pr[mi][h]), c);
-            }
-            if constexpr (refill_p) {
-                __builtin_amdgcn_sched_barrier(0);
-                fetch_p(st_q, mi);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        });
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) acc[mi][s] = mfma_bf16(qw[i], pw[mi][i], acc[mi][s]);
+        } else {
+            each<MI>([&](auto mic) {
+                constexpr int mi = decltype(mic)::value;
+                f32x4& c = acc[mi][s];
+                if constexpr (MODE == COLS_FP8) {
+                    c = mfma_fp8<s % BQ, mi % BP>(qr[s % RING], pr[mi], c, qs[s / BQ], ps[mi / BP]);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) c = mfma_bf16(__builtin_bit_cast(bf16x8, qr[s % RING][h]), __builtin_bit_cast(bf16x8, pr[mi][h]), c);
+                }
+                if constexpr (refill_p) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    fetch_p(st_q, mi);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            });
+        }
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (refill_q) fetch_q(st_q, (s + RING) % NI);
-        constexpr int i = (s + RING) % NI;
+        constexpr int i = (s + RING) % NI, DEAL = STAGES > 2 ? NI : RING;
 #pragma unroll
-        for (int j = i * LPT / NI; j < (i + 1) * LPT / NI; ++j) load(j);
+        for (int j = i * LPT / DEAL; j < (i + 1) * LPT / DEAL && i < DEAL; ++j) load(j);
     };
     // A step: its first NI - RING slots (`head`), then, when the next step has landed everywhere and this one's stage is free (what is left of it is in registers), the last RING
     // (`edge`), which bring in the next step's first blocks and, P's as they are done with, all of P.
@@ -252,7 +271,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         fetch_scales(sn, ps_next, qs_next);
         each<RING>([&](auto i) {
             constexpr int s = NI - RING + decltype(i)::value;
-            slot(std::integral_constant<int, s>(), std::true_type(), std::integral_constant<bool, s == NI - 1>(), sn, load);
+            slot(std::integral_constant<int, s>(), std::true_type(), std::integral_constant<bool, s == (WIDE ? NI - RING : NI - 1)>(), sn, load);
         });
         if constexpr (FP8) {
 #pragma unroll
@@ -309,58 +328,66 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     }
     each<RING>([&](auto i) { slot(std::integral_constant<int, NI - RING + decltype(i)::value>(), std::false_type(), std::false_type(), 0, none); });
 
-    // ---- epilogue.  A lane has rows spread<BP>(mi, l16) of its wavefront's, and of each 16 BQ columns the 4 BQ from 4 BQ quad on.
-    constexpr int NG = NV / BQ, W4 = BQ;               // groups of 16 BQ columns; pieces of four columns of a lane in one
-    const uint16_t* const bias = P.bias;
-    auto column = [&](int g) { return n0 + wn_out + g * 16 * BQ + quad * 4 * BQ; };
-    // piece c of group g: columns 4 c .. 4 c + 3 of the lane's: element x is block (4 c + x) % BQ's, entry (4 c + x) / BQ
+    // ---- epilogue.  A lane has rows spread<BP>(mi, l16) of its wavefront's, and of each group of 16 BQ columns the 4 BQ from 4 BQ quad on.
+    constexpr int W4 = BQ, NG = NV / BQ;               // pieces of four columns of a lane in a group; groups
+    auto column = [&](int g) { return n0 + wn_out + (g * 4 + quad) * 4 * W4; };
+    auto row_of = [&](int mi) { return wm + spread<BP>(mi, l16); };
+    // element x of piece c of group g, of the blocks from `first` on
+    auto element = [&](int mi, int first, int g, int c, int x) -> float& { return reinterpret_cast<float(&)[4]>(acc[mi][first + g * BQ + (4 * c + x) % BQ])[(4 * c + x) / BQ]; };
     auto piece = [&](int mi, int first, int g, int c) {
-        f32x4 v;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) v[x] = acc[mi][first + g * BQ + (4 * c + x) % BQ][(4 * c + x) / BQ];
-        return v;
+        return f32x4{element(mi, first, g, c, 0), element(mi, first, g, c, 1), element(mi, first, g, c, 2), element(mi, first, g, c, 3)};
     };
-    auto bias4 = [&](const uint16_t* b, int col) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if (!b) return v;
-        if (col + 4 <= N) return load4(reinterpret_cast<const __bf16*>(b) + col);
-#pragma unroll
-        for (int x = 0; x < 3; ++x)
-            if (col + x < N) v[x] = bf16_to_f32(b[col + x]);
-        return v;
-    };
-    auto store = [&](auto* p, int64_t at, int col, f32x4 v) {
+    // the tile's bias, which a thread each has had in a register since the start (fetched here it would take a trip to memory, and held by every lane 16 registers)
+    float* const bias = reinterpret_cast<float*>(lds + STAGES * STAGE);
+    if (tid < BN) bias[tid] = bf16_to_f32(bias_raw);
+    __syncthreads();
+    // (a row's last columns one by one)
+    auto store = [&](auto* p, int64_t at, int col, const f32x4 (&v)[W4]) {
         using T = std::remove_pointer_t<decltype(p)>;
-        if (col + 4 <= N) store4(p + at, v);
-        else
+        if (col + 4 * W4 <= N) {
 #pragma unroll
-            for (int x = 0; x < 3; ++x)
-                if (col + x < N) p[at + x] = (T)v[x];
+            for (int c = 0; c < W4; c += 2) {
+                if constexpr (std::is_same_v<T, float>) {
+                    store4(p + at + 4 * c, v[c]);
+                    store4(p + at + 4 * c + 4, v[c + 1]);
+                } else {
+                    store8(p + at + 4 * c, f32x8{v[c], v[c + 1]});
+                }
+            }
+        } else
+#pragma unroll
+            for (int x = 0; x < 4 * W4; ++x)
+                if (col + x < N) p[at + x] = (T)v[x / 4][x % 4];
     };
-    auto residual4 = [&](auto* p, int64_t at, int col) {
-        if (col + 4 <= N) return load4(p + at);
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](auto* p, int64_t at, int col, f32x4 (&v)[W4]) {
+        if (col + 4 * W4 <= N) {
 #pragma unroll
-        for (int x = 0; x < 3; ++x)
-            if (col + x < N) v[x] = (float)p[at + x];
-        return v;
+            for (int c = 0; c < W4; c += 2) {
+                const f32x8 r = load8(p + at + 4 * c);
+                v[c] += r.lo;
+                v[c + 1] += r.hi;
+            }
+        } else
+#pragma unroll
+            for (int x = 0; x < 4 * W4; ++x)
+                if (col + x < N) v[x / 4][x % 4] += (float)p[at + x];
     };
     __bf16* const zb = reinterpret_cast<__bf16*>(P.z);
-    uint32_t top[OUT8 ? MI : 1];
+    float top[OUT8 ? MI : 1];
 #pragma unroll
-    for (int mi = 0; mi < (OUT8 ? MI : 1); ++mi) top[mi] = 0;
+    for (int mi = 0; mi < (OUT8 ? MI : 1); ++mi) top[mi] = 0.f;
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
         const int col = column(gr);
         f32x4 bv[W4], bg[W4];
 #pragma unroll
         for (int c = 0; c < W4; ++c) {
-            bv[c] = bias4(bias, col + 4 * c);
-            if (GATED) bg[c] = bias4(bias ? bias + N : nullptr, col + 4 * c);
+            bv[c] = *reinterpret_cast<const f32x4*>(bias + col - n0 + 4 * c);
+            if (GATED) bg[c] = *reinterpret_cast<const f32x4*>(bias + BN_OUT + col - n0 + 4 * c);
         }
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
-            const int m = m0 + wm + spread<BP>(mi, l16);
+            const int m = m0 + row_of(mi);
             f32x4 v[W4], g[W4];
 #pragma unroll
             for (int c = 0; c < W4; ++c) {
@@ -368,54 +395,56 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
                 if (GATED) g[c] = piece(mi, GATED ? NV : 0, gr, c) + bg[c];
             }
             if constexpr (GATED) {
-                if (!OUT8 && P.z && m < M)
-#pragma unroll
-                    for (int c = 0; c < W4; ++c) {
-                        store(zb, (int64_t)m * 2 * N + col + 4 * c, col + 4 * c, v[c]);
-                        store(zb, (int64_t)m * 2 * N + N + col + 4 * c, col + 4 * c, g[c]);
-                    }
+                if (!OUT8 && P.z && m < M) {
+                    store(zb, (int64_t)m * 2 * N + col, col, v);
+                    store(zb, (int64_t)m * 2 * N + N + col, col, g);
+                }
                 apply_act(P.act, g);
 #pragma unroll
                 for (int c = 0; c < W4; ++c) v[c] *= g[c];
             } else {
                 apply_act(P.act, v);
-                if (P.res && m < M)
-#pragma unroll
-                    for (int c = 0; c < W4; ++c) {
-                        const int64_t at = (int64_t)m * N + col + 4 * c;
-                        v[c] += P.y_f32 ? residual4(static_cast<const float*>(P.res), at, col + 4 * c) : residual4(static_cast<const __bf16*>(P.res), at, col + 4 * c);
-                    }
+                if (P.res && m < M) {
+                    if (P.y_f32) add(static_cast<const float*>(P.res), (int64_t)m * N + col, col, v);
+                    else add(static_cast<const __bf16*>(P.res), (int64_t)m * N + col, col, v);
+                }
             }
             if constexpr (OUT8) {
-                // kept where the value's sums were, until the block's largest is known
+                // kept where the value's sums were, until the block's largest is known (N is a multiple of 16: a lane's columns are all there or none)
 #pragma unroll
                 for (int c = 0; c < W4; ++c) {
-                    if (col + 4 * c < N) top[mi] = fp8_magnitude(top[mi], v[c]);
+                    if (col < N) top[mi] = fp8_top(top[mi], v[c]);
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) acc[mi][gr * BQ + (4 * c + x) % BQ][(4 * c + x) / BQ] = v[c][x];
+                    for (int x = 0; x < 4; ++x) element(mi, 0, gr, c, x) = v[c][x];
                 }
             } else if (m < M) {
-#pragma unroll
-                for (int c = 0; c < W4; ++c) {
-                    const int64_t at = (int64_t)m * N + col + 4 * c;
-                    if (P.y_f32) store(static_cast<float*>(P.y), at, col + 4 * c, v[c]);
-                    else store(static_cast<__bf16*>(P.y), at, col + 4 * c, v[c]);
-                }
+                if (P.y_f32) store(static_cast<float*>(P.y), (int64_t)m * N + col, col, v);
+                else store(static_cast<__bf16*>(P.y), (int64_t)m * N + col, col, v);
             }
         }
     }
     if constexpr (OUT8) {
-        uint32_t* const meet = reinterpret_cast<uint32_t*>(lds + STAGES * STAGE);      // [WGN][BM]
+        uint32_t* const meet = reinterpret_cast<uint32_t*>(bias + BN);      // [WGN][BM]
+        bool finite = true;
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
-            uint32_t u = max(top[mi], (uint32_t)__shfl_xor((int)top[mi], 16));
+            uint32_t u = __float_as_uint(top[mi]);
+            if (u >= 0x7f800000u) {
+                finite = false;
+                u = 0;
+#pragma unroll
+                for (int i = 0; i < NG * W4; ++i)
+                    if (column(i / W4) < N) u = fp8_magnitude(u, piece(mi, 0, i / W4, i % W4));
+            }
+            u = max(u, (uint32_t)__shfl_xor((int)u, 16));
             u = max(u, (uint32_t)__shfl_xor((int)u, 32));
-            if (quad == 0) meet[(wave % WGN) * BM + wm + spread<BP>(mi, l16)] = u;
+            if (quad == 0) meet[(wave % WGN) * BM + row_of(mi)] = u;
         }
         __syncthreads();
+        const bool plain = __all(finite);
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
-            const int r = wm + spread<BP>(mi, l16), m = m0 + r;
+            const int r = row_of(mi), m = m0 + r;
             uint32_t u = 0;
 #pragma unroll
             for (int w = 0; w < WGN; ++w) u = max(u, meet[w * BM + r]);
@@ -426,9 +455,13 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
                     u32x4 w;
+                    if (plain)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) w[c] = fp8_pack(piece(mi, 0, g, c), inv);
-                    const int col = column(g);         // (N is a multiple of 16)
+                        for (int c = 0; c < 4; ++c) w[c] = fp8_pack_finite(piece(mi, 0, g, c), inv);
+                    else
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) w[c] = fp8_pack(piece(mi, 0, g, c), inv);
+                    const int col = column(g);
                     if (col < N) *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(P.y) + (int64_t)m * N + col) = w;
                 }
             }
@@ -599,13 +632,32 @@ __global__ __launch_bounds__(64 * FEW_NW) void few_rows_kernel(const ColsProblem
 }
 
 // ---- launches
+// (threads of a launch stay below 2^32)
+inline bool cols_too_many(int64_t M, int64_t N, bool gated) { return ((M + 63) / 64) * (((gated ? 2 : 1) * N + 63) / 64) >= 1 << 22; }
+
+// Which tiles: the ones whose launch is taken to be the shortest, us.  `slots` workgroups fit the chip; every full round of them takes rest + step for each 128 bytes of K, and so does
+// the last, or, with no more than a workgroup a CU where there is room for two, alone_rest and alone_step.  (Fitted to launches of 16 to 8192 rows and five widths and depths from 320 to 5120 each, cold: off by
+// 6 to 17 %, but what matters is which is least.)
+struct ColsTile { int bm, bn, slots; float base, rest, step, alone_rest, alone_step; };
+template <int TILES>
+inline int cols_choose(const ColsTile (&tiles)[TILES], int64_t M, int64_t columns, int64_t Kb, float& least) {
+    int best = 0;
+    least = 0.f;
+    const float steps = (float)((Kb + 127) / 128);
+    for (int i = 0; i < TILES; ++i) {
+        const ColsTile& t = tiles[i];
+        const int64_t n = ((M + t.bm - 1) / t.bm) * ((columns + t.bn - 1) / t.bn), left = n % t.slots;
+        const float us = t.base + (float)(n / t.slots + (left > 256 ? 1 : 0)) * (t.rest + steps * t.step) + (left > 0 && left <= 256 ? t.alone_rest + steps * t.alone_step : 0.f);
+        if (i == 0 || us < least) best = i, least = us;
+    }
+    return best;
+}
 template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8>
 static int launch_cols(ColsProblem& P, hipStream_t stream) {
     constexpr int BN_OUT = GATED ? BN / 2 : BN;
     P.tiles_m = (P.M + BM - 1) / BM;
     P.tiles_n = (P.N + BN_OUT - 1) / BN_OUT;
     const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n;
-    SD_REQUIRE(tiles < (1 << 22), SD_EUNSUPPORTED, "linear: M=%d N=%d: 2^22 tiles and more", P.M, P.N);        // (threads of a launch stay below 2^32)
     const bool guard = P.Kb % 128 != 0;
     if (SD_DRY_RUN("gemm cols%s%s%s %dx%d/%d waves/%d stages%s; ", MODE == COLS_BF16 ? "" : MODE == COLS_FP8 ? " 8 bits" : " 8 bits wide", GATED ? " gated" : "", OUT8 ? " to 8 bits" : "", BM, BN, WGM * WGN, STAGES, guard ? " guard" : "")) return SD_OK;
     const dim3 grid((unsigned)((tiles + 7) & ~7ll)), block(64 * WGM * WGN);

@@ -14,6 +14,7 @@ static int linear8_check(const char* who, const uint8_t* x, const uint8_t* x_sca
     SD_REQUIRE(M < (1 << 27) && N < (1 << 22), SD_EUNSUPPORTED, "%s: M=%d N=%d (M below 2^27, N below 2^22)", who, M, N);
     SD_REQUIRE(act >= SD_ACT_NONE && act <= SD_ACT_RELU, SD_EINVAL, "%s: activation %d", who, act);
     SD_REQUIRE(K > 0 && K % 16 == 0 && K < (1 << 22), SD_EUNSUPPORTED, "%s: K=%d is not a positive multiple of 16 below 2^22", who, K);
+    SD_REQUIRE(!cols_too_many(M, w_rows, false), SD_EUNSUPPORTED, "%s: M=%d N=%d (2^22 tiles of 64 x 64 and more)", who, M, N);
     if (M == 0 || N == 0) return SD_OK;
     const int rc = fp8_check(who, "x", x, x_scales, x_lds, M, K);
     return rc ? rc : fp8_check(who, "W", W, w_scales, w_lds, w_rows, K);
@@ -26,6 +27,55 @@ static ColsProblem problem8(const uint8_t* x, const uint8_t* x_scales, int64_t x
     P.bias = bias; P.act = act; P.y = y;
     P.M = M; P.N = N; P.Kb = K;
     return P;
+}
+
+// Tiles (gemm_cols.hpp's rule).  The fastest of 50 launches each: it takes launches 1.1 % (plain), 0.4 % (gated), 0 % (to 8 bits), 2 % (y in fp32) longer than theirs in the mean.
+static const ColsTile PLAIN8[] = {{256, 256, 256, 0.f, 7.1f, 1.134f, 7.1f, 1.134f}, {128, 256, 256, 0.f, 5.7f, 0.62f, 5.7f, 0.62f}, {256, 128, 256, 0.f, 5.5f, 0.618f, 5.5f, 0.618f},
+                                  {128, 128, 512, 0.f, 6.6f, 1.027f, 3.9f, 0.669f}, {64, 128, 512, 0.2f, 3.5f, 0.704f, 3.5f, 0.302f}, {64, 64, 512, 1.1f, 2.3f, 0.409f, 2.3f, 0.189f}};
+static const ColsTile GATED8[] = {{256, 256, 256, 0.f, 5.7f, 1.4f, 5.7f, 1.4f}, {128, 256, 256, 0.f, 4.9f, 0.744f, 4.9f, 0.744f}, {256, 128, 256, 0.f, 5.f, 0.675f, 5.f, 0.675f},
+                                  {128, 128, 512, 0.f, 4.7f, 0.994f, 3.7f, 0.762f}, {64, 128, 512, 1.4f, 2.7f, 0.655f, 2.1f, 0.381f}, {64, 64, 512, 0.f, 2.8f, 0.528f, 3.5f, 0.306f}};
+static const ColsTile GATED8_TO_8[] = {{256, 256, 256, 0.f, 6.8f, 1.32f, 6.8f, 1.32f}, {128, 256, 256, 0.f, 5.4f, 0.735f, 5.4f, 0.735f}, {64, 256, 256, 0.7f, 4.2f, 0.626f, 4.2f, 0.626f}};
+static const ColsTile WIDE8[] = {{128, 128, 512, 0.3f, 16.7f, 1.407f, 7.5f, 1.071f}, {64, 128, 512, 1.9f, 8.7f, 0.94f, 3.1f, 0.601f}, {64, 64, 512, 1.1f, 5.1f, 0.566f, 3.3f, 0.406f}};
+
+// Few rows: straight from the weights where that is one workgroup a CU.  With y in fp32, whose tiles are slower, with more rows and columns a workgroup too.  (us, these kernels / tiles:
+// 32 x 1280 x 5120 7.7 / 10.6, 32 x 1280 x 1280 4.1 / 5.1, 64 x 1280 x 5120 10.3 / 11.1, but 128 of them 12.9 / 11.2; y in fp32 256 x 1280 x 1280 7.3 / 8.4, 128 of them 5.9 / 8.3.)
+template <bool GATED>
+static int launch_few8(const ColsProblem& P, bool& taken, hipStream_t s) {
+    const int64_t r16 = (P.M + 15) / 16, r32 = (P.M + 31) / 32, c16 = (P.N + 15) / 16, c32 = (P.N + 31) / 32;
+    taken = true;
+    if (r16 * c16 <= 256) return launch_few<true, GATED, 1, 1, GATED ? 2 : 4>(P, s);
+    if (r32 * c16 <= 256) return launch_few<true, GATED, 2, 1, GATED ? 2 : 4>(P, s);
+    if (P.y_f32 && r32 * c32 <= 256) return launch_few<true, GATED, 2, 2, GATED ? 2 : 3>(P, s);
+    if constexpr (!GATED)
+        if (P.y_f32 && (P.M + 63) / 64 * c32 <= 256) return launch_few<true, false, 4, 2, 2>(P, s);
+    taken = false;
+    return SD_OK;
+}
+// y in 8 bits by way of fp32, in two launches: where a block's columns lie in several workgroups (few rows, smaller tiles), which a long reduction makes up for.  (us, one launch / two, of which the second
+// and its start are some 6: 64 x 1280 x 5120 30.2 / 18, 256 of them 32.5 / 22; 64 x 5120 x 1280 11.6 / 13.)
+static bool gated8_two_launches(int M, int N, int K) {
+    float one, two;
+    cols_choose(GATED8_TO_8, M, 2ll * N, K, one);
+    cols_choose(GATED8, M, 2ll * N, K, two);
+    if ((int64_t)((M + 15) / 16) * ((N + 15) / 16) <= 256) two = 3.f + 0.18f * (float)((K + 127) / 128);
+    return two + 6.f + (float)M * N * 2e-6f < one;
+}
+static int launch_gated8(ColsProblem& P, bool wide, hipStream_t s) {
+    float us;
+    if (wide)
+        switch (cols_choose(WIDE8, P.M, 2ll * P.N, P.Kb, us)) {
+        case 0: return launch_cols<COLS_FP8_WIDE, 128, 128, 2, 2, 2, true, false>(P, s);
+        case 1: return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 2, 3, true, false>(P, s);
+        default: return launch_cols<COLS_FP8_WIDE, 64, 64, 2, 1, 4, true, false>(P, s);
+        }
+    switch (cols_choose(GATED8, P.M, 2ll * P.N, P.Kb, us)) {
+    case 0: return launch_cols<COLS_FP8, 256, 256, 2, 4, 2, true, false>(P, s);
+    case 1: return launch_cols<COLS_FP8, 128, 256, 2, 4, 3, true, false>(P, s);
+    case 2: return launch_cols<COLS_FP8, 256, 128, 4, 2, 3, true, false>(P, s);
+    case 3: return launch_cols<COLS_FP8, 128, 128, 2, 2, 2, true, false>(P, s);
+    case 4: return launch_cols<COLS_FP8, 64, 128, 2, 2, 3, true, false>(P, s);
+    default: return launch_cols<COLS_FP8, 64, 64, 2, 1, 4, true, false>(P, s);
+    }
 }
 
 }  // namespace sd
@@ -45,17 +95,28 @@ extern "C" int sd_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int6
     P.res = residual;
     P.y_f32 = y_dtype == SD_F32;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (M <= 16) return launch_few<true, false, 1, 1, 4>(P, s);
-    if (P.y_f32) return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 2, 3, false, false>(P, s);
-    if (M <= 512) return launch_cols<COLS_FP8, 64, 128, 2, 2, 3, false, false>(P, s);
-    return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, false, false>(P, s);
+    bool taken;
+    const int few = launch_few8<false>(P, taken, s);
+    if (taken) return few;
+    float us;
+    if (P.y_f32)
+        switch (cols_choose(WIDE8, M, N, K, us)) {
+        case 0: return launch_cols<COLS_FP8_WIDE, 128, 128, 2, 2, 2, false, false>(P, s);
+        case 1: return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 4, 3, false, false>(P, s);
+        default: return launch_cols<COLS_FP8_WIDE, 64, 64, 2, 2, 4, false, false>(P, s);
+        }
+    switch (cols_choose(PLAIN8, M, N, K, us)) {
+    case 0: return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, false, false>(P, s);
+    case 1: return launch_cols<COLS_FP8, 128, 256, 2, 4, 3, false, false>(P, s);
+    case 2: return launch_cols<COLS_FP8, 256, 128, 4, 2, 3, false, false>(P, s);
+    case 3: return launch_cols<COLS_FP8, 128, 128, 2, 2, 2, false, false>(P, s);
+    case 4: return launch_cols<COLS_FP8, 64, 128, 2, 2, 3, false, false>(P, s);
+    default: return launch_cols<COLS_FP8, 64, 64, 2, 2, 4, false, false>(P, s);
+    }
 }
 
-// few rows whose y goes out in 8 bits: y in fp32 first, as a block's columns lie in several workgroups
-static bool gated8_few(int M) { return M <= 16; }
 extern "C" size_t sd_gated_linear_fp8_workspace_bytes(int32_t M, int32_t N, int32_t K) {
-    (void)K;
-    if (M <= 0 || N <= 0 || !gated8_few(M) || N >= (1 << 22)) return 256;
+    if (M <= 0 || N <= 0 || K <= 0 || M >= (1 << 27) || N >= (1 << 21) || !gated8_two_launches(M, N, K)) return 0;
     return round_up((size_t)M * N * 4, 256);
 }
 
@@ -78,22 +139,24 @@ extern "C" int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales
     ColsProblem P = problem8(x, x_scales, x_lds, W, w_scales, w_lds, bias, act, y, M, N, K);
     P.y_f32 = y_dtype == SD_F32;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (gated8_few(M)) {
-        if (!out8) return launch_few<true, true, 1, 1, 2>(P, s);
+    bool taken;
+    if (out8 && !gated8_two_launches(M, N, K)) {
+        P.ys = y_scales;
+        P.ldys = y_lds;
+        float us;
+        switch (cols_choose(GATED8_TO_8, M, 2ll * N, K, us)) {
+        case 0: return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, true, true>(P, s);
+        case 1: return launch_cols<COLS_FP8, 128, 256, 4, 2, 3, true, true>(P, s);
+        default: return launch_cols<COLS_FP8, 64, 256, 2, 2, 3, true, true>(P, s);
+        }
+    }
+    if (out8) {
         const size_t need = sd_gated_linear_fp8_workspace_bytes(M, N, K);
         SD_REQUIRE(ws && ws_bytes >= need && (reinterpret_cast<uintptr_t>(ws) & 255u) == 0, SD_EWORKSPACE, "gated_linear_fp8_fwd: workspace of %zu bytes, need %zu, 256-byte aligned", ws_bytes, need);
         P.y = ws;
         P.y_f32 = 1;
-        rc = launch_few<true, true, 1, 1, 2>(P, s);
-        return rc ? rc : launch_quantize(ws, true, static_cast<uint8_t*>(y), y_scales, y_lds, M, N, s);
     }
-    if (out8) {
-        P.ys = y_scales;
-        P.ldys = y_lds;
-        if (M <= 512) return launch_cols<COLS_FP8, 128, 256, 4, 2, 3, true, true>(P, s);
-        return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, true, true>(P, s);
-    }
-    if (P.y_f32) return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 2, 3, true, false>(P, s);
-    if (M <= 512) return launch_cols<COLS_FP8, 64, 128, 2, 2, 3, true, false>(P, s);
-    return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, true, false>(P, s);
+    rc = launch_few8<true>(P, taken, s);
+    if (!taken) rc = launch_gated8(P, y_dtype == SD_F32, s);
+    return rc || !out8 ? rc : launch_quantize(ws, true, static_cast<uint8_t*>(y), y_scales, y_lds, M, N, s);
 }
