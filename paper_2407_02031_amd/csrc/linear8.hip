@@ -58,7 +58,7 @@ static bool gated8_two_launches(int M, int N, int K) {
     cols_choose(GATED8_TO_8, M, 2ll * N, K, one);
     cols_choose(GATED8, M, 2ll * N, K, two);
     if ((int64_t)((M + 15) / 16) * ((N + 15) / 16) <= 256) two = 3.f + 0.18f * (float)((K + 127) / 128);
-    return two + 6.f + (float)M * N * 2e-6f < one;
+    return two + 9.f + (float)M * N * 2e-6f < one;
 }
 static int launch_gated8(ColsProblem& P, bool wide, hipStream_t s) {
     float us;

@@ -477,7 +477,7 @@ def rows8(B, g, M, K, scale=1.0, spread=1.0):
 
 
 def product(x, W, bias, fp32):
-    """z and its bound.  Products are exact.  In bf16 (few rows, or y in fp32) every one of K + 8 additions may be off by 2 U of the sum of magnitudes.  The scaled MFMA adds
+    """z and its bound.  Products are exact.  In bf16 (y in fp32, and few rows, for which this bound is the looser one too) every one of K + 8 additions may be off by 2 U of the sum of magnitudes.  The scaled MFMA adds
     eight products at a time and drops what is below 2^-13 of the largest one's power of two: seven of them lose less than 2^-13 of it each."""
     xd, wd = values(x), values(W)
     z, mag = xd @ wd.T, xd.abs() @ wd.abs().T
@@ -485,7 +485,7 @@ def product(x, W, bias, fp32):
         z, mag = z + bias.double(), mag + bias.double().abs()
     M, K = x.q.shape
     e = (K + 8) * 2 * U * mag
-    if not fp32 and M > 16:
+    if not fp32:
         xa, wa = xd.abs().float(), wd.abs().float()
         top = sum((xa[:, None, k:k + 8] * wa[None, :, k:k + 8]).amax(2).double() for k in range(0, K, 8)) if M * wd.shape[0] <= 1 << 20 else mag
         e = e + 7 * 2.0 ** -13 * top
@@ -607,6 +607,162 @@ def test_fp8_special_values(B):
     e = B.Fp8Rows(x8.q[:0], x8.scales[:, :0])
     assert B.linear_fp8_fwd(e, W8).shape == (0, 48) and B.gated_linear_fp8_fwd(e, B.Fp8Rows(W8.q[:32], W8.scales[:, :32]), out_dtype=torch.float8_e4m3fn).q.shape == (0, 16)
     assert B.linear_fp8_fwd(x8, B.Fp8Rows(W8.q[:0], W8.scales[:, :0])).shape == (600, 0)
+
+
+LIN8_KERNELS = [("bfloat16", *c) for c in [
+    (1, 1, 768, "few rows 8 bits 16x16"), (4579, 1, 768, "few rows 8 bits 32x16"), (849, 2353, 768, "gemm cols 8 bits 128x128/4 waves/2 stages"), (8807, 197, 784, "gemm cols 8 bits 128x128/4 waves/2 stages guard"),
+    (1310, 5559, 768, "gemm cols 8 bits 128x256/8 waves/3 stages"), (1325, 5606, 16, "gemm cols 8 bits 128x256/8 waves/3 stages guard"), (8380, 424, 768, "gemm cols 8 bits 256x128/8 waves/3 stages"),
+    (11162, 289, 864, "gemm cols 8 bits 256x128/8 waves/3 stages guard"), (9654, 792, 128, "gemm cols 8 bits 256x256/8 waves/2 stages"), (3914, 2073, 768, "gemm cols 8 bits 256x256/8 waves/2 stages"),
+    (10005, 781, 800, "gemm cols 8 bits 256x256/8 waves/2 stages guard"), (11378, 129, 128, "gemm cols 8 bits 64x128/4 waves/3 stages"), (8735, 73, 768, "gemm cols 8 bits 64x128/4 waves/3 stages"),
+    (8200, 72, 944, "gemm cols 8 bits 64x128/4 waves/3 stages guard"), (1, 4216, 768, "gemm cols 8 bits 64x64/4 waves/4 stages"), (3, 4463, 784, "gemm cols 8 bits 64x64/4 waves/4 stages guard")]] + [("float32", *c) for c in [
+    (4281, 1, 768, "few rows 8 bits 32x16"), (1, 4228, 784, "few rows 8 bits 32x32"), (8397, 1, 16, "few rows 8 bits 64x32"), (11391, 154, 768, "gemm cols 8 bits wide 128x128/4 waves/2 stages"),
+    (11271, 153, 784, "gemm cols 8 bits wide 128x128/4 waves/2 stages guard"), (8239, 67, 896, "gemm cols 8 bits wide 64x128/8 waves/3 stages"), (9071, 78, 16, "gemm cols 8 bits wide 64x128/8 waves/3 stages guard"),
+    (71, 4864, 768, "gemm cols 8 bits wide 64x64/4 waves/4 stages"), (66, 4143, 816, "gemm cols 8 bits wide 64x64/4 waves/4 stages guard")]]
+
+
+@pytest.mark.parametrize("yt,M,N,K,kernel", LIN8_KERNELS)
+def test_linear_fp8_every_kernel(B, yt, M, N, K, kernel):
+    """Each kernel with and without bias and residual; the choice does not depend on them."""
+    import torch
+    yt, g = getattr(torch, yt), gen(M + K)
+    x, W = rows8(B, g, M, K), rows8(B, g, N, K, 1.3 / math.sqrt(K), 0.3)
+    bias, res = randn(g, N, scale=0.5).bfloat16(), randn(g, M, N, dtype=yt)
+    with B.dry_run() as names:
+        B.linear_fp8_fwd(x, W, bias, 1, residual=res, out_dtype=yt)
+        B.linear_fp8_fwd(x, W, out_dtype=yt)
+    assert names == [kernel] * 2
+    check_linear8(B, x, W, bias, 3, res, yt)
+    check_linear8(B, x, W, None, 0, None, yt)
+
+
+GATED8_KERNELS = [("bfloat16", *c) for c in [
+    (1, 16, 768, "few rows 8 bits gated 16x16"), (17, 2096, 768, "few rows 8 bits gated 32x16"), (149, 5616, 128, "gemm cols 8 bits gated 128x128/4 waves/2 stages"), (4934, 800, 1280, "gemm cols 8 bits gated 128x128/4 waves/2 stages"),
+    (808, 4640, 912, "gemm cols 8 bits gated 128x128/4 waves/2 stages guard"), (525, 5600, 768, "gemm cols 8 bits gated 128x256/8 waves/3 stages"), (10904, 144, 16, "gemm cols 8 bits gated 128x256/8 waves/3 stages guard"),
+    (555, 5504, 928, "gemm cols 8 bits gated 128x256/8 waves/3 stages guard"), (11125, 144, 768, "gemm cols 8 bits gated 256x128/8 waves/3 stages"), (10904, 144, 800, "gemm cols 8 bits gated 256x128/8 waves/3 stages guard"),
+    (10892, 336, 768, "gemm cols 8 bits gated 256x256/8 waves/2 stages"), (6700, 592, 784, "gemm cols 8 bits gated 256x256/8 waves/2 stages guard"), (65, 4416, 768, "gemm cols 8 bits gated 64x128/4 waves/3 stages"),
+    (69, 4544, 832, "gemm cols 8 bits gated 64x128/4 waves/3 stages guard"), (1, 4144, 768, "gemm cols 8 bits gated 64x64/2 waves/4 stages"), (1, 4256, 848, "gemm cols 8 bits gated 64x64/2 waves/4 stages guard")]] + [("float32", *c) for c in [
+    (17, 2224, 784, "few rows 8 bits gated 32x16"), (1, 4288, 768, "few rows 8 bits gated 32x32"), (130, 5600, 896, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages"),
+    (145, 5632, 784, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages guard"), (70, 4336, 768, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages"), (67, 4480, 848, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages guard"),
+    (8255, 16, 768, "gemm cols 8 bits wide gated 64x64/2 waves/4 stages"), (8909, 16, 784, "gemm cols 8 bits wide gated 64x64/2 waves/4 stages guard")]] + [("float8_e4m3fn", *c) for c in [
+    (1, 16, 1936, "few rows 8 bits gated 16x16; quantize"), (9309, 144, 768, "gemm cols 8 bits gated to 8 bits 128x256/8 waves/3 stages"), (9045, 144, 880, "gemm cols 8 bits gated to 8 bits 128x256/8 waves/3 stages guard"),
+    (6662, 544, 768, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages"), (11037, 272, 784, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages guard"), (1, 16, 768, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages"),
+    (3, 144, 784, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages guard")]]
+
+
+@pytest.mark.parametrize("yt,M,N,K,kernel", GATED8_KERNELS)
+def test_gated_fp8_every_kernel(B, yt, M, N, K, kernel):
+    import torch
+    yt, g = getattr(torch, yt), gen(M + K)
+    x, W = rows8(B, g, M, K), rows8(B, g, 2 * N, K, 1.3 / math.sqrt(K), 0.3)
+    bias = randn(g, 2 * N, scale=0.5).bfloat16()
+    with B.dry_run() as names:
+        B.gated_linear_fp8_fwd(x, W, bias, 1, out_dtype=yt)
+        B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=yt)
+    assert "; ".join(names) == "; ".join([kernel] * 2)
+    check_gated8(B, x, W, bias, 3, yt)
+    check_gated8(B, x, W, None, 2, yt)
+
+
+@pytest.mark.parametrize("M,N,K", [(300, 1296, 5120), (130, 640, 4112)])
+def test_gated_fp8_in_two_launches(B, M, N, K):
+    """Tiles whose columns are not whole blocks of y: y in fp32 into the workspace, which is all that is asked for"""
+    import torch
+    g = gen(M)
+    x, W = rows8(B, g, M, K), rows8(B, g, 2 * N, K, 1.3 / math.sqrt(K), 0.3)
+    need = B.lib().sd_gated_linear_fp8_workspace_bytes(M, N, K)
+    assert need == M * N * 4
+    with B.dry_run() as names:
+        B.gated_linear_fp8_fwd(x, W, out_dtype=torch.float8_e4m3fn)
+    assert len(names) == 2 and names[1] == "quantize"
+    y = check_gated8(B, x, W, None, 3, torch.float8_e4m3fn)
+    ws = torch.full((need + 256,), 77, dtype=torch.uint8, device="cuda")
+    mine = B.gated_linear_fp8_fwd(x, W, out_dtype=torch.float8_e4m3fn, ws=ws)
+    assert torch.equal(mine.q.view(torch.uint8), y.q.view(torch.uint8)) and (ws[need:] == 77).all()
+
+
+def test_scales_at_their_ends(B):
+    """The least, the largest and the NaN scale byte, as a caller's own rows may have them, mean the same in every kernel"""
+    import torch
+    g = gen(11)
+    K, N = 256, 48
+    W = rows8(B, g, N, K, 1.0, 0.0)
+    for M in (3, 600):
+        for yt in (torch.bfloat16, torch.float32):
+            x = rows8(B, g, M, K, 1.0, 0.0)
+            s = x.scales.contiguous().view(torch.uint8).clone()
+            s[0, 1], s[1, 2] = 255, 0                     # NaN; 2^-127
+            s = torch.nn.functional.pad(s, (0, -M % 4)).view(torch.float8_e8m0fnu)[:, :M]
+            mine = B.Fp8Rows(x.q, s)
+            y, clean = B.linear_fp8_fwd(mine, W, out_dtype=yt), B.linear_fp8_fwd(x, W, out_dtype=yt)
+            assert y[1].isnan().all()
+            keep = [i for i in range(M) if i not in (1, 2)]
+            assert torch.equal(y[keep], clean[keep])
+            # row 2 is its first block's product alone: the second's, below 2^-127 * 448^2 * 128, is nothing beside it
+            first = values(x)[2:3, :128] @ values(W)[:, :128].T
+            assert torch.allclose(y[2:3].double(), first, rtol=2.0 ** -7, atol=1e-2 * float(first.abs().max()))
+        big = B.quantize_fp8(torch.full((M, K), 2.0 ** 100, device="cuda"))
+        tiny = B.quantize_fp8(torch.full((16, K), 2.0 ** -100, device="cuda"))
+        for yt in (torch.bfloat16, torch.float32):
+            assert (B.linear_fp8_fwd(big, tiny, out_dtype=yt) == 256).all()
+
+
+def test_fp8_offsets_past_32_bits(B):
+    """Rows of x, of W and of y beyond 2^32 bytes"""
+    import torch
+    K = 4096
+    M = 2 ** 32 // K + 70
+    x = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, M, 65536):
+        x[i:i + 65536].normal_()
+    x8 = B.quantize_fp8(x)
+    del x
+    few = lambda a, rows: B.Fp8Rows(a.q[rows], torch.nn.functional.pad(a.scales[:, rows].view(torch.uint8), (0, -len(range(*rows.indices(a.q.shape[0]))) % 4)).view(torch.float8_e8m0fnu)[:, :len(range(*rows.indices(a.q.shape[0])))])
+    last = slice(M - 70, M)
+    W = rows8(B, gen(1), 32, K, 1 / 64, 0.0)
+    y = B.linear_fp8_fwd(x8, W)
+    z, ez = product(few(x8, last), W, None, False)
+    within(y[last], z, ez)
+    # as weights: value and gate far apart
+    xs = rows8(B, gen(2), 20, K, 1 / 64, 0.0)
+    N = M // 32 * 16
+    Wg = B.Fp8Rows(x8.q[:2 * N], x8.scales[:, :2 * N])
+    for yt in (torch.float8_e4m3fn, torch.bfloat16):
+        y = B.gated_linear_fp8_fwd(xs, Wg, None, 0, out_dtype=yt)
+        y = values(y) if yt == torch.float8_e4m3fn else y.double()
+        cols = slice(N - 128, N)
+        v, g = (product(xs, few(x8, slice(s + N - 128, s + N)), None, False)[0] for s in (0, N))
+        assert float((y[:, cols] - v * g).norm() / (v * g).norm()) < 2.0 ** -4
+    del y, Wg, x8
+    # a y of more than 2^32 bytes, in bf16 and its z
+    M, N = 40000, 54016
+    x, W, bias, g = lin_inputs(M, 2 * N, 64, 5)
+    y, z = B.gated_linear_fwd(x, W, bias, save_z=True)
+    assert y.numel() * 2 > 2 ** 32
+    rows = slice(M - 40, M)
+    check = B.gated_linear_fwd(x[rows].contiguous(), W, bias, save_z=True)
+    zr = x[rows].double() @ W.double().T + bias.double()
+    within(z[rows], zr, 72 * U * (x[rows].double().abs() @ W.double().abs().T + bias.double().abs()))
+    assert float((y[rows].double() - check[0].double()).norm() / check[0].double().norm()) < 2.0 ** -8
+
+
+GATED_KERNELS = [(1, 1, 384, "few rows gated 16x16"), (4249, 1, 8, "few rows gated 32x16"), (3, 4271, 392, "few rows gated 32x32"), (8507, 74, 64, "gemm cols gated 128x128/4 waves/2 stages"), (5481, 162, 384, "gemm cols gated 128x128/4 waves/2 stages"),
+                 (141, 5711, 464, "gemm cols gated 128x128/4 waves/2 stages guard"), (524, 5757, 384, "gemm cols gated 128x256/8 waves/3 stages"), (2420, 1606, 400, "gemm cols gated 128x256/8 waves/3 stages guard"),
+                 (5466, 350, 384, "gemm cols gated 256x128/8 waves/3 stages"), (11124, 129, 408, "gemm cols gated 256x128/8 waves/3 stages guard"), (10947, 334, 64, "gemm cols gated 256x256/8 waves/2 stages"),
+                 (10947, 334, 384, "gemm cols gated 256x256/8 waves/2 stages"), (770, 5075, 392, "gemm cols gated 256x256/8 waves/2 stages guard"), (8523, 34, 384, "gemm cols gated 64x128/4 waves/3 stages"),
+                 (9192, 37, 392, "gemm cols gated 64x128/4 waves/3 stages guard"), (8277, 1, 384, "gemm cols gated 64x64/2 waves/4 stages"), (8417, 3, 464, "gemm cols gated 64x64/2 waves/4 stages guard")]
+
+
+@pytest.mark.parametrize("M,N,K,kernel", GATED_KERNELS)
+def test_gated_fwd_every_kernel(B, M, N, K, kernel):
+    import torch
+    x, W, bias, _ = lin_inputs(M, 2 * N, K, M + K)
+    for yt in (torch.bfloat16, torch.float32):
+        with B.dry_run() as names:
+            B.gated_linear_fwd(x, W, bias, out_dtype=yt, save_z=True)
+            B.gated_linear_fwd(x, W, None, 0, out_dtype=yt)
+        assert names == [kernel] * 2
+        check_gated_fwd(B, x, W, bias, 3, yt)
+        check_gated_fwd(B, x, W, None, 2, yt, save_z=False)
 
 
 # ---- together ----------------------------------------------------------------------------------------------------------------
