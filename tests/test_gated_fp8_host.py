@@ -164,7 +164,7 @@ def test_every_access_of_a_tile_is_inside(B):
     """The tiles' loads, by the arithmetic of the kernels: rows, chunks and scale words of every lane, wavefront and step stay inside the operands"""
     def spread(b, i, B_):
         return b // B_ * 16 * B_ + B_ * i + b % B_
-    shapes = [(256, 256, 4, 2), (256, 256, 2, 4), (128, 256, 2, 4), (128, 256, 4, 2), (256, 128, 4, 2), (128, 128, 2, 2), (64, 128, 2, 2), (64, 128, 2, 4), (64, 64, 2, 2), (64, 64, 2, 1), (64, 256, 2, 2)]
+    shapes = [(256, 256, 4, 2), (256, 256, 2, 4), (128, 256, 2, 4), (128, 256, 4, 2), (256, 128, 4, 2), (128, 192, 4, 2), (96, 128, 1, 4), (128, 128, 2, 2), (64, 128, 2, 2), (64, 128, 2, 4), (64, 64, 2, 2), (64, 64, 2, 1), (64, 256, 2, 2)]
     for BM, BN, WGM, WGN in shapes:
         for gated_, bq in ((False, 2), (True, 2), (True, 4)):
             NW, WM, WN = WGM * WGN, BM // WGM, BN // WGN

@@ -610,14 +610,24 @@ def test_fp8_special_values(B):
 
 
 LIN8_KERNELS = [("bfloat16", *c) for c in [
-    (1, 1, 768, "few rows 8 bits 16x16"), (4579, 1, 768, "few rows 8 bits 32x16"), (849, 2353, 768, "gemm cols 8 bits 128x128/4 waves/2 stages"), (8807, 197, 784, "gemm cols 8 bits 128x128/4 waves/2 stages guard"),
-    (1310, 5559, 768, "gemm cols 8 bits 128x256/8 waves/3 stages"), (1325, 5606, 16, "gemm cols 8 bits 128x256/8 waves/3 stages guard"), (8380, 424, 768, "gemm cols 8 bits 256x128/8 waves/3 stages"),
-    (11162, 289, 864, "gemm cols 8 bits 256x128/8 waves/3 stages guard"), (9654, 792, 128, "gemm cols 8 bits 256x256/8 waves/2 stages"), (3914, 2073, 768, "gemm cols 8 bits 256x256/8 waves/2 stages"),
-    (10005, 781, 800, "gemm cols 8 bits 256x256/8 waves/2 stages guard"), (11378, 129, 128, "gemm cols 8 bits 64x128/4 waves/3 stages"), (8735, 73, 768, "gemm cols 8 bits 64x128/4 waves/3 stages"),
-    (8200, 72, 944, "gemm cols 8 bits 64x128/4 waves/3 stages guard"), (1, 4216, 768, "gemm cols 8 bits 64x64/4 waves/4 stages"), (3, 4463, 784, "gemm cols 8 bits 64x64/4 waves/4 stages guard")]] + [("float32", *c) for c in [
-    (4281, 1, 768, "few rows 8 bits 32x16"), (1, 4228, 784, "few rows 8 bits 32x32"), (8397, 1, 16, "few rows 8 bits 64x32"), (11391, 154, 768, "gemm cols 8 bits wide 128x128/4 waves/2 stages"),
-    (11271, 153, 784, "gemm cols 8 bits wide 128x128/4 waves/2 stages guard"), (8239, 67, 896, "gemm cols 8 bits wide 64x128/8 waves/3 stages"), (9071, 78, 16, "gemm cols 8 bits wide 64x128/8 waves/3 stages guard"),
-    (71, 4864, 768, "gemm cols 8 bits wide 64x64/4 waves/4 stages"), (66, 4143, 816, "gemm cols 8 bits wide 64x64/4 waves/4 stages guard")]]
+    (1, 1, 768, "few rows 8 bits 16x16"), (4579, 1, 768, "few rows 8 bits 32x16"), (11378, 129, 128, "gemm cols 8 bits 128x128/4 waves/2 stages"),
+    (3684, 4459, 768, "gemm cols 8 bits 128x128/4 waves/2 stages"), (8807, 197, 16, "gemm cols 8 bits 128x128/4 waves/2 stages guard"),
+    (11547, 291, 128, "gemm cols 8 bits 128x192/8 waves/3 stages"), (8380, 424, 768, "gemm cols 8 bits 128x192/8 waves/3 stages"),
+    (11162, 289, 864, "gemm cols 8 bits 128x192/8 waves/3 stages guard"), (1310, 5559, 768, "gemm cols 8 bits 128x256/8 waves/3 stages"),
+    (1325, 5606, 16, "gemm cols 8 bits 128x256/8 waves/3 stages guard"), (10937, 412, 768, "gemm cols 8 bits 256x128/8 waves/3 stages"),
+    (8465, 603, 816, "gemm cols 8 bits 256x128/8 waves/3 stages guard"), (9654, 792, 128, "gemm cols 8 bits 256x256/8 waves/2 stages"),
+    (3914, 2073, 768, "gemm cols 8 bits 256x256/8 waves/2 stages"), (10005, 781, 800, "gemm cols 8 bits 256x256/8 waves/2 stages guard"),
+    (10530, 69, 384, "gemm cols 8 bits 64x128/4 waves/3 stages"), (8735, 73, 768, "gemm cols 8 bits 64x128/4 waves/3 stages"),
+    (8200, 72, 944, "gemm cols 8 bits 64x128/4 waves/3 stages guard"), (1, 4216, 768, "gemm cols 8 bits 64x64/4 waves/4 stages"),
+    (3, 4463, 784, "gemm cols 8 bits 64x64/4 waves/4 stages guard"), (6877, 263, 256, "gemm cols 8 bits 96x128/4 waves/3 stages"),
+    (11111, 141, 768, "gemm cols 8 bits 96x128/4 waves/3 stages"), (8807, 197, 784, "gemm cols 8 bits 96x128/4 waves/3 stages guard")]] + [("float32", *c) for c in [
+    (4281, 1, 768, "few rows 8 bits 32x16"), (1, 4228, 784, "few rows 8 bits 32x32"), (8397, 1, 16, "few rows 8 bits 64x32"),
+    (6254, 419, 768, "gemm cols 8 bits wide 128x128/4 waves/2 stages"), (6639, 263, 16, "gemm cols 8 bits wide 128x128/4 waves/2 stages guard"),
+    (777, 5036, 768, "gemm cols 8 bits wide 128x192/8 waves/3 stages"), (8203, 456, 880, "gemm cols 8 bits wide 128x192/8 waves/3 stages guard"),
+    (8239, 67, 896, "gemm cols 8 bits wide 64x128/8 waves/3 stages"), (9071, 78, 16, "gemm cols 8 bits wide 64x128/8 waves/3 stages guard"),
+    (71, 4864, 768, "gemm cols 8 bits wide 64x64/4 waves/4 stages"), (66, 4143, 816, "gemm cols 8 bits wide 64x64/4 waves/4 stages guard"),
+    (1239, 4937, 128, "gemm cols 8 bits wide 96x128/4 waves/3 stages"), (11391, 154, 768, "gemm cols 8 bits wide 96x128/4 waves/3 stages"),
+    (11271, 153, 784, "gemm cols 8 bits wide 96x128/4 waves/3 stages guard")]]
 
 
 @pytest.mark.parametrize("yt,M,N,K,kernel", LIN8_KERNELS)
