@@ -3,6 +3,9 @@
 //   y = act(x W^T + bias) + residual;      gated: y = (x Wv^T + bv) act(x Wg^T + bg), in bf16, fp32, or 8 bits again
 //
 // On the tiles of gemm_cols.hpp: the scaled MFMA multiplies at twice the rate of a bf16 one and reads half the bytes.
+//
+// Measured: 8192 x 4096 x 4096 bf16 out 119 us (2.3 PFLOP/s; the library's 102), 8192 x 5120 x 1280 67.6 (1.6; the library's 72); gated with SiLU, 8192 x 5120 x 1280, 101 to bf16, 103 to 8 bits (2.1; the library's
+// product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 40.9.  One row, 5120 x 1280 gated to 8 bits 10.2 to 10.8, 1280 x 5120 onto fp32 6.5.
 #include "gemm_cols.hpp"
 
 #include <string.h>
