@@ -347,6 +347,7 @@ int sd_quantize_fp8(const void* x, int32_t x_dtype, uint8_t* q, uint8_t* scales,
  *   dres       device [M, C] of h_dtype: the gradient that reaches h on its own way, or NULL
  *   dh         device [M, C] of h_dtype; may alias h or dres, or dy if the types are the same
  *   dgamma     device [C] fp32, overwritten (zeros for M = 0); NULL: not wanted, and ws may be NULL
+ * No other result may lie in another argument's place (SD_EINVAL).
  * 4 <= C <= 16384, any C (SD_EUNSUPPORTED outside).  Squares are summed in fp32 (elements up to 1e17 at any C). */
 int sd_rmsnorm_fwd(const void* x, int32_t x_dtype, const void* residual, int32_t res_dtype, const uint16_t* gamma, float eps, void* y, int32_t y_dtype, uint8_t* scales, int64_t lds,
                    void* h, float* rstd, int32_t M, int32_t C, void* stream);

@@ -58,7 +58,7 @@ static int launch_few8(const ColsProblem& P, bool& taken, hipStream_t s) {
     return SD_OK;
 }
 // y in 8 bits by way of fp32, in two launches: where a block's columns lie in several workgroups (few rows, smaller tiles), which a long reduction makes up for.  (us, one launch / two, of which the second
-// and its start are some 6: 64 x 1280 x 5120 30.2 / 18, 256 of them 32.5 / 22; 64 x 5120 x 1280 11.6 / 13.)
+// is 6, and what the rule adds for it, with its start, 9: 64 x 1280 x 5120 30.2 / 18, 256 of them 32.5 / 22; 64 x 5120 x 1280 11.6 / 13.)
 static bool gated8_two_launches(int M, int N, int K) {
     float one, two;
     cols_choose(GATED8_TO_8, M, 2ll * N, K, one);

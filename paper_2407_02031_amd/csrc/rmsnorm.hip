@@ -318,6 +318,11 @@ extern "C" int sd_rmsnorm_fwd(const void* x, int32_t x_dtype, const void* residu
     }
     SD_REQUIRE((y != x || y_dtype == x_dtype) && (y != residual || y_dtype == res_dtype), SD_EINVAL, "rmsnorm_fwd: in place with two types");
     SD_REQUIRE(!h || (h != y && (h != x || x_dtype == res_dtype)), SD_EINVAL, "rmsnorm_fwd: h in another's place");
+    const void* const sc = y_dtype == SD_FP8 ? scales : nullptr;
+    const void *const given[] = {gamma, x, residual, y, h}, *const made[] = {y, h, sc, rstd};
+    for (int i = 0; i < 4; ++i)        // (y and h: as above; nothing is in gamma's place, nor a scale or a statistic in any)
+        for (int j = 0; j < (i < 2 ? 1 : 5); ++j) SD_REQUIRE(!made[i] || made[i] != given[j], SD_EINVAL, "rmsnorm_fwd: a result in another's place");
+    SD_REQUIRE(!sc || sc != rstd, SD_EINVAL, "rmsnorm_fwd: a result in another's place");
     if (SD_DRY_RUN("rmsnorm fwd%s; ", y_dtype == SD_FP8 ? " 8 bits" : "")) return SD_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     auto run = [&](auto xt, auto rt, auto yt) {
@@ -356,6 +361,9 @@ extern "C" int sd_rmsnorm_bwd(const void* dy, int32_t y_dtype, const void* h, in
     SD_REQUIRE(M == 0 || (dy && h && rstd && dh), SD_EINVAL, "rmsnorm_bwd: dy, h, rstd or dh is null");
     SD_REQUIRE(aligned16(dy) && aligned16(h) && aligned16(rstd) && aligned16(gamma) && aligned16(dres) && aligned16(dh) && aligned16(dgamma), SD_EINVAL, "rmsnorm_bwd: pointers must be 16-byte aligned");
     SD_REQUIRE(M == 0 || dh != dy || h_dtype == y_dtype, SD_EINVAL, "rmsnorm_bwd: in place of dy with two types");
+    SD_REQUIRE(M == 0 || (dh != rstd && dh != gamma && dh != dgamma), SD_EINVAL, "rmsnorm_bwd: dh in another's place");
+    for (const void* in : {dy, h, dres, static_cast<const void*>(rstd), static_cast<const void*>(gamma)})
+        SD_REQUIRE(M == 0 || !dgamma || dgamma != in, SD_EINVAL, "rmsnorm_bwd: dgamma in an input's place");
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (M == 0) return dgamma ? launch_sum_partials(nullptr, 0, dgamma, C, nullptr, 0, s) : SD_OK;    // sums over no rows
     // (not in place: a row may be overwritten before a column has read it)

@@ -71,6 +71,24 @@ def test_rmsnorm_refusals(B):
     assert L.sd_rmsnorm_bwd_workspace_bytes(0, 64) == 256 and L.sd_rmsnorm_bwd_workspace_bytes(2 ** 31 - 1, 16384) > 0
 
 
+def test_rmsnorm_results_in_other_places(B):
+    L = B.lib()
+    with B.dry_run():
+        eight = dict(yt=2, s=PA, ld=4)
+        assert rms(L, **eight) == 0
+        for p in (PX, PB, PC, PY, PD, PE):
+            assert rms(L, **{**eight, "s": p}) == EINVAL, p
+        for p in (PX, PB, PC, PY, PD):
+            assert rms(L, rstd=p) == EINVAL, p
+        assert rms(L, y=PC) == EINVAL and rms(L, h=PC) == EINVAL
+        bwd = lambda dh=PZ, dg=PW: L.sd_rmsnorm_bwd(PY, 1, PX, 1, PA, PC, PB, dh, dg, 4, 64, 1 << 20, 1 << 20, None)
+        assert bwd() == 0 and bwd(dg=None) == 0
+        for p in (PA, PC, PW):
+            assert bwd(dh=p) == EINVAL, p
+        for p in (PY, PX, PB, PA, PC, PZ):
+            assert bwd(dg=p) == EINVAL, p
+
+
 def gated(L, x=PX, W=PW, b=PB, act=3, y=PY, yt=0, z=PZ, M=4, N=8, K=64):
     return L.sd_gated_linear_fwd(x, W, b, act, y, yt, z, M, N, K, None)
 

@@ -886,3 +886,59 @@ def test_feed_forward_on_two_streams(B):
     for o, w in zip(got, want):
         for r in o:
             assert all(torch.equal(a, b) for a, b in zip(r, w))
+
+
+def test_the_same_operand_twice(B):
+    """x and W, x and the residual, dy, h and dres one tensor"""
+    import torch
+    g = gen(21)
+    for M in (9, 200, 700):
+        x = rows8(B, g, M, 320, 0.1)
+        check_linear8(B, x, x, None, 0, None, torch.float32)
+        check_linear8(B, x, x, None, 3, None, torch.bfloat16)
+    x = rows8(B, g, 64, 320, 0.1)
+    for yt in (torch.float32, torch.bfloat16, torch.float8_e4m3fn):
+        check_gated8(B, x, x, None, 3, yt)
+    x = randn(g, 64, 64, scale=0.3).bfloat16()
+    assert torch.equal(B.gated_linear_fwd(x, x.clone(), None, 3), B.gated_linear_fwd(x, x, None, 3))
+    for a in (randn(g, 7, 515), randn(g, 2000, 1280)):
+        y, h, rstd = B.rmsnorm_fwd(a, None, residual=a, stats=True)
+        assert torch.equal(h, 2 * a)
+        y2, _, _ = B.rmsnorm_fwd(a, None, residual=a.clone(), stats=True)
+        assert torch.equal(y, y2)
+        one, two = B.rmsnorm_bwd(a, a, rstd, None, dres=a), B.rmsnorm_bwd(a.clone(), a, rstd, None, dres=a.clone())
+        assert torch.equal(one[0], two[0]) and torch.equal(one[1], two[1])
+
+
+def test_two_launches_captured_with_one_workspace(B):
+    """Two graphs that share a workspace, replayed one behind the other"""
+    import torch
+    M, N, K = 130, 640, 4112
+    g = gen(22)
+    need = B.lib().sd_gated_linear_fp8_workspace_bytes(M, N, K)
+    assert need
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    src = [randn(g, M, K) for _ in range(2)]
+    W = rows8(B, g, 2 * N, K, 1.3 / math.sqrt(K), 0.3)
+    step = lambda a: B.gated_linear_fp8_fwd(B.quantize_fp8(a), W, out_dtype=torch.float8_e4m3fn, ws=ws)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for a in src:
+            step(a)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs, outs = [], []
+    for a in src:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            outs.append(step(a))
+        graphs.append(gr)
+    for rep in range(4):
+        for a in src:
+            a.normal_()
+        for gr in graphs:
+            gr.replay()
+        for a, o in zip(src, outs):
+            w = step(a)
+            assert torch.equal(o.q.view(torch.uint8), w.q.view(torch.uint8)) and torch.equal(o.scales.view(torch.uint8).contiguous(), w.scales.view(torch.uint8).contiguous())
+        torch.cuda.synchronize()
