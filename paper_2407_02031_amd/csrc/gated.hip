@@ -11,9 +11,9 @@
 
 namespace sd {
 
-// (gemm_cols.hpp's rule; it takes 50 launches 0.7 % longer in the mean than the fastest of these)
+// (gemm_cols.hpp's rule; it takes 48 launches 1 % longer in the mean than the fastest of these)
 static const ColsTile GATED16[] = {{256, 256, 256, 0.f, 5.6f, 1.518f, 5.6f, 1.518f}, {128, 256, 256, 0.f, 5.1f, 0.816f, 5.1f, 0.816f}, {256, 128, 256, 0.f, 5.4f, 0.721f, 5.4f, 0.721f},
-                                   {128, 128, 512, 0.f, 8.3f, 1.042f, 2.8f, 0.889f}, {64, 128, 512, 0.1f, 4.1f, 0.719f, 2.6f, 0.451f}, {64, 64, 512, 0.f, 3.5f, 0.523f, 3.3f, 0.31f}};
+                                   {128, 128, 256, 0.f, 4.6f, 0.527f, 4.6f, 0.527f}, {64, 128, 512, 0.8f, 3.7f, 0.71f, 2.5f, 0.408f}, {64, 64, 512, 1.5f, 2.4f, 0.447f, 1.8f, 0.244f}};
 
 }  // namespace sd
 
@@ -38,7 +38,7 @@ extern "C" int sd_gated_linear_fwd(const uint16_t* x, const uint16_t* W, const u
     P.y_f32 = y_dtype == SD_F32;
     P.M = M; P.N = N; P.Kb = 2 * K;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    // Few rows: straight from the weights where that is one workgroup a CU (us, these kernels / tiles: 16 x 5120 x 1280 10.1 / 10.7, 64 x 1280 x 5120 22.6 / 29.8, 128 x 1280 x 1280 9.7 / 8.8)
+    // Few rows: straight from the weights where that is one workgroup a CU (us, these kernels / tiles: 16 x 5120 x 1280 10.0 / 10.0, 64 x 1280 x 5120 22.6 / 29.5, 32 x 4096 x 4096 20.1 / 22.5, but 128 x 1280 x 1280 9.7 / 7.5)
     const int64_t r16 = (M + 15) / 16, r32 = (M + 31) / 32, c16 = (N + 15) / 16, c32 = (N + 31) / 32;
     if (r16 * c16 <= 256) return launch_few<false, true, 1, 1, 3>(P, s);
     if (r32 * c16 <= 256) return launch_few<false, true, 2, 1, 3>(P, s);
@@ -48,8 +48,8 @@ extern "C" int sd_gated_linear_fwd(const uint16_t* x, const uint16_t* W, const u
     case 0: return launch_cols<COLS_BF16, 256, 256, 2, 4, 2, true, false>(P, s);
     case 1: return launch_cols<COLS_BF16, 128, 256, 2, 4, 3, true, false>(P, s);
     case 2: return launch_cols<COLS_BF16, 256, 128, 4, 2, 3, true, false>(P, s);
-    case 3: return launch_cols<COLS_BF16, 128, 128, 2, 2, 2, true, false>(P, s);
+    case 3: return launch_cols<COLS_BF16, 128, 128, 2, 2, 3, true, false, 2>(P, s);
     case 4: return launch_cols<COLS_BF16, 64, 128, 2, 2, 3, true, false>(P, s);
-    default: return launch_cols<COLS_BF16, 64, 64, 2, 1, 4, true, false>(P, s);
+    default: return launch_cols<COLS_BF16, 64, 64, 2, 1, 4, true, false, 2>(P, s);
     }
 }

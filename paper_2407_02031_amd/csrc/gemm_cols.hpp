@@ -9,6 +9,9 @@
 //     each block's result, has 8 (16) neighbouring columns of one row of D in all.  Epilogues work in registers and store 16 bytes a lane, without a detour through LDS.  The
 //     rows are sorted where they are loaded: which row of memory goes into which row of LDS costs nothing.  The same for P, four blocks to 64 rows, whose four scales are then one word.
 //   - Gated: half of a wavefront's Q blocks are rows of the value, half rows of the gate, of the same columns.
+//   - KS = 2: WGM x WGN wavefronts work on the first half of each step, as many on the second, and their sums meet in LDS.  A wavefront alone on its SIMD issues a vector instruction every
+//     3.1 to 4 ns, two together one every 2: so in tiles that would have four wavefronts on a CU, mostly those of widened operands (1976 x 1280 x 5120 onto fp32 41 -> 35 us with 96 x 128) and of
+//     long reductions (gated in bf16, 512 x 640 x 2560 14.4 -> 12.9 with 64 x 64, 1024 x 1280 x 5120 65 -> 53 with 128 x 128).
 #pragma once
 #include "gemm_dma.hpp"
 #include "fp8.hpp"
@@ -54,23 +57,22 @@ __device__ __forceinline__ void dma4(const void* gptr, uint32_t lds_base) {
 // operands' bytes all that counts, they are widened to bf16, exactly and with their scales, and multiplied as those.
 enum ColsMode { COLS_BF16, COLS_FP8, COLS_FP8_WIDE };
 
-// 16 e4m3 elements times 2^(s - 127), s a byte, which is what the conversion looks at of an fp32 scale
-__device__ __forceinline__ void widen16(const u32x4& w, uint32_t s, bf16x8 (&o)[2]) {
+// Eight e4m3 elements times 2^(s - 127), s a byte, which is what the conversion looks at of an fp32 scale
+__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi, uint32_t s) {
     const float scale = __uint_as_float(s << 23);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        union { bf16x8 v; bf16x2 p[4]; } u;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            u.p[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i * 2 + j], scale, false);
-            u.p[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i * 2 + j], scale, true);
-        }
-        o[i] = u.v;
-    }
+    union { bf16x8 v; bf16x2 p[4]; } u;
+    u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+    u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+    u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return u.v;
 }
+// ... eight of a lane's 32 of a step
+template <int H>
+__device__ __forceinline__ bf16x8 widen8(const u32x4 (&w)[H], int i, uint32_t s) { return widen8(w[i / 2][i % 2 * 2], w[i / 2][i % 2 * 2 + 1], s); }
 __device__ __forceinline__ void widen32(const u32x4 (&w)[2], uint32_t s, bf16x8 (&o)[4]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) widen16(w[h], s, reinterpret_cast<bf16x8(&)[2]>(o[2 * h]));
+    for (int i = 0; i < 4; ++i) o[i] = widen8(w, i, s);
 }
 __device__ __forceinline__ f32x4 mfma_bf16(bf16x8 q, bf16x8 p, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, p, c, 0, 0, 0); }
 __device__ __forceinline__ i32x8 words8(const u32x4 (&w)[2]) {
@@ -90,12 +92,13 @@ __device__ __forceinline__ void each(F f) {
     }
 }
 
-template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8, bool GUARD>
+template <int MODE, int BM, int BN, int WGM, int WGN, int KS, int STAGES, bool GATED, bool OUT8, bool GUARD>
 __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, u32x4* const lds) {
     constexpr bool FP8 = MODE != COLS_BF16, WIDE = MODE == COLS_FP8_WIDE;
-    constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NI = WN / 16;
-    constexpr int LPT = (BM + BN) / 8 / NW;            // loads of a wavefront and step
-    constexpr int JP = BM / 8 / NW;                    // ... of them of P
+    constexpr int NW = WGM * WGN * KS, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NI = WN / 16;
+    constexpr int ROWS8 = (BM + BN) / 8, LPT = (ROWS8 + NW - 1) / NW;      // loads of a step, and of a wavefront
+    constexpr bool EVEN = BM / 8 % NW == 0 && BN / 8 % NW == 0;            // (where not, some are made twice, and a wavefront's are of P or of Q as its number says)
+    constexpr int HC = 2 / KS;                         // chunks of a row's step that a lane works on
     constexpr int SW = cols_scale_words<FP8, BM, BN>();
     constexpr int STAGE = (BM + BN) * 8 + SW / 4;      // 16-byte chunks
     constexpr int PIECES = SW / 64;
@@ -104,7 +107,8 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     constexpr int NV = GATED ? NI / 2 : NI;            // blocks of columns of the result
     constexpr int BP = MI % 4 == 0 ? 4 : 2, BQ = OUT8 ? 4 : 2;
     constexpr int BN_OUT = GATED ? BN / 2 : BN, WN_OUT = GATED ? WN / 2 : WN;
-    static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0 && MI % BP == 0 && NV % BQ == 0 && NI % RING == 0 && STAGES >= 2 && STAGES <= 4, "tile");
+    static_assert(MI % BP == 0 && NV % BQ == 0 && NI % RING == 0 && (!WIDE || NI % 2 == 0) && STAGES >= 2 && STAGES <= 4, "tile");
+    static_assert(KS == 1 || (KS == 2 && MODE != COLS_FP8 && MI % 2 == 0 && !OUT8 && WGM * WGN * MI * NI * 64 <= STAGES * STAGE), "halves");
     static_assert(!FP8 || PIECES <= NW, "scales");
     static_assert(NW * 64 >= BN, "bias");
     static_assert(!OUT8 || (GATED && FP8 && BN_OUT == FP8_BLOCK), "a tile's columns are one block of y");
@@ -120,7 +124,8 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, quad = lane >> 4;
-    const int wm = (wave / WGN) * WM, wn = (wave % WGN) * WN, wn_out = (wave % WGN) * WN_OUT;
+    const int half = KS == 2 ? wave / (WGM * WGN) : 0;
+    const int wm = (KS == 2 ? wave % (WGM * WGN) : wave) / WGN * WM, wn = (wave % WGN) * WN, wn_out = (wave % WGN) * WN_OUT;
 
     // ---- loads: load j of a wavefront fills rows 8 (j NW + wave) .. + 8 of a stage, lane l the chunk at position l % 8 of row l / 8.  They lie in one block, so what
     // differs between value and gate is the wavefront's base.
@@ -128,11 +133,12 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     const uint8_t* base[LPT];
     const uint8_t* const pb = P.p + (int64_t)m0 * Kb;
     const uint8_t* const qb = P.q + (int64_t)n0 * Kb;
-    auto chunk = [&](int j) { return swz<8>((j * NW + wave) * 8 + (lane >> 3), lane & 7) * 16; };
+    auto eight = [&](int j) { return EVEN ? j * NW + wave : min(j * NW + wave, ROWS8 - 1); };
+    auto chunk = [&](int j) { return swz<8>(eight(j) * 8 + (lane >> 3), lane & 7) * 16; };
 #pragma unroll
     for (int j = 0; j < LPT; ++j) {
-        const int first = (j * NW + wave) * 8, row = first + (lane >> 3);
-        if (j < JP) {
+        const int first = eight(j) * 8, row = first + (lane >> 3);
+        if (EVEN ? j < BM / 8 / NW : first < BM) {
             const int w = first / WM, b = first % WM / 16;
             const int r = min(m0 + w * WM + spread<BP>(b, row % 16), M - 1) - m0;
             base[j] = pb;
@@ -165,11 +171,10 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         }
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
-    const uint32_t wave_base = lds_base + (uint32_t)wave * 1024;
     const uint32_t scale_base = lds_base + (uint32_t)((BM + BN) * 128 + (PIECES ? wave % (PIECES ? PIECES : 1) : 0) * 256);
     // load j of step t; steps are loaded in order, each once
     auto load = [&](int j, int t, int stg, auto partial) {
-        const uint32_t to = wave_base + (uint32_t)stg * (STAGE * 16) + (uint32_t)j * (NW * 1024);
+        const uint32_t to = lds_base + (uint32_t)stg * (STAGE * 16) + (uint32_t)eight(j) * 1024;
         const int kb = t * 128;
         if (decltype(partial)::value && kb + 128 > Kb) {
             const uint8_t* const src = base[j] + kb + off[j];
@@ -189,18 +194,19 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // ---- operands in registers: P's blocks, and a ring of Q's.  A lane has chunks quad and quad + 4 of a row, of either operand: which k an MFMA's lane has does not matter, if it is the same ones.
-    u32x4 pr[MI][2], qr[RING][2];
+    // ---- operands in registers: P's blocks, and a ring of Q's.  A lane has chunks quad and quad + 4 of a row, of halves the one or the other, of either operand: which k an MFMA's lane has does not matter, if it is the same ones.
+    u32x4 pr[MI][HC], qr[RING][HC];
     uint32_t ps[FP8 ? MI / BP : 1], qs[FP8 ? NI / BQ : 1];     // scales of the step being multiplied
     const int lsw = swz<8>(l16, 0);
     const u32x4* const frag = lds + l16 * 8;
+    auto part = [&](int h) { return ((KS == 2 ? half : h) * 4 + quad) ^ lsw; };
     auto fetch_p = [&](int st, int mi) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) pr[mi][h] = frag[st * STAGE + (wm + mi * 16) * 8 + ((h * 4 + quad) ^ lsw)];
+        for (int h = 0; h < HC; ++h) pr[mi][h] = frag[st * STAGE + (wm + mi * 16) * 8 + part(h)];
     };
     auto fetch_q = [&](int st, int ni) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) qr[ni % RING][h] = frag[st * STAGE + (BM + wn + ni * 16) * 8 + ((h * 4 + quad) ^ lsw)];
+        for (int h = 0; h < HC; ++h) qr[ni % RING][h] = frag[st * STAGE + (BM + wn + ni * 16) * 8 + part(h)];
     };
     auto fetch_scales = [&](int st, auto& p, auto& q) {
         if constexpr (FP8) {
@@ -218,7 +224,12 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
             }
         }
     };
-    bf16x8 pw[WIDE ? MI : 1][4], qw[4];
+    uint32_t ps_next[FP8 ? MI / BP : 1], qs_next[FP8 ? NI / BQ : 1];
+    // Widened: all of P's blocks, and Q's block of this slot and the next
+    bf16x8 pw[WIDE ? MI : 1][2 * HC], qw[2][2 * HC];
+    auto scale_of = [](auto& words, int i, auto per) { return (words[i / decltype(per)::value] >> (i % decltype(per)::value * 8)) & 255u; };
+    using PerP = std::integral_constant<int, BP>;
+    using PerQ = std::integral_constant<int, BQ>;
     // Slot s: Q block s by all of P's, then `load`'s share of another step's loads, dealt over the slots from the edge on.  (No branches in here: the compiler would move the MFMAs past them, all
     // to the end of the step.)
     auto slot = [&](auto sc, auto refill_qc, auto refill_pc, int st_q, auto load) {
@@ -226,18 +237,27 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         constexpr bool refill_q = decltype(refill_qc)::value, refill_p = decltype(refill_pc)::value;
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (WIDE) {
-            if constexpr (s == 0) each<MI>([&](auto mi) { widen32(pr[mi], (ps[mi / BP] >> (mi % BP * 8)) & 255u, pw[mi]); });
-            widen32(qr[s % RING], (qs[s / BQ] >> (s % BQ * 8)) & 255u, qw);
-        }
-        if constexpr (WIDE) {
-            // (P's raw blocks are done with since they were widened)
+            // What the slot multiplies was widened in the one before; in the last, P's blocks of the next step are, behind the products.  Raw blocks are free a slot earlier than they would be,
+            // and the compiler may order the slot's conversions and products (put between them one by one they took 15 % longer).
+            constexpr bool last = s == NI - 1;
             if constexpr (refill_p)
 #pragma unroll
                 for (int mi = 0; mi < MI; ++mi) fetch_p(st_q, mi);
+            if constexpr (refill_q) fetch_q(st_q, (s + RING) % NI);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2 * HC; ++i)
+                if constexpr (!last) qw[(s + 1) % 2][i] = widen8(qr[(s + 1) % RING], i, scale_of(qs, s + 1, PerQ()));
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi) acc[mi][s] = mfma_bf16(qw[i], pw[mi][i], acc[mi][s]);
+            for (int i = 0; i < 2 * HC; ++i)
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) acc[mi][s] = mfma_bf16(qw[s % 2][i], pw[mi][i], acc[mi][s]);
+            if constexpr (last && refill_q)
+#pragma unroll
+                for (int i = 0; i < 2 * HC; ++i) {
+                    qw[0][i] = widen8(qr[0], i, scale_of(qs_next, 0, PerQ()));
+#pragma unroll
+                    for (int mi = 0; mi < MI; ++mi) pw[mi][i] = widen8(pr[mi], i, scale_of(ps_next, mi, PerP()));
+                }
         } else {
             each<MI>([&](auto mic) {
                 constexpr int mi = decltype(mic)::value;
@@ -246,7 +266,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
                     c = mfma_fp8<s % BQ, mi % BP>(qr[s % RING], pr[mi], c, qs[s / BQ], ps[mi / BP]);
                 } else {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) c = mfma_bf16(__builtin_bit_cast(bf16x8, qr[s % RING][h]), __builtin_bit_cast(bf16x8, pr[mi][h]), c);
+                    for (int h = 0; h < HC; ++h) c = mfma_bf16(__builtin_bit_cast(bf16x8, qr[s % RING][h]), __builtin_bit_cast(bf16x8, pr[mi][h]), c);
                 }
                 if constexpr (refill_p) {
                     __builtin_amdgcn_sched_barrier(0);
@@ -256,14 +276,13 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
             });
         }
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (refill_q) fetch_q(st_q, (s + RING) % NI);
+        if constexpr (refill_q && !WIDE) fetch_q(st_q, (s + RING) % NI);
         constexpr int i = (s + RING) % NI, DEAL = STAGES > 2 ? NI : RING;
 #pragma unroll
         for (int j = i * LPT / DEAL; j < (i + 1) * LPT / DEAL && i < DEAL; ++j) load(j);
     };
     // A step: its first NI - RING slots (`head`), then, when the next step has landed everywhere and this one's stage is free (what is left of it is in registers), the last RING
     // (`edge`), which bring in the next step's first blocks and, P's as they are done with, all of P.
-    uint32_t ps_next[FP8 ? MI / BP : 1], qs_next[FP8 ? NI / BQ : 1];
     auto head = [&](int st, auto load) {
         each<NI - RING>([&](auto s) { slot(s, std::true_type(), std::false_type(), st, load); });
     };
@@ -300,6 +319,14 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     for (int mi = 0; mi < MI; ++mi) fetch_p(0, mi);
 #pragma unroll
     for (int s = 0; s < RING; ++s) fetch_q(0, s);
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int i = 0; i < 2 * HC; ++i) {
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) pw[mi][i] = widen8(pr[mi], i, scale_of(ps, mi, PerP()));
+            qw[0][i] = widen8(qr[0], i, scale_of(qs, 0, PerQ()));
+        }
+    }
     head(0, none);
     int st = 0, t = 0;
     const int nfull = GUARD ? Kb / 128 : nk;     // whole steps
@@ -328,10 +355,21 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     }
     each<RING>([&](auto i) { slot(std::integral_constant<int, NI - RING + decltype(i)::value>(), std::false_type(), std::false_type(), 0, none); });
 
+    // the halves' sums, of which each half finishes one half of the rows' blocks
+    constexpr int ME = MI / KS;
+    if constexpr (KS == 2) {
+        __syncthreads();
+        f32x4* const swap = reinterpret_cast<f32x4*>(lds) + (wave % (WGM * WGN)) * (MI * NI * 64) + lane;
+#pragma unroll
+        for (int i = 0; i < ME * NI; ++i) swap[((1 - half) * ME * NI + i) * 64] = half ? acc[i / NI][i % NI] : acc[ME + i / NI][i % NI];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ME * NI; ++i) acc[i / NI][i % NI] = (half ? acc[ME + i / NI][i % NI] : acc[i / NI][i % NI]) + swap[(half * ME * NI + i) * 64];
+    }
     // ---- epilogue.  A lane has rows spread<BP>(mi, l16) of its wavefront's, and of each group of 16 BQ columns the 4 BQ from 4 BQ quad on.
     constexpr int W4 = BQ, NG = NV / BQ;               // pieces of four columns of a lane in a group; groups
     auto column = [&](int g) { return n0 + wn_out + (g * 4 + quad) * 4 * W4; };
-    auto row_of = [&](int mi) { return wm + spread<BP>(mi, l16); };
+    auto row_of = [&](int mi) { return wm + (KS == 2 ? spread<BP>(half * ME + mi, l16) : spread<BP>(mi, l16)); };
     // element x of piece c of group g, of the blocks from `first` on
     auto element = [&](int mi, int first, int g, int c, int x) -> float& { return reinterpret_cast<float(&)[4]>(acc[mi][first + g * BQ + (4 * c + x) % BQ])[(4 * c + x) / BQ]; };
     auto piece = [&](int mi, int first, int g, int c) {
@@ -386,7 +424,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
             if (GATED) bg[c] = *reinterpret_cast<const f32x4*>(bias + BN_OUT + col - n0 + 4 * c);
         }
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
+        for (int mi = 0; mi < ME; ++mi) {
             const int m = m0 + row_of(mi);
             f32x4 v[W4], g[W4];
 #pragma unroll
@@ -469,13 +507,13 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     }
 }
 
-template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8, bool GUARD>
-__global__ __launch_bounds__(64 * WGM * WGN, (cols_lds_chunks<MODE != COLS_BF16, BM, BN, WGN, STAGES, OUT8>() * 16 <= 80 * 1024 ? 2 : 1)) void cols_kernel(const ColsProblem P) {
+template <int MODE, int BM, int BN, int WGM, int WGN, int KS, int STAGES, bool GATED, bool OUT8, bool GUARD>
+__global__ __launch_bounds__(64 * WGM * WGN * KS, (cols_lds_chunks<MODE != COLS_BF16, BM, BN, WGN, STAGES, OUT8>() * 16 <= 80 * 1024 ? 2 : 1)) void cols_kernel(const ColsProblem P) {
     __shared__ u32x4 lds[cols_lds_chunks<MODE != COLS_BF16, BM, BN, WGN, STAGES, OUT8>()];
     const int total = P.tiles_m * P.tiles_n, per = (total + 7) >> 3;
     const int tile = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
     if (tile >= total) return;
-    cols_tile<MODE, BM, BN, WGM, WGN, STAGES, GATED, OUT8, GUARD>(P, tile, lds);
+    cols_tile<MODE, BM, BN, WGM, WGN, KS, STAGES, GATED, OUT8, GUARD>(P, tile, lds);
 }
 
 // Few rows (one token's, a guidance pair's, a short text's).  A workgroup has 16 MB rows and 16 NB columns (of a gated product of value and gate each); its eight wavefronts take every eighth
@@ -652,17 +690,17 @@ inline int cols_choose(const ColsTile (&tiles)[TILES], int64_t M, int64_t column
     }
     return best;
 }
-template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8>
+template <int MODE, int BM, int BN, int WGM, int WGN, int STAGES, bool GATED, bool OUT8, int KS = 1>
 static int launch_cols(ColsProblem& P, hipStream_t stream) {
     constexpr int BN_OUT = GATED ? BN / 2 : BN;
     P.tiles_m = (P.M + BM - 1) / BM;
     P.tiles_n = (P.N + BN_OUT - 1) / BN_OUT;
     const int64_t tiles = (int64_t)P.tiles_m * P.tiles_n;
     const bool guard = P.Kb % 128 != 0;
-    if (SD_DRY_RUN("gemm cols%s%s%s %dx%d/%d waves/%d stages%s; ", MODE == COLS_BF16 ? "" : MODE == COLS_FP8 ? " 8 bits" : " 8 bits wide", GATED ? " gated" : "", OUT8 ? " to 8 bits" : "", BM, BN, WGM * WGN, STAGES, guard ? " guard" : "")) return SD_OK;
-    const dim3 grid((unsigned)((tiles + 7) & ~7ll)), block(64 * WGM * WGN);
-    if (guard) hipLaunchKernelGGL((cols_kernel<MODE, BM, BN, WGM, WGN, STAGES, GATED, OUT8, true>), grid, block, 0, stream, P);
-    else hipLaunchKernelGGL((cols_kernel<MODE, BM, BN, WGM, WGN, STAGES, GATED, OUT8, false>), grid, block, 0, stream, P);
+    if (SD_DRY_RUN("gemm cols%s%s%s %dx%d/%d waves/%d stages%s; ", MODE == COLS_BF16 ? "" : MODE == COLS_FP8 ? " 8 bits" : " 8 bits wide", GATED ? " gated" : "", OUT8 ? " to 8 bits" : "", BM, BN, WGM * WGN * KS, STAGES, guard ? " guard" : "")) return SD_OK;
+    const dim3 grid((unsigned)((tiles + 7) & ~7ll)), block(64 * WGM * WGN * KS);
+    if (guard) hipLaunchKernelGGL((cols_kernel<MODE, BM, BN, WGM, WGN, KS, STAGES, GATED, OUT8, true>), grid, block, 0, stream, P);
+    else hipLaunchKernelGGL((cols_kernel<MODE, BM, BN, WGM, WGN, KS, STAGES, GATED, OUT8, false>), grid, block, 0, stream, P);
     SD_HIP_CHECK(hipGetLastError());
     return SD_OK;
 }

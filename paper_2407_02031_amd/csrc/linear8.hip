@@ -5,7 +5,7 @@
 // On the tiles of gemm_cols.hpp: the scaled MFMA multiplies at twice the rate of a bf16 one and reads half the bytes.
 //
 // Measured: 8192 x 4096 x 4096 bf16 out 119 us (2.3 PFLOP/s; the library's 102), 8192 x 5120 x 1280 67.6 (1.6; the library's 72); gated with SiLU, 8192 x 5120 x 1280, 101 to bf16, 103 to 8 bits (2.1; the library's
-// product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 40.9.  One row, 5120 x 1280 gated to 8 bits 10.2 to 10.8, 1280 x 5120 onto fp32 6.5.
+// product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 32.2.  One row, 5120 x 1280 gated to 8 bits 10.2 to 10.8, 1280 x 5120 onto fp32 6.5.
 #include "gemm_cols.hpp"
 
 #include <string.h>
@@ -32,19 +32,20 @@ static ColsProblem problem8(const uint8_t* x, const uint8_t* x_scales, int64_t x
     return P;
 }
 
-// Tiles (gemm_cols.hpp's rule).  It takes 50 to 70 launches each 0.6 % (plain), 0.4 % (gated), 0 % (to 8 bits) and 1 % (y in fp32) longer in the mean than the fastest of these tiles.
+// Tiles (gemm_cols.hpp's rule).  It takes 50 to 72 launches each 0.6 % (plain), 0.4 % (gated), 0 % (to 8 bits), 1.1 % (y in fp32) and 0.6 % (gated, y in fp32) longer in the mean than the fastest of these tiles.
 static const ColsTile PLAIN8[] = {{256, 256, 256, 0.f, 7.1f, 1.134f, 7.1f, 1.134f}, {128, 256, 256, 0.f, 5.7f, 0.62f, 5.7f, 0.62f}, {256, 128, 256, 0.f, 5.5f, 0.618f, 5.5f, 0.618f},
                                   {128, 192, 256, 0.f, 5.2f, 0.625f, 5.2f, 0.625f}, {96, 128, 256, 1.f, 3.f, 0.522f, 3.f, 0.522f}, {128, 128, 512, 0.f, 6.6f, 0.995f, 3.7f, 0.724f},
                                   {64, 128, 512, 0.4f, 3.4f, 0.702f, 3.2f, 0.324f}, {64, 64, 512, 1.2f, 2.1f, 0.436f, 2.2f, 0.193f}};
 static const ColsTile GATED8[] = {{256, 256, 256, 0.f, 5.7f, 1.4f, 5.7f, 1.4f}, {128, 256, 256, 0.f, 4.9f, 0.744f, 4.9f, 0.744f}, {256, 128, 256, 0.f, 5.f, 0.675f, 5.f, 0.675f},
                                   {128, 128, 512, 0.f, 4.7f, 0.994f, 3.7f, 0.762f}, {64, 128, 512, 1.4f, 2.7f, 0.655f, 2.1f, 0.381f}, {64, 64, 512, 0.f, 2.8f, 0.528f, 3.5f, 0.306f}};
 static const ColsTile GATED8_TO_8[] = {{256, 256, 256, 0.f, 6.8f, 1.32f, 6.8f, 1.32f}, {128, 256, 256, 0.f, 5.4f, 0.735f, 5.4f, 0.735f}, {64, 256, 256, 0.7f, 4.2f, 0.626f, 4.2f, 0.626f}};
-static const ColsTile WIDE8[] = {{128, 192, 256, 0.f, 13.2f, 1.112f, 13.2f, 1.112f}, {96, 128, 256, 1.f, 8.3f, 0.819f, 8.3f, 0.819f}, {128, 128, 512, 0.f, 18.3f, 1.352f, 8.4f, 1.025f},
-                                 {64, 128, 512, 1.7f, 8.6f, 0.982f, 3.5f, 0.595f}, {64, 64, 512, 1.2f, 5.2f, 0.594f, 3.4f, 0.401f}};
-static const ColsTile GATED_WIDE8[] = {{128, 128, 512, 0.3f, 16.7f, 1.407f, 7.5f, 1.071f}, {64, 128, 512, 1.9f, 8.7f, 0.94f, 3.1f, 0.601f}, {64, 64, 512, 1.1f, 5.1f, 0.566f, 3.3f, 0.406f}};
+static const ColsTile WIDE8[] = {{128, 256, 256, 0.f, 13.3f, 1.243f, 13.3f, 1.243f}, {128, 192, 256, 0.f, 11.1f, 1.072f, 11.1f, 1.072f}, {96, 128, 256, 0.f, 7.9f, 0.615f, 7.9f, 0.615f},
+                                 {64, 128, 512, 2.1f, 8.2f, 0.918f, 3.6f, 0.491f}, {64, 64, 512, 1.9f, 4.5f, 0.617f, 2.7f, 0.363f}};
+static const ColsTile GATED_WIDE8[] = {{128, 128, 512, 2.f, 5.3f, 1.445f, 2.6f, 1.027f}, {128, 128, 256, 0.3f, 5.1f, 0.722f, 5.1f, 0.722f}, {64, 128, 512, 2.3f, 3.4f, 0.875f, 2.2f, 0.503f},
+                                       {64, 64, 512, 2.5f, 2.7f, 0.514f, 1.6f, 0.323f}};
 
 // Few rows: straight from the weights where that is one workgroup a CU.  With y in fp32, whose tiles are slower, with more rows and columns a workgroup too.  (us, these kernels / tiles:
-// 32 x 1280 x 5120 7.7 / 10.6, 32 x 1280 x 1280 4.1 / 5.1, 64 x 1280 x 5120 10.3 / 11.1, but 128 of them 12.9 / 11.2; y in fp32 256 x 1280 x 1280 7.3 / 8.4, 128 of them 5.9 / 8.3.)
+// 32 x 1280 x 5120 7.7 / 10.6, 32 x 1280 x 1280 4.1 / 5.1, 64 x 1280 x 5120 10.3 / 11.1, but 128 of them 12.9 / 11.2; y in fp32 256 x 1280 x 1280 7.5 / 8.2, 128 of them 5.8 / 8.0; gated 64 x 1280 x 5120 12.8 / 17.1.)
 template <bool GATED>
 static int launch_few8(const ColsProblem& P, bool& taken, hipStream_t s) {
     const int64_t r16 = (P.M + 15) / 16, r32 = (P.M + 31) / 32, c16 = (P.N + 15) / 16, c32 = (P.N + 31) / 32;
@@ -71,8 +72,9 @@ static int launch_gated8(ColsProblem& P, bool wide, hipStream_t s) {
     if (wide)
         switch (cols_choose(GATED_WIDE8, P.M, 2ll * P.N, P.Kb, us)) {
         case 0: return launch_cols<COLS_FP8_WIDE, 128, 128, 2, 2, 2, true, false>(P, s);
-        case 1: return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 2, 3, true, false>(P, s);
-        default: return launch_cols<COLS_FP8_WIDE, 64, 64, 2, 1, 4, true, false>(P, s);
+        case 1: return launch_cols<COLS_FP8_WIDE, 128, 128, 2, 2, 3, true, false, 2>(P, s);
+        case 2: return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 2, 3, true, false>(P, s);
+        default: return launch_cols<COLS_FP8_WIDE, 64, 64, 2, 1, 4, true, false, 2>(P, s);
         }
     switch (cols_choose(GATED8, P.M, 2ll * P.N, P.Kb, us)) {
     case 0: return launch_cols<COLS_FP8, 256, 256, 2, 4, 2, true, false>(P, s);
@@ -107,11 +109,11 @@ extern "C" int sd_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int6
     float us;
     if (P.y_f32)
         switch (cols_choose(WIDE8, M, N, K, us)) {
-        case 0: return launch_cols<COLS_FP8_WIDE, 128, 192, 4, 2, 3, false, false>(P, s);
-        case 1: return launch_cols<COLS_FP8_WIDE, 96, 128, 1, 4, 3, false, false>(P, s);
-        case 2: return launch_cols<COLS_FP8_WIDE, 128, 128, 2, 2, 2, false, false>(P, s);
-        case 3: return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 4, 3, false, false>(P, s);
-        default: return launch_cols<COLS_FP8_WIDE, 64, 64, 2, 2, 4, false, false>(P, s);
+        case 0: return launch_cols<COLS_FP8_WIDE, 128, 256, 2, 4, 3, false, false>(P, s);
+        case 1: return launch_cols<COLS_FP8_WIDE, 128, 192, 4, 2, 3, false, false>(P, s);
+        case 2: return launch_cols<COLS_FP8_WIDE, 96, 128, 1, 4, 3, false, false, 2>(P, s);
+        case 3: return launch_cols<COLS_FP8_WIDE, 64, 128, 2, 2, 3, false, false, 2>(P, s);
+        default: return launch_cols<COLS_FP8_WIDE, 64, 64, 2, 2, 4, false, false, 2>(P, s);
         }
     switch (cols_choose(PLAIN8, M, N, K, us)) {
     case 0: return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, false, false>(P, s);

@@ -218,6 +218,21 @@ def test_every_access_of_a_tile_is_inside(B):
                         assert at % 4 == 0 and 0 <= at <= total - 1
 
 
+def test_halved_steps(B):
+    """Tiles whose wavefronts take half of each step: every row is loaded, also where some are dealt twice, and the halves' sums meet inside the stages"""
+    for BM, BN, WGM, WGN, stages in ((96, 128, 1, 4, 3), (64, 128, 2, 2, 3), (64, 64, 2, 2, 4), (128, 128, 2, 2, 3), (64, 64, 2, 1, 4)):
+        group, total = WGM * WGN, (BM + BN) // 8
+        waves = 2 * group
+        dealt = [min(j * waves + w, total - 1) for j in range(-(-total // waves)) for w in range(waves)]
+        assert sorted(set(dealt)) == list(range(total))
+        blocks = (BM // WGM // 16) * (BN // WGN // 16)
+        at = lambda wave, write: {(wave % group * blocks + ((1 - wave // group if write else wave // group) * blocks // 2 + i)) * 64 + lane for i in range(blocks // 2) for lane in range(64)}
+        written = [at(w, True) for w in range(waves)]
+        assert sum(map(len, written)) == len(set().union(*written)) and max(map(max, written)) < stages * (BM + BN) * 8
+        for w in range(waves):
+            assert at(w, False) == written[(w + group) % waves]       # what the other half wrote
+
+
 def test_binding_refuses_what_the_c_call_cannot_see(B):
     import torch
     q, s = torch.zeros(6, 144, dtype=torch.float8_e4m3fn), torch.zeros(2, 8, dtype=torch.uint8).view(torch.float8_e8m0fnu)

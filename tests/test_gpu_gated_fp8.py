@@ -622,12 +622,12 @@ LIN8_KERNELS = [("bfloat16", *c) for c in [
     (3, 4463, 784, "gemm cols 8 bits 64x64/4 waves/4 stages guard"), (6877, 263, 256, "gemm cols 8 bits 96x128/4 waves/3 stages"),
     (11111, 141, 768, "gemm cols 8 bits 96x128/4 waves/3 stages"), (8807, 197, 784, "gemm cols 8 bits 96x128/4 waves/3 stages guard")]] + [("float32", *c) for c in [
     (4281, 1, 768, "few rows 8 bits 32x16"), (1, 4228, 784, "few rows 8 bits 32x32"), (8397, 1, 16, "few rows 8 bits 64x32"),
-    (6254, 419, 768, "gemm cols 8 bits wide 128x128/4 waves/2 stages"), (6639, 263, 16, "gemm cols 8 bits wide 128x128/4 waves/2 stages guard"),
+    (6254, 419, 768, "gemm cols 8 bits wide 64x64/8 waves/4 stages"), (6639, 263, 16, "gemm cols 8 bits wide 96x128/8 waves/3 stages guard"),
     (777, 5036, 768, "gemm cols 8 bits wide 128x192/8 waves/3 stages"), (8203, 456, 880, "gemm cols 8 bits wide 128x192/8 waves/3 stages guard"),
     (8239, 67, 896, "gemm cols 8 bits wide 64x128/8 waves/3 stages"), (9071, 78, 16, "gemm cols 8 bits wide 64x128/8 waves/3 stages guard"),
-    (71, 4864, 768, "gemm cols 8 bits wide 64x64/4 waves/4 stages"), (66, 4143, 816, "gemm cols 8 bits wide 64x64/4 waves/4 stages guard"),
-    (1239, 4937, 128, "gemm cols 8 bits wide 96x128/4 waves/3 stages"), (11391, 154, 768, "gemm cols 8 bits wide 96x128/4 waves/3 stages"),
-    (11271, 153, 784, "gemm cols 8 bits wide 96x128/4 waves/3 stages guard")]]
+    (71, 4864, 768, "gemm cols 8 bits wide 64x64/8 waves/4 stages"), (66, 4143, 816, "gemm cols 8 bits wide 64x64/8 waves/4 stages guard"),
+    (1239, 4937, 128, "gemm cols 8 bits wide 128x256/8 waves/3 stages"), (8465, 603, 816, "gemm cols 8 bits wide 128x256/8 waves/3 stages guard"), (11391, 154, 768, "gemm cols 8 bits wide 96x128/8 waves/3 stages"),
+    (11271, 153, 784, "gemm cols 8 bits wide 96x128/8 waves/3 stages guard")]]
 
 
 @pytest.mark.parametrize("yt,M,N,K,kernel", LIN8_KERNELS)
@@ -651,9 +651,10 @@ GATED8_KERNELS = [("bfloat16", *c) for c in [
     (555, 5504, 928, "gemm cols 8 bits gated 128x256/8 waves/3 stages guard"), (11125, 144, 768, "gemm cols 8 bits gated 256x128/8 waves/3 stages"), (10904, 144, 800, "gemm cols 8 bits gated 256x128/8 waves/3 stages guard"),
     (10892, 336, 768, "gemm cols 8 bits gated 256x256/8 waves/2 stages"), (6700, 592, 784, "gemm cols 8 bits gated 256x256/8 waves/2 stages guard"), (65, 4416, 768, "gemm cols 8 bits gated 64x128/4 waves/3 stages"),
     (69, 4544, 832, "gemm cols 8 bits gated 64x128/4 waves/3 stages guard"), (1, 4144, 768, "gemm cols 8 bits gated 64x64/2 waves/4 stages"), (1, 4256, 848, "gemm cols 8 bits gated 64x64/2 waves/4 stages guard")]] + [("float32", *c) for c in [
-    (17, 2224, 784, "few rows 8 bits gated 32x16"), (1, 4288, 768, "few rows 8 bits gated 32x32"), (130, 5600, 896, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages"),
-    (145, 5632, 784, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages guard"), (70, 4336, 768, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages"), (67, 4480, 848, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages guard"),
-    (8255, 16, 768, "gemm cols 8 bits wide gated 64x64/2 waves/4 stages"), (8909, 16, 784, "gemm cols 8 bits wide gated 64x64/2 waves/4 stages guard")]] + [("float8_e4m3fn", *c) for c in [
+    (17, 2224, 784, "few rows 8 bits gated 32x16"), (1, 4288, 768, "few rows 8 bits gated 32x32"), (130, 5600, 896, "gemm cols 8 bits wide gated 128x128/8 waves/3 stages"),
+    (145, 5632, 784, "gemm cols 8 bits wide gated 128x128/8 waves/3 stages guard"), (412, 4800, 768, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages"),
+    (583, 3328, 848, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages guard"), (70, 4336, 768, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages"), (67, 4480, 848, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages guard"),
+    (8255, 16, 768, "gemm cols 8 bits wide gated 64x64/4 waves/4 stages"), (8909, 16, 784, "gemm cols 8 bits wide gated 64x64/4 waves/4 stages guard")]] + [("float8_e4m3fn", *c) for c in [
     (1, 16, 1936, "few rows 8 bits gated 16x16; quantize"), (9309, 144, 768, "gemm cols 8 bits gated to 8 bits 128x256/8 waves/3 stages"), (9045, 144, 880, "gemm cols 8 bits gated to 8 bits 128x256/8 waves/3 stages guard"),
     (6662, 544, 768, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages"), (11037, 272, 784, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages guard"), (1, 16, 768, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages"),
     (3, 144, 784, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages guard")]]
@@ -755,11 +756,11 @@ def test_fp8_offsets_past_32_bits(B):
     assert float((y[rows].double() - check[0].double()).norm() / check[0].double().norm()) < 2.0 ** -8
 
 
-GATED_KERNELS = [(1, 1, 384, "few rows gated 16x16"), (4249, 1, 8, "few rows gated 32x16"), (3, 4271, 392, "few rows gated 32x32"), (8507, 74, 64, "gemm cols gated 128x128/4 waves/2 stages"), (5481, 162, 384, "gemm cols gated 128x128/4 waves/2 stages"),
-                 (141, 5711, 464, "gemm cols gated 128x128/4 waves/2 stages guard"), (524, 5757, 384, "gemm cols gated 128x256/8 waves/3 stages"), (2420, 1606, 400, "gemm cols gated 128x256/8 waves/3 stages guard"),
+GATED_KERNELS = [(1, 1, 384, "few rows gated 16x16"), (4249, 1, 8, "few rows gated 32x16"), (3, 4271, 392, "few rows gated 32x32"), (8507, 74, 64, "gemm cols gated 64x64/4 waves/4 stages"), (5481, 162, 384, "gemm cols gated 128x128/8 waves/3 stages"),
+                 (141, 5711, 464, "gemm cols gated 128x128/8 waves/3 stages guard"), (524, 5757, 384, "gemm cols gated 128x256/8 waves/3 stages"), (2420, 1606, 400, "gemm cols gated 128x256/8 waves/3 stages guard"),
                  (5466, 350, 384, "gemm cols gated 256x128/8 waves/3 stages"), (11124, 129, 408, "gemm cols gated 256x128/8 waves/3 stages guard"), (10947, 334, 64, "gemm cols gated 256x256/8 waves/2 stages"),
                  (10947, 334, 384, "gemm cols gated 256x256/8 waves/2 stages"), (770, 5075, 392, "gemm cols gated 256x256/8 waves/2 stages guard"), (8523, 34, 384, "gemm cols gated 64x128/4 waves/3 stages"),
-                 (9192, 37, 392, "gemm cols gated 64x128/4 waves/3 stages guard"), (8277, 1, 384, "gemm cols gated 64x64/2 waves/4 stages"), (8417, 3, 464, "gemm cols gated 64x64/2 waves/4 stages guard")]
+                 (9192, 37, 392, "gemm cols gated 64x128/4 waves/3 stages guard"), (8277, 1, 384, "gemm cols gated 64x64/4 waves/4 stages"), (8417, 3, 464, "gemm cols gated 64x64/4 waves/4 stages guard")]
 
 
 @pytest.mark.parametrize("M,N,K,kernel", GATED_KERNELS)
