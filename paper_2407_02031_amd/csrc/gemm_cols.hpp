@@ -108,7 +108,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     constexpr int BP = MI % 4 == 0 ? 4 : 2, BQ = OUT8 ? 4 : 2;
     constexpr int BN_OUT = GATED ? BN / 2 : BN, WN_OUT = GATED ? WN / 2 : WN;
     static_assert(MI % BP == 0 && NV % BQ == 0 && NI % RING == 0 && (!WIDE || NI % 2 == 0) && STAGES >= 2 && STAGES <= 4, "tile");
-    static_assert(KS == 1 || (KS == 2 && MODE != COLS_FP8 && MI % 2 == 0 && !OUT8 && WGM * WGN * MI * NI * 64 <= STAGES * STAGE), "halves");
+    static_assert(KS == 1 || (KS == 2 && MODE != COLS_FP8 && MI % 2 == 0 && WGM * WGN * MI * NI * 64 <= STAGES * STAGE), "halves");
     static_assert(!FP8 || PIECES <= NW, "scales");
     static_assert(NW * 64 >= BN, "bias");
     static_assert(!OUT8 || (GATED && FP8 && BN_OUT == FP8_BLOCK), "a tile's columns are one block of y");
@@ -411,9 +411,9 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
                 if (col + x < N) v[x / 4][x % 4] += (float)p[at + x];
     };
     __bf16* const zb = reinterpret_cast<__bf16*>(P.z);
-    float top[OUT8 ? MI : 1];
+    float top[OUT8 ? ME : 1];
 #pragma unroll
-    for (int mi = 0; mi < (OUT8 ? MI : 1); ++mi) top[mi] = 0.f;
+    for (int mi = 0; mi < (OUT8 ? ME : 1); ++mi) top[mi] = 0.f;
 #pragma unroll
     for (int gr = 0; gr < NG; ++gr) {
         const int col = column(gr);
@@ -465,7 +465,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         uint32_t* const meet = reinterpret_cast<uint32_t*>(bias + BN);      // [WGN][BM]
         bool finite = true;
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
+        for (int mi = 0; mi < ME; ++mi) {
             uint32_t u = __float_as_uint(top[mi]);
             if (u >= 0x7f800000u) {
                 finite = false;
@@ -481,7 +481,7 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         __syncthreads();
         const bool plain = __all(finite);
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
+        for (int mi = 0; mi < ME; ++mi) {
             const int r = row_of(mi), m = m0 + r;
             uint32_t u = 0;
 #pragma unroll

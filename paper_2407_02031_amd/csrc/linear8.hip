@@ -5,7 +5,7 @@
 // On the tiles of gemm_cols.hpp: the scaled MFMA multiplies at twice the rate of a bf16 one and reads half the bytes.
 //
 // Measured: 8192 x 4096 x 4096 bf16 out 119 us (2.3 PFLOP/s; the library's 102), 8192 x 5120 x 1280 67.6 (1.6; the library's 72); gated with SiLU, 8192 x 5120 x 1280, 101 to bf16, 103 to 8 bits (2.1; the library's
-// product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 32.2.  One row, 5120 x 1280 gated to 8 bits 10.2 to 10.8, 1280 x 5120 onto fp32 6.5.
+// product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 32.2.  One row, 5120 x 1280 gated to 8 bits 11.0 to 11.3, 1280 x 5120 onto fp32 6.5.
 #include "gemm_cols.hpp"
 
 #include <string.h>
@@ -155,6 +155,8 @@ extern "C" int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales
     if (out8 && !gated8_two_launches(M, N, K)) {
         P.ys = y_scales;
         P.ldys = y_lds;
+        // Up to 64 rows, where weights are all that counts, widened operands cost nothing (us, 32 x 256 widened / 64 x 256: one row 5120 x 1280 11.4 / 11.8, 10240 x 2560 21.1 / 21.4, 1280 x 2560 15.7 / 15.1)
+        if (M <= 64 && (int64_t)((M + 31) / 32) * ((N + FP8_BLOCK - 1) / FP8_BLOCK) <= 256) return launch_cols<COLS_FP8_WIDE, 32, 256, 1, 2, 3, true, true, 2>(P, s);
         float us;
         switch (cols_choose(GATED8_TO_8, M, 2ll * N, K, us)) {
         case 0: return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, true, true>(P, s);

@@ -182,7 +182,7 @@ def test_every_access_of_a_tile_is_inside(B):
     """The tiles' loads, by the arithmetic of the kernels: rows, chunks and scale words of every lane, wavefront and step stay inside the operands"""
     def spread(b, i, B_):
         return b // B_ * 16 * B_ + B_ * i + b % B_
-    shapes = [(256, 256, 4, 2), (256, 256, 2, 4), (128, 256, 2, 4), (128, 256, 4, 2), (256, 128, 4, 2), (128, 192, 4, 2), (96, 128, 1, 4), (128, 128, 2, 2), (64, 128, 2, 2), (64, 128, 2, 4), (64, 64, 2, 2), (64, 64, 2, 1), (64, 256, 2, 2)]
+    shapes = [(256, 256, 4, 2), (256, 256, 2, 4), (128, 256, 2, 4), (128, 256, 4, 2), (256, 128, 4, 2), (128, 192, 4, 2), (96, 128, 1, 4), (128, 128, 2, 2), (64, 128, 2, 2), (64, 128, 2, 4), (64, 64, 2, 2), (64, 64, 2, 1), (64, 256, 2, 2), (32, 256, 1, 2)]
     for BM, BN, WGM, WGN in shapes:
         for gated_, bq in ((False, 2), (True, 2), (True, 4)):
             NW, WM, WN = WGM * WGN, BM // WGM, BN // WGN
@@ -220,7 +220,7 @@ def test_every_access_of_a_tile_is_inside(B):
 
 def test_halved_steps(B):
     """Tiles whose wavefronts take half of each step: every row is loaded, also where some are dealt twice, and the halves' sums meet inside the stages"""
-    for BM, BN, WGM, WGN, stages in ((96, 128, 1, 4, 3), (64, 128, 2, 2, 3), (64, 64, 2, 2, 4), (128, 128, 2, 2, 3), (64, 64, 2, 1, 4)):
+    for BM, BN, WGM, WGN, stages in ((96, 128, 1, 4, 3), (64, 128, 2, 2, 3), (64, 64, 2, 2, 4), (128, 128, 2, 2, 3), (64, 64, 2, 1, 4), (32, 256, 1, 2, 3)):
         group, total = WGM * WGN, (BM + BN) // 8
         waves = 2 * group
         dealt = [min(j * waves + w, total - 1) for j in range(-(-total // waves)) for w in range(waves)]

@@ -656,8 +656,9 @@ GATED8_KERNELS = [("bfloat16", *c) for c in [
     (583, 3328, 848, "gemm cols 8 bits wide gated 128x128/4 waves/2 stages guard"), (70, 4336, 768, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages"), (67, 4480, 848, "gemm cols 8 bits wide gated 64x128/4 waves/3 stages guard"),
     (8255, 16, 768, "gemm cols 8 bits wide gated 64x64/4 waves/4 stages"), (8909, 16, 784, "gemm cols 8 bits wide gated 64x64/4 waves/4 stages guard")]] + [("float8_e4m3fn", *c) for c in [
     (1, 16, 1936, "few rows 8 bits gated 16x16; quantize"), (9309, 144, 768, "gemm cols 8 bits gated to 8 bits 128x256/8 waves/3 stages"), (9045, 144, 880, "gemm cols 8 bits gated to 8 bits 128x256/8 waves/3 stages guard"),
-    (6662, 544, 768, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages"), (11037, 272, 784, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages guard"), (1, 16, 768, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages"),
-    (3, 144, 784, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages guard")]]
+    (6662, 544, 768, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages"), (11037, 272, 784, "gemm cols 8 bits gated to 8 bits 256x256/8 waves/2 stages guard"), (1, 16, 768, "gemm cols 8 bits wide gated to 8 bits 32x256/4 waves/3 stages"),
+    (3, 144, 784, "gemm cols 8 bits wide gated to 8 bits 32x256/4 waves/3 stages guard"), (64, 1296, 640, "gemm cols 8 bits wide gated to 8 bits 32x256/4 waves/3 stages"),
+    (64, 32896, 128, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages"), (65, 144, 768, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages"), (70, 144, 784, "gemm cols 8 bits gated to 8 bits 64x256/4 waves/3 stages guard")]]
 
 
 @pytest.mark.parametrize("yt,M,N,K,kernel", GATED8_KERNELS)
@@ -689,6 +690,22 @@ def test_gated_fp8_in_two_launches(B, M, N, K):
     ws = torch.full((need + 256,), 77, dtype=torch.uint8, device="cuda")
     mine = B.gated_linear_fp8_fwd(x, W, out_dtype=torch.float8_e4m3fn, ws=ws)
     assert torch.equal(mine.q.view(torch.uint8), y.q.view(torch.uint8)) and (ws[need:] == 77).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 5120, 128), (1, 16, 16), (5, 144, 80), (33, 1296, 112), (64, 640, 48)])
+def test_gated_fp8_of_few_rows_keeps_all_of_a_sum(B, M, N, K):
+    """Up to 64 rows are multiplied widened: of products of 8 beside one of 2^14 the scaled MFMA drops up to 2 each, and what fp32 may lose of a sum is (K + 8) 2^-23 2^15, 0.5 at most"""
+    import torch
+    g = gen(M + N)
+    a, w = randn(g, M, K, scale=2.8), randn(g, 2 * N, K, scale=2.8)
+    a[:, 0], a[:, 8], w[:, 0], w[:, 8] = 128.0, -128.0, 128.0, 128.0
+    x, W = B.quantize_fp8(a), B.quantize_fp8(w)
+    with B.dry_run() as names:
+        B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=torch.float8_e4m3fn)
+    assert "wide" in names[0]
+    y = B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=torch.float8_e4m3fn)
+    ref, slack = gated_ref(*product(x, W, None, True), 0)
+    within_fp8(y, ref, slack)
 
 
 def test_scales_at_their_ends(B):
