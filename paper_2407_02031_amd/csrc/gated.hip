@@ -4,7 +4,7 @@
 //
 // Both projections, the activation and the product in one kernel (gemm_cols.hpp); v and g are kept in bf16 where the backward pass (linear.hip) wants them.
 //
-// Measured: 8192 x 5120 x 1280 with SiLU 188 us, 213 with v and g kept (252 MB of results; 1.0 to 1.1 PFLOP/s, the library's product alone 176).
+// Measured: 8192 x 5120 x 1280 with SiLU 188 us, 209 with v and g kept (252 MB of results; 1.0 to 1.1 PFLOP/s, the library's product alone 176).
 #include "gemm_cols.hpp"
 
 #include <string.h>

@@ -379,8 +379,10 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     float* const bias = reinterpret_cast<float*>(lds + STAGES * STAGE);
     if (tid < BN) bias[tid] = bf16_to_f32(bias_raw);
     __syncthreads();
-    // (a row's last columns one by one)
-    auto store = [&](auto* p, int64_t at, int col, const f32x4 (&v)[W4]) {
+    // A row's last columns one by one.  What is stored `past` the caches leaves them to the operands.  z, which waits for the backward pass (us, norm, gated layer and linear layer, past / through: 8192 x 1280
+    // to 5120 370 / 386, 16384 x 640 to 2560 211 / 247, 8192 x 320 to 1280 57.3 / 56.6; with their backward passes 1092 / 1095, 734 / 736, 177 / 176).  Not y in bf16 or fp32, though a launch alone would gain up to
+    // 13 % (8192 x 1280 to 5120 163 / 188 us): the linear layer behind it loses as much (both 288 / 285, 4096 rows 167 / 162).
+    auto store = [&](auto* p, int64_t at, int col, const f32x4 (&v)[W4], auto past) {
         using T = std::remove_pointer_t<decltype(p)>;
         if (col + 4 * W4 <= N) {
 #pragma unroll
@@ -388,6 +390,11 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
                 if constexpr (std::is_same_v<T, float>) {
                     store4(p + at + 4 * c, v[c]);
                     store4(p + at + 4 * c + 4, v[c + 1]);
+                } else if constexpr (decltype(past)::value) {
+                    bf16x8u o;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) o[x] = (__bf16)v[c + x / 4][x % 4];
+                    __builtin_nontemporal_store(o, reinterpret_cast<bf16x8u*>(p + at + 4 * c));
                 } else {
                     store8(p + at + 4 * c, f32x8{v[c], v[c + 1]});
                 }
@@ -434,8 +441,8 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
             }
             if constexpr (GATED) {
                 if (!OUT8 && P.z && m < M) {
-                    store(zb, (int64_t)m * 2 * N + col, col, v);
-                    store(zb, (int64_t)m * 2 * N + N + col, col, g);
+                    store(zb, (int64_t)m * 2 * N + col, col, v, std::true_type());
+                    store(zb, (int64_t)m * 2 * N + N + col, col, g, std::true_type());
                 }
                 apply_act(P.act, g);
 #pragma unroll
@@ -456,8 +463,8 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
                     for (int x = 0; x < 4; ++x) element(mi, 0, gr, c, x) = v[c][x];
                 }
             } else if (m < M) {
-                if (P.y_f32) store(static_cast<float*>(P.y), (int64_t)m * N + col, col, v);
-                else store(static_cast<__bf16*>(P.y), (int64_t)m * N + col, col, v);
+                if (P.y_f32) store(static_cast<float*>(P.y), (int64_t)m * N + col, col, v, std::false_type());
+                else store(static_cast<__bf16*>(P.y), (int64_t)m * N + col, col, v, std::false_type());
             }
         }
     }
@@ -480,6 +487,8 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         }
         __syncthreads();
         const bool plain = __all(finite);
+        // (y of half the bytes, if it is large, does: 8192 x 1280 to 5120 92.3 / 104.7 us past / through, with the linear layer behind it 213 / 218, 4096 rows 54 / 63.5 and 115.4 / 116.8; 1024 rows 25.4 / 27.7, but 51.2 / 49.7)
+        const bool past = (int64_t)M * N > 8ll << 20;
 #pragma unroll
         for (int mi = 0; mi < ME; ++mi) {
             const int r = row_of(mi), m = m0 + r;
@@ -500,7 +509,11 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
 #pragma unroll
                         for (int c = 0; c < 4; ++c) w[c] = fp8_pack(piece(mi, 0, g, c), inv);
                     const int col = column(g);
-                    if (col < N) *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(P.y) + (int64_t)m * N + col) = w;
+                    if (col < N) {
+                        u32x4* const to = reinterpret_cast<u32x4*>(static_cast<uint8_t*>(P.y) + (int64_t)m * N + col);
+                        if (past) __builtin_nontemporal_store(w, to);
+                        else *to = w;
+                    }
                 }
             }
         }

@@ -4,7 +4,7 @@
 //
 // On the tiles of gemm_cols.hpp: the scaled MFMA multiplies at twice the rate of a bf16 one and reads half the bytes.
 //
-// Measured: 8192 x 4096 x 4096 bf16 out 119 us (2.3 PFLOP/s; the library's 102), 8192 x 5120 x 1280 67.6 (1.6; the library's 72); gated with SiLU, 8192 x 5120 x 1280, 101 to bf16, 103 to 8 bits (2.1; the library's
+// Measured: 8192 x 4096 x 4096 bf16 out 119 us (2.3 PFLOP/s; the library's 102), 8192 x 5120 x 1280 67.6 (1.6; the library's 72); gated with SiLU, 8192 x 5120 x 1280, 101 to bf16, 102 to 8 bits (2.1; the library's
 // product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 32.2.  One row, 5120 x 1280 gated to 8 bits 11.0 to 11.3, 1280 x 5120 onto fp32 6.5.
 #include "gemm_cols.hpp"
 
