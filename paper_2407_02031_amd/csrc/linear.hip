@@ -153,7 +153,9 @@ struct DzCut {
 
 // The same of a gated layer: dy [M, N] and z = [v, g] [M, 2 N] in, dz = [dy act(g), dy v act'(g)] [M, Np] out, Np 2 N rounded up to a multiple of 8; its column sums are 2 N.  Where N is
 // no multiple of eight, accesses to the gate's half are aligned to an element alone.  Bound by HBM: 8192 x 5120 bf16 with SiLU 72 to 74 us (420 MB, 5.7 TB/s).  dz is rounded to bf16 as above.
-template <class D, bool STORE, bool SUMS, int CT, int NT>
+// PAST: a large z is read past the caches, which dz has to itself then (all of the backward pass, us, past / through: 8192 x 1280 to 5120 456 / 463, 8192 x 640 to 2560 151 / 157, 4096 x 1280 to 5120 231.7 / 233.4;
+// but 2048 135.5 / 134.8 and 2048 x 640 to 2560 50.6 / 49.4).
+template <class D, bool STORE, bool SUMS, bool PAST, int CT, int NT>
 __global__ __launch_bounds__(NT) void gated_dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
     constexpr int SUB = NT / CT, BATCH = 2;
     constexpr int PARTS = CT < 64 ? NT / 64 : SUB;          // sums of a column that meet in LDS
@@ -168,6 +170,11 @@ __global__ __launch_bounds__(NT) void gated_dz_kernel(const D* __restrict__ dy, 
     const __bf16* const zb = reinterpret_cast<const __bf16*>(z);
     __bf16* const out = reinterpret_cast<__bf16*>(dz);
     const int at = c + 8 <= N ? c : N - 8;        // (as in dz_kernel)
+    auto load_z = [](const __bf16* p) {
+        if constexpr (!PAST) return load8(p);
+        const bf16x8u v = __builtin_nontemporal_load(reinterpret_cast<const bf16x8u*>(p));
+        return f32x8{{(float)v[0], (float)v[1], (float)v[2], (float)v[3]}, {(float)v[4], (float)v[5], (float)v[6], (float)v[7]}};
+    };
     auto all = [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
         auto one = [&](f32x4& d, f32x4& v, const f32x4& g) {        // d <- dy act(g), v <- dy v act'(g)
@@ -196,8 +203,8 @@ __global__ __launch_bounds__(NT) void gated_dz_kernel(const D* __restrict__ dy, 
                 for (int i = 0; i < BATCH; ++i) {
                     const int64_t row = min(r + i * SUB, r1 - 1);
                     d[i] = load8(dy + row * N + at);
-                    v[i] = load8(zb + row * 2 * N + at);
-                    g[i] = load8(zb + row * 2 * N + N + at);
+                    v[i] = load_z(zb + row * 2 * N + at);
+                    g[i] = load_z(zb + row * 2 * N + N + at);
                 }
 #pragma unroll
                 for (int i = 0; i < BATCH; ++i)
@@ -864,9 +871,16 @@ extern "C" int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16
             using D = std::remove_pointer_t<decltype(t)>;
             constexpr int CT = decltype(ct)::value, NT = decltype(nt)::value;
             const D* const d = static_cast<const D*>(dy);
-            if (store && dbias) hipLaunchKernelGGL((gated_dz_kernel<D, true, true, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
-            else if (store) hipLaunchKernelGGL((gated_dz_kernel<D, true, false, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
-            else hipLaunchKernelGGL((gated_dz_kernel<D, false, true, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
+            auto launch = [&](auto stored, auto summed, auto past) {
+                hipLaunchKernelGGL((gated_dz_kernel<D, decltype(stored)::value, decltype(summed)::value, decltype(past)::value, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
+            };
+            const std::true_type yes;
+            const std::false_type no;
+            if constexpr (CT == 64)
+                if (store && (int64_t)M * N > 16ll << 20) return dbias ? launch(yes, yes, yes) : launch(yes, no, yes);
+            if (store && dbias) launch(yes, yes, no);
+            else if (store) launch(yes, no, no);
+            else launch(no, yes, no);
         };
         auto by_cut = [&](auto* t) {
             if (cut.ct == 2) run(t, std::integral_constant<int, 2>(), std::integral_constant<int, 1024>());

@@ -434,6 +434,26 @@ def test_gated_bwd_large(B, M, N, K):
     check_gated_bwd(B, randn(g, M, N), x, W, z, 2, torch.float32)
 
 
+@pytest.mark.parametrize("M,N,K", [(8200, 2064, 16), (8400, 2001, 24)])
+def test_gated_results_past_the_caches(B, M, N, K):
+    """z of more than 2^25 elements"""
+    import torch
+    x, W, bias, g = lin_inputs(M, 2 * N, K, M + N)
+    check_gated_fwd(B, x, W, bias, 3, torch.bfloat16)
+    _, z = B.gated_linear_fwd(x, W, bias, 3, save_z=True)
+    dy = randn(g, M, N).bfloat16()
+    check_gated_bwd(B, dy, x, W, z, 3, torch.bfloat16)
+    check_gated_bwd(B, dy.float(), x, W, z, 1, torch.float32)
+
+
+def test_gated_fp8_past_the_caches(B):
+    """y in 8 bits of more than 2^23 elements"""
+    import torch
+    g = gen(31)
+    x, W = rows8(B, g, 8200, 144), rows8(B, g, 2 * 1040, 144, 0.1)
+    check_gated8(B, x, W, randn(g, 2 * 1040, scale=0.5).bfloat16(), 3, torch.float8_e4m3fn)
+
+
 def test_gated_gradients_against_differences(B):
     import torch
     M, N, K = 3, 9, 16
