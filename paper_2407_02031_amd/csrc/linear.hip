@@ -151,15 +151,27 @@ struct DzCut {
     }
 };
 
+constexpr int GATED_DZ_THREADS = 256;
+// ... of a gated layer's: 64 x 4 threads for any rows.  (Few rows in one block, as above, would take workgroups of 1024 threads whose registers do not hold two columns' sums of eight: all of the
+// backward pass, us, these / those: one row of 1280 to 5120 27.6 / 40.5, 200 41 / 51, 77 of 640 to 640 12.0 / 16.1, 1000 of 640 to 64 17.3 / 23.1.)
+struct GatedDzCut {
+    int rows;
+    int64_t col_wgs, blocks;
+    GatedDzCut(int64_t M, int64_t N) {
+        col_wgs = (N + 511) / 512;
+        const int64_t r = M * col_wgs / 512;
+        rows = r >= 32 ? 32 : r >= 16 ? 16 : 8;
+        blocks = (M + rows - 1) / rows;
+    }
+};
 // The same of a gated layer: dy [M, N] and z = [v, g] [M, 2 N] in, dz = [dy act(g), dy v act'(g)] [M, Np] out, Np 2 N rounded up to a multiple of 8; its column sums are 2 N.  Where N is
 // no multiple of eight, accesses to the gate's half are aligned to an element alone.  Bound by HBM: 8192 x 5120 bf16 with SiLU 72 to 74 us (420 MB, 5.7 TB/s).  dz is rounded to bf16 as above.
 // PAST: a large z is read past the caches, which dz has to itself then (all of the backward pass, us, past / through: 8192 x 1280 to 5120 456 / 463, 8192 x 640 to 2560 151 / 157, 4096 x 1280 to 5120 231.7 / 233.4;
 // but 2048 135.5 / 134.8 and 2048 x 640 to 2560 50.6 / 49.4).
-template <class D, bool STORE, bool SUMS, bool PAST, int CT, int NT>
-__global__ __launch_bounds__(NT) void gated_dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
-    constexpr int SUB = NT / CT, BATCH = 2;
-    constexpr int PARTS = CT < 64 ? NT / 64 : SUB;          // sums of a column that meet in LDS
-    __shared__ f32x8 sh[2 * (PARTS - 1) * CT];
+template <class D, bool STORE, bool SUMS, bool PAST>
+__global__ __launch_bounds__(GATED_DZ_THREADS) void gated_dz_kernel(const D* __restrict__ dy, const uint16_t* __restrict__ z, int act, uint16_t* __restrict__ dz, float* __restrict__ sums, int M, int N, int Np, int rows, int blocks) {
+    constexpr int CT = 64, SUB = GATED_DZ_THREADS / CT, BATCH = 2;
+    __shared__ f32x8 sh[2 * (SUB - 1) * CT];
     const int t = threadIdx.x % CT, sub = threadIdx.x / CT;
     const int cols = (int)blockIdx.x / blocks, block = (int)blockIdx.x - cols * blocks;
     const int c = (cols * CT + t) * 8;
@@ -248,27 +260,14 @@ __global__ __launch_bounds__(NT) void gated_dz_kernel(const D* __restrict__ dy, 
         for (int64_t r = r0; r < r1; r += SUB)
             for (int e = 2 * N; e < Np; ++e) dz[r * Np + e] = 0;
     if (SUMS) {
-        int part = sub;
-        if constexpr (CT < 64) {       // the rows of a wavefront
-#pragma unroll
-            for (int o = CT; o < 64; o *= 2)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    sv.lo[e] += __shfl_xor(sv.lo[e], o);
-                    sv.hi[e] += __shfl_xor(sv.hi[e], o);
-                    sg.lo[e] += __shfl_xor(sg.lo[e], o);
-                    sg.hi[e] += __shfl_xor(sg.hi[e], o);
-                }
-            part = threadIdx.x >> 6;
-        }
-        if (part && (CT >= 64 || (threadIdx.x & 63) < CT)) {
-            sh[(part - 1) * 2 * CT + t] = sv;
-            sh[(part - 1) * 2 * CT + CT + t] = sg;
+        if (sub) {
+            sh[(sub - 1) * 2 * CT + t] = sv;
+            sh[(sub - 1) * 2 * CT + CT + t] = sg;
         }
         __syncthreads();
         if (threadIdx.x >= CT || c >= N) return;
 #pragma unroll
-        for (int w = 0; w < PARTS - 1; ++w) {
+        for (int w = 0; w < SUB - 1; ++w) {
             sv.lo += sh[w * 2 * CT + t].lo;
             sv.hi += sh[w * 2 * CT + t].hi;
             sg.lo += sh[w * 2 * CT + CT + t].lo;
@@ -708,7 +707,7 @@ struct GatedBwdWs {
     size_t dz, sums, dx_parts, dw_parts;
     GatedBwdWs(int64_t M, int64_t N, int64_t K) {
         dz = (size_t)M * ((2 * N + 7) & ~7ll) * 2;
-        sums = (size_t)DzCut(M, N).blocks * 2 * N * 4;
+        sums = (size_t)GatedDzCut(M, N).blocks * 2 * N * 4;
         const BwdPlan p(M, 2 * N, K);
         dx_parts = p.x.bytes();
         dw_parts = p.w.bytes();
@@ -861,33 +860,29 @@ extern "C" int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16
     float* const dx_parts = static_cast<float*>(w.take(b.dx_parts));
     float* const dw_parts = static_cast<float*>(w.take(b.dw_parts));
     const int Np = (2 * N + 7) & ~7;
-    const DzCut cut(M, N);
+    const GatedDzCut cut(M, N);
     const int blocks = (int)cut.blocks;
     const bool store = dx || dW;
     if (!SD_DRY_RUN("gated dz%s%s; ", store ? "" : " sums only", dbias ? "" : " no sums")) {
         const dim3 grid((unsigned)(cut.blocks * cut.col_wgs));
         float* const to = blocks == 1 ? dbias : sums;
-        auto run = [&](auto* t, auto ct, auto nt) {
+        auto run = [&](auto* t) {
             using D = std::remove_pointer_t<decltype(t)>;
-            constexpr int CT = decltype(ct)::value, NT = decltype(nt)::value;
             const D* const d = static_cast<const D*>(dy);
             auto launch = [&](auto stored, auto summed, auto past) {
-                hipLaunchKernelGGL((gated_dz_kernel<D, decltype(stored)::value, decltype(summed)::value, decltype(past)::value, CT, NT>), grid, dim3(NT), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
+                hipLaunchKernelGGL((gated_dz_kernel<D, decltype(stored)::value, decltype(summed)::value, decltype(past)::value>), grid, dim3(GATED_DZ_THREADS), 0, s, d, z, act, dz, to, M, N, Np, cut.rows, blocks);
             };
             const std::true_type yes;
             const std::false_type no;
-            if constexpr (CT == 64)
-                if (store && (int64_t)M * N > 16ll << 20) return dbias ? launch(yes, yes, yes) : launch(yes, no, yes);
-            if (store && dbias) launch(yes, yes, no);
-            else if (store) launch(yes, no, no);
-            else launch(no, yes, no);
+            const bool past = (int64_t)M * N > 16ll << 20;
+            if (!store) launch(no, yes, no);
+            else if (dbias && past) launch(yes, yes, yes);
+            else if (dbias) launch(yes, yes, no);
+            else if (past) launch(yes, no, yes);
+            else launch(yes, no, no);
         };
-        auto by_cut = [&](auto* t) {
-            if (cut.ct == 2) run(t, std::integral_constant<int, 2>(), std::integral_constant<int, 1024>());
-            else run(t, std::integral_constant<int, 64>(), std::integral_constant<int, 256>());
-        };
-        if (y_dtype == SD_F32) by_cut(static_cast<float*>(nullptr));
-        else by_cut(static_cast<__bf16*>(nullptr));
+        if (y_dtype == SD_F32) run(static_cast<float*>(nullptr));
+        else run(static_cast<__bf16*>(nullptr));
         SD_HIP_CHECK(hipGetLastError());
     }
     if (dbias && blocks > 1) {
