@@ -577,10 +577,11 @@ _E4M3, _E8M0 = (torch.float8_e4m3fn,), (torch.float8_e8m0fnu,)
 
 def _new_fp8(x: torch.Tensor, M: int, K: int):
     """Room for rows in 8 bits, its two addresses and the distance of its blocks' scales."""
-    q = x.new_empty((M, K), dtype=torch.float8_e4m3fn)
-    ld = (M + 3) & ~3
-    s = x.new_empty(((K + 127) // 128, ld), dtype=torch.float8_e8m0fnu)
-    return Fp8Rows(q, s if ld == M else s.narrow(1, 0, M)), q.data_ptr(), s.data_ptr(), ld
+    # (with strides given these take 1.2 and 0.7 us; new_empty and narrow 1.45 and 1.1)
+    dev, ld, blocks = x.device, (M + 3) & ~3, (K + 127) // 128
+    q = torch.empty_strided((M, K), (K, 1), dtype=torch.float8_e4m3fn, device=dev)
+    s = torch.empty_strided((blocks, ld), (ld, 1), dtype=torch.float8_e8m0fnu, device=dev)
+    return Fp8Rows(q, s if ld == M else s.as_strided((blocks, M), (ld, 1))), q.data_ptr(), s.data_ptr(), ld
 
 
 def _expect_fp8(name: str, x: Fp8Rows, M: int, K: int, dev: int):
@@ -689,11 +690,11 @@ def gated_linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_
     pw = _expect("W", W, (2 * N, K), _BF16, dev)
     pb = _expect("bias", bias, (2 * N,), _BF16, dev)
     if out is None:
-        y = x.new_empty((M, N), dtype=out_dtype)
+        y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.device)
     else:
         y = out
     py = _expect("out", y, (M, N), _FLOATS, dev)
-    z = x.new_empty((M, 2 * N)) if save_z else None
+    z = torch.empty_strided((M, 2 * N), (2 * N, 1), dtype=torch.bfloat16, device=x.device) if save_z else None
     _check(_lib.sd_gated_linear_fwd(px, pw, pb, act, py, _dt(y), z.data_ptr() if save_z else None, M, N, K, _raw_stream(dev)))
     return (y, z) if save_z else y
 
@@ -727,7 +728,7 @@ def linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_NONE, re
     px, pxs, ldx = _expect_fp8("x", x, M, K, dev)
     pw, pws, ldw = _expect_fp8("W", W, N, K, dev)
     pb = _expect("bias", bias, (N,), _BF16, dev)
-    y = out if out is not None else x.q.new_empty((M, N), dtype=out_dtype)
+    y = out if out is not None else torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.q.device)
     py = _expect("out", y, (M, N), _FLOATS, dev)
     pr = _expect("residual", residual, (M, N), (y.dtype,), dev)
     _check(_lib.sd_linear_fp8_fwd(px, pxs, ldx, pw, pws, ldw, pb, act, pr, py, _dt(y), M, N, K, _raw_stream(dev)))
@@ -755,7 +756,7 @@ def gated_linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_SI
         if nwk or ws is not None:
             w, pwk, nwk = _scratch(x.q, nwk, ws, dev)
     else:
-        y = out if out is not None else x.q.new_empty((M, N), dtype=out_dtype)
+        y = out if out is not None else torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.q.device)
         py, yt = _expect("out", y, (M, N), _FLOATS, dev), _dt(y)
         pys = pwk = None
         ldy = nwk = 0
