@@ -369,7 +369,7 @@ def _on(x: torch.Tensor) -> int:
     dev = x.get_device()
     if dev < 0:
         raise ValueError(f"a tensor on {x.device}: not on a GPU")
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():      # (x is on one, so they are initialised: torch.cuda.current_device, which makes sure, takes twice as long)
         raise ValueError(f"a tensor on {x.device}, the current device is {torch.cuda.current_device()}")
     return dev
 
@@ -628,8 +628,11 @@ def rmsnorm_fwd(x: torch.Tensor, gamma=None, eps: float = 1e-6, residual=None, o
     rt = ld = 0
     if residual is not None:
         pr, rt = _expect("residual", residual, shape, _FLOATS, dev), _dt(residual)
-        h = h_out if h_out is not None else torch.empty_like(residual)
-        ph = _expect("h_out", h, shape, (residual.dtype,), dev)
+        if h_out is None:
+            h = torch.empty_like(residual)
+            ph = h.data_ptr()
+        else:
+            h, ph = h_out, _expect("h_out", h_out, shape, (residual.dtype,), dev)
     elif h_out is not None:
         raise ValueError("h_out: without a residual h is x")
     if isinstance(out, Fp8Rows) or (out is None and out_dtype == torch.float8_e4m3fn):
@@ -640,9 +643,11 @@ def rmsnorm_fwd(x: torch.Tensor, gamma=None, eps: float = 1e-6, residual=None, o
             y, py, ps, ld = _new_fp8(x, M, Cc)
         else:
             y, (py, ps, ld) = out, _expect_fp8("out", out, M, Cc, dev)
+    elif out is None:
+        y = torch.empty_like(x, dtype=out_dtype)
+        py, yt = y.data_ptr(), _dt(y)
     else:
-        y = out if out is not None else torch.empty_like(x, dtype=out_dtype)
-        py, yt = _expect("out", y, shape, _FLOATS, dev), _dt(y)
+        y, py, yt = out, _expect("out", out, shape, _FLOATS, dev), _dt(out)
     if stats:
         rstd = x.new_empty(shape[:-1], dtype=torch.float32)
         prs = rstd.data_ptr()
@@ -691,9 +696,9 @@ def gated_linear_fwd(x: torch.Tensor, W: torch.Tensor, bias=None, act: int = SD_
     pb = _expect("bias", bias, (2 * N,), _BF16, dev)
     if out is None:
         y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.device)
+        py = y.data_ptr()
     else:
-        y = out
-    py = _expect("out", y, (M, N), _FLOATS, dev)
+        y, py = out, _expect("out", out, (M, N), _FLOATS, dev)
     z = torch.empty_strided((M, 2 * N), (2 * N, 1), dtype=torch.bfloat16, device=x.device) if save_z else None
     _check(_lib.sd_gated_linear_fwd(px, pw, pb, act, py, _dt(y), z.data_ptr() if save_z else None, M, N, K, _raw_stream(dev)))
     return (y, z) if save_z else y
@@ -728,8 +733,11 @@ def linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_NONE, re
     px, pxs, ldx = _expect_fp8("x", x, M, K, dev)
     pw, pws, ldw = _expect_fp8("W", W, N, K, dev)
     pb = _expect("bias", bias, (N,), _BF16, dev)
-    y = out if out is not None else torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.q.device)
-    py = _expect("out", y, (M, N), _FLOATS, dev)
+    if out is None:
+        y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.q.device)
+        py = y.data_ptr()
+    else:
+        y, py = out, _expect("out", out, (M, N), _FLOATS, dev)
     pr = _expect("residual", residual, (M, N), (y.dtype,), dev)
     _check(_lib.sd_linear_fp8_fwd(px, pxs, ldx, pw, pws, ldw, pb, act, pr, py, _dt(y), M, N, K, _raw_stream(dev)))
     return y
@@ -756,8 +764,12 @@ def gated_linear_fp8_fwd(x: Fp8Rows, W: Fp8Rows, bias=None, act: int = SD_ACT_SI
         if nwk or ws is not None:
             w, pwk, nwk = _scratch(x.q, nwk, ws, dev)
     else:
-        y = out if out is not None else torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.q.device)
-        py, yt = _expect("out", y, (M, N), _FLOATS, dev), _dt(y)
+        if out is None:
+            y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=x.q.device)
+            py = y.data_ptr()
+        else:
+            y, py = out, _expect("out", out, (M, N), _FLOATS, dev)
+        yt = _dt(y)
         pys = pwk = None
         ldy = nwk = 0
     _check(_lib.sd_gated_linear_fp8_fwd(px, pxs, ldx, pw, pws, ldw, pb, act, py, yt, pys, ldy, M, N, K, pwk, nwk, _raw_stream(dev)))
