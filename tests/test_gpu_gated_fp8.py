@@ -980,3 +980,23 @@ def test_two_launches_captured_with_one_workspace(B):
             w = step(a)
             assert torch.equal(o.q.view(torch.uint8), w.q.view(torch.uint8)) and torch.equal(o.scales.view(torch.uint8).contiguous(), w.scales.view(torch.uint8).contiguous())
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 10240, 5120), (16, 10240, 5120), (33, 5120, 5120), (64, 5120, 4096), (64, 1296, 5120), (7, 5120, 5120), (1, 16, 5120)])
+def test_gated_fp8_of_few_rows_in_two_launches_keeps_all_of_a_sum(B, M, N, K):
+    """The bytes are those of y in fp32, which is summed whole.  (Two products of 2^14 cancel, with smaller ones beside them of which the scaled MFMA would drop up to 2 each.)"""
+    import torch
+    g = gen(M + N)
+    a, w = randn(g, M, K, scale=2.8), randn(g, 2 * N, K, scale=2.8)
+    a[:, 0], a[:, 8], w[:, 0], w[:, 8] = 128.0, -128.0, 128.0, 128.0
+    a[:, 128:] = 0                                # sums of 128 products: fp32 loses 136 2^-23 2^15, 0.6, at most
+    x, W = B.quantize_fp8(a), B.quantize_fp8(w)
+    with B.dry_run() as names:
+        y = B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=torch.float8_e4m3fn)
+    assert names[1] == "quantize" and ("wide" in names[0] or "few rows" in names[0])
+    y = B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=torch.float8_e4m3fn)
+    whole = B.quantize_fp8(B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=torch.float32))
+    assert torch.equal(y.q.view(torch.uint8), whole.q.view(torch.uint8)) and torch.equal(y.scales.contiguous().view(torch.uint8), whole.scales.contiguous().view(torch.uint8))
+    first = lambda r: B.Fp8Rows(r.q[:, :128], r.scales[:1])
+    ref, slack = gated_ref(*product(first(x), first(W), None, True), 0)
+    within_fp8(y, ref, slack)
