@@ -46,25 +46,45 @@ static const ColsTile GATED_WIDE8[] = {{128, 128, 512, 2.f, 5.3f, 1.445f, 2.6f, 
 
 // Few rows: straight from the weights where that is one workgroup a CU.  With y in fp32, whose tiles are slower, with more rows and columns a workgroup too.  (us, these kernels / tiles:
 // 32 x 1280 x 5120 7.7 / 10.6, 32 x 1280 x 1280 4.1 / 5.1, 64 x 1280 x 5120 10.3 / 11.1, but 128 of them 12.9 / 11.2; y in fp32 256 x 1280 x 1280 7.5 / 8.2, 128 of them 5.8 / 8.0; gated 64 x 1280 x 5120 12.8 / 17.1.)
+enum FewRows { FEW_NONE, FEW_16x16, FEW_32x16, FEW_32x32, FEW_64x32 };
+static FewRows few8_choose(bool gated, bool y_f32, int M, int N) {
+    const int64_t r16 = (M + 15) / 16, r32 = (M + 31) / 32, r64 = (M + 63) / 64, c16 = (N + 15) / 16, c32 = (N + 31) / 32;
+    if (r16 * c16 <= 256) return FEW_16x16;
+    if (r32 * c16 <= 256) return FEW_32x16;
+    if (y_f32 && r32 * c32 <= 256) return FEW_32x32;
+    return !gated && y_f32 && r64 * c32 <= 256 ? FEW_64x32 : FEW_NONE;
+}
 template <bool GATED>
 static int launch_few8(const ColsProblem& P, bool& taken, hipStream_t s) {
-    const int64_t r16 = (P.M + 15) / 16, r32 = (P.M + 31) / 32, c16 = (P.N + 15) / 16, c32 = (P.N + 31) / 32;
-    taken = true;
-    if (r16 * c16 <= 256) return launch_few<true, GATED, 1, 1, GATED ? 2 : 4>(P, s);
-    if (r32 * c16 <= 256) return launch_few<true, GATED, 2, 1, GATED ? 2 : 4>(P, s);
-    if (P.y_f32 && r32 * c32 <= 256) return launch_few<true, GATED, 2, 2, GATED ? 2 : 3>(P, s);
-    if constexpr (!GATED)
-        if (P.y_f32 && (P.M + 63) / 64 * c32 <= 256) return launch_few<true, false, 4, 2, 2>(P, s);
-    taken = false;
-    return SD_OK;
+    const FewRows few = few8_choose(GATED, P.y_f32, P.M, P.N);
+    taken = few != FEW_NONE;
+    switch (few) {
+    case FEW_16x16: return launch_few<true, GATED, 1, 1, GATED ? 2 : 4>(P, s);
+    case FEW_32x16: return launch_few<true, GATED, 2, 1, GATED ? 2 : 4>(P, s);
+    case FEW_32x32: return launch_few<true, GATED, 2, 2, GATED ? 2 : 3>(P, s);
+    case FEW_64x32:
+        if constexpr (!GATED) return launch_few<true, false, 4, 2, 2>(P, s);
+    default: return SD_OK;
+    }
 }
 // y in 8 bits by way of fp32, in two launches: where a block's columns lie in several workgroups (few rows, smaller tiles), which a long reduction makes up for.  (us, one launch / two, of which the second
 // is 6, and what the rule adds for it, with its start, 9: 64 x 1280 x 5120 30.2 / 18, 256 of them 32.5 / 22; 64 x 5120 x 1280 11.6 / 13.)
+// Each as it is launched, up to 64 rows widened.  The one launch of these draws the weights through one CU for each 128 columns, the slower the more of them there are (us, one launch as taken and as measured, two as measured: one row 5120 x 1280
+// 12.6 / 11.9, 9.2; 5120 x 2560 20.7 / 20.8, 12.6; 5120 x 5120 36.9 / 35.1, 19.2; 10240 x 5120 43.3 / 40.9, 30.6; 3 rows 15552 x 4144 42.1 / 42.8, 29.4).
+static bool gated8_one_widened(int M, int N) { return M <= 64 && (int64_t)((M + 31) / 32) * ((N + FP8_BLOCK - 1) / FP8_BLOCK) <= 256; }
 static bool gated8_two_launches(int M, int N, int K) {
     float one, two;
-    cols_choose(GATED8_TO_8, M, 2ll * N, K, one);
-    cols_choose(GATED8, M, 2ll * N, K, two);
-    if ((int64_t)((M + 15) / 16) * ((N + 15) / 16) <= 256) two = 3.f + 0.18f * (float)((K + 127) / 128);
+    const float steps = (float)((K + 127) / 128);
+    if (gated8_one_widened(M, N)) one = 4.5f + (0.65f + 0.004f * (float)((N + FP8_BLOCK - 1) / FP8_BLOCK)) * steps;
+    else cols_choose(GATED8_TO_8, M, 2ll * N, K, one);
+    switch (few8_choose(true, true, M, N)) {        // (within 15 % of these kernels at 5 to 40 steps)
+    case FEW_16x16: two = 3.f + 0.18f * steps; break;
+    case FEW_32x16: two = 3.f + 0.24f * steps; break;
+    case FEW_32x32: two = 3.5f + 0.3f * steps; break;
+    default:
+        if (M <= 64) cols_choose(GATED_WIDE8, M, 2ll * N, K, two);
+        else cols_choose(GATED8, M, 2ll * N, K, two);
+    }
     return two + 9.f + (float)M * N * 2e-6f < one;
 }
 static int launch_gated8(ColsProblem& P, bool wide, hipStream_t s) {
@@ -156,7 +176,7 @@ extern "C" int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales
         P.ys = y_scales;
         P.ldys = y_lds;
         // Up to 64 rows, where weights are all that counts, widened operands cost nothing (us, 32 x 256 widened / 64 x 256: one row 5120 x 1280 11.4 / 11.8, 10240 x 2560 21.1 / 21.4, 1280 x 2560 15.7 / 15.1)
-        if (M <= 64 && (int64_t)((M + 31) / 32) * ((N + FP8_BLOCK - 1) / FP8_BLOCK) <= 256) return launch_cols<COLS_FP8_WIDE, 32, 256, 1, 2, 3, true, true, 2>(P, s);
+        if (gated8_one_widened(M, N)) return launch_cols<COLS_FP8_WIDE, 32, 256, 1, 2, 3, true, true, 2>(P, s);
         float us;
         switch (cols_choose(GATED8_TO_8, M, 2ll * N, K, us)) {
         case 0: return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, true, true>(P, s);

@@ -264,3 +264,16 @@ def test_rmsnorm_kernels_are_all_launched(B):
     p = rb"I[^E]*?Li(\d+)ELi(\d+)ELi(\d+)E"
     assert shapes_of(b"rms_fwd_kernel", rb"I.{1,60}?Li(\d+)ELi(\d+)ELi(\d+)E") == short | {(16, 5, 2), (16, 8, 5)} | long
     assert shapes_of(b"rms_bwd_kernel", p) == shapes_of(b"rms_bwd_few_kernel", p) == short | {(64, 1, 0)} | long
+
+
+@pytest.mark.parametrize("M,N,K,first", [(12, 3632, 1760, "few rows 8 bits gated 16x16"), (29, 1328, 1904, "few rows 8 bits gated 16x16"), (17, 2240, 2352, "few rows 8 bits gated 32x16"), (125, 992, 2576, "few rows 8 bits gated 32x16"),
+                                         (2, 5680, 2592, "few rows 8 bits gated 32x32"), (242, 976, 3088, "few rows 8 bits gated 32x32"), (53, 15760, 2272, "gemm cols 8 bits wide gated 64x128"), (3, 15552, 4144, "gemm cols 8 bits wide gated 64x128"),
+                                         (47, 7232, 3008, "gemm cols 8 bits wide gated 64x64"), (1, 5120, 1280, None), (1, 20000, 1280, None), (64, 1296, 640, None), (1, 5120, 128, None)])
+def test_one_launch_or_two_by_what_is_launched(B, M, N, K, first):
+    """Sizes of which two launches take 40 to 95 % of one's time go by way of fp32, and those of which one takes no longer do not"""
+    L, ld = B.lib(), 1 << 20
+    need = L.sd_gated_linear_fp8_workspace_bytes(M, N, K)
+    assert bool(need) == (first is not None)
+    with B.dry_run() as names:
+        assert gat8(L, M=M, N=N, K=K, xl=ld, yl=ld, wl=ld, ws=PE if need else None, n=need) == 0
+    assert (names[0].startswith(first) and names[1] == "quantize") if first else (len(names) == 1 and "to 8 bits 32x256" in names[0])
