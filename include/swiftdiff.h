@@ -52,6 +52,7 @@ extern "C" {
 #define SD_ACT_GELU_TANH 2 /* its tanh form                                           */
 #define SD_ACT_SILU 3      /* z / (1 + exp(-z))                                       */
 #define SD_ACT_RELU 4      /* its slope at 0 is 0                                     */
+#define SD_WHOLE_SUMS 256  /* added to the activation of a layer of 8-bit rows        */
 
 /* One linear projection with an optional rank-r adapter (Section 2, "Low-Rank
  * Adaptation": the patched weight is the base weight plus a rank-r product).
@@ -432,12 +433,15 @@ int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, cons
 
 /* ---- linear_fp8_fwd / gated_linear_fp8_fwd -----------------------------------------------
  * The linear and the gated linear layer of rows in 8 bits (above), for serving: products of e4m3 values with both
- * blocks' scales.  With y in fp32 they are those of bf16, which holds every element, summed in fp32.  Else the matrix core may add eight
- * neighbouring products at a time, of which it drops what is below 2^-13 of the largest, and those sums in fp32: 1.5e-5 of a sum of
- * random terms.
+ * blocks' scales.  With y in fp32, or where SD_WHOLE_SUMS is added to act, they are those of bf16, which holds every element, summed
+ * in fp32.  Else the matrix core may add eight neighbouring products at a time, of which it drops what is below 2^-13 of the largest,
+ * and those sums in fp32: 1.5e-5 of a sum of random terms, for which y in bf16 or 8 bits may be its neighbour.  Whether it does depends
+ * on the sizes (for few rows mostly not), so a row alone and among others may differ in that.  Whole sums of many rows take up to twice
+ * as long.
  *   y = act(x W^T + bias) + residual;       gated: y = (x Wv^T + bv) act(x Wg^T + bg)
  *   x          device [M, K] in 8 bits with x_scales, x_lds;  W device [N, K], gated [2 N, K] (Wv first), with w_scales, w_lds
  *   bias       device [N] or [2 N] bf16, or NULL;  residual device [M, N] of y_dtype, or NULL; may alias y
+ *   act        SD_ACT_*, or the sum of it and SD_WHOLE_SUMS
  *   y          device [M, N] of y_dtype: bf16, fp32, or, gated, SD_FP8 with y_scales, y_lds, for the next product; aliases no input
  *              but the residual
  * K is a multiple of 16 below 2^22, M below 2^27, N below 2^22, gated a multiple of 16 below 2^21, and M / 64 times the

@@ -6,6 +6,7 @@
 //
 // Measured: 8192 x 4096 x 4096 bf16 out 119 us (2.3 PFLOP/s; the library's 102), 8192 x 5120 x 1280 67.6 (1.6; the library's 72); gated with SiLU, 8192 x 5120 x 1280, 101 to bf16, 102 to 8 bits (2.1; the library's
 // product alone 107), of which the main loops take 79.  1976 x 1280 x 5120 onto fp32 32.2.  One row, 5120 x 1280 gated to 8 bits 11.0 to 11.3, 1280 x 5120 onto fp32 6.5.
+// With sums asked for whole (widened operands): 8192 x 5120 x 1280 106 to bf16, gated 194 to bf16, 207 to 8 bits; 1976 x 1280 x 5120 to bf16 31 for 25.
 #include "gemm_cols.hpp"
 
 #include <string.h>
@@ -44,19 +45,22 @@ static const ColsTile WIDE8[] = {{128, 256, 256, 0.f, 13.3f, 1.243f, 13.3f, 1.24
 static const ColsTile GATED_WIDE8[] = {{128, 128, 512, 2.f, 5.3f, 1.445f, 2.6f, 1.027f}, {128, 128, 256, 0.3f, 5.1f, 0.722f, 5.1f, 0.722f}, {64, 128, 512, 2.3f, 3.4f, 0.875f, 2.2f, 0.503f},
                                        {64, 64, 512, 2.5f, 2.7f, 0.514f, 1.6f, 0.323f}};
 
-// Few rows: straight from the weights where that is one workgroup a CU.  With y in fp32, whose tiles are slower, with more rows and columns a workgroup too.  (us, these kernels / tiles:
+// y in 8 bits of sums that the caller wants whole.  (6 % off 240 launches of 65 to 8192 rows in the mean, and the fastest of these each time.)
+static const ColsTile GATED_WIDE8_TO_8[] = {{128, 256, 256, 0.f, 6.4f, 1.29f, 6.4f, 1.29f}, {64, 256, 256, 0.4f, 5.1f, 0.745f, 5.1f, 0.745f}, {32, 256, 256, 0.8f, 3.9f, 0.575f, 3.9f, 0.575f}};
+
+// Few rows: straight from the weights where that is one workgroup a CU.  With widened operands, whose tiles are slower, with more rows and columns a workgroup too.  (us, these kernels / tiles:
 // 32 x 1280 x 5120 7.7 / 10.6, 32 x 1280 x 1280 4.1 / 5.1, 64 x 1280 x 5120 10.3 / 11.1, but 128 of them 12.9 / 11.2; y in fp32 256 x 1280 x 1280 7.5 / 8.2, 128 of them 5.8 / 8.0; gated 64 x 1280 x 5120 12.8 / 17.1.)
 enum FewRows { FEW_NONE, FEW_16x16, FEW_32x16, FEW_32x32, FEW_64x32 };
-static FewRows few8_choose(bool gated, bool y_f32, int M, int N) {
+static FewRows few8_choose(bool gated, bool wide, int M, int N) {
     const int64_t r16 = (M + 15) / 16, r32 = (M + 31) / 32, r64 = (M + 63) / 64, c16 = (N + 15) / 16, c32 = (N + 31) / 32;
     if (r16 * c16 <= 256) return FEW_16x16;
     if (r32 * c16 <= 256) return FEW_32x16;
-    if (y_f32 && r32 * c32 <= 256) return FEW_32x32;
-    return !gated && y_f32 && r64 * c32 <= 256 ? FEW_64x32 : FEW_NONE;
+    if (wide && r32 * c32 <= 256) return FEW_32x32;
+    return !gated && wide && r64 * c32 <= 256 ? FEW_64x32 : FEW_NONE;
 }
 template <bool GATED>
-static int launch_few8(const ColsProblem& P, bool& taken, hipStream_t s) {
-    const FewRows few = few8_choose(GATED, P.y_f32, P.M, P.N);
+static int launch_few8(const ColsProblem& P, bool wide, bool& taken, hipStream_t s) {
+    const FewRows few = few8_choose(GATED, wide, P.M, P.N);
     taken = few != FEW_NONE;
     switch (few) {
     case FEW_16x16: return launch_few<true, GATED, 1, 1, GATED ? 2 : 4>(P, s);
@@ -112,6 +116,8 @@ using namespace sd;
 
 extern "C" int sd_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int64_t x_lds, const uint8_t* W, const uint8_t* w_scales, int64_t w_lds, const uint16_t* bias, int32_t act, const void* residual,
                                  void* y, int32_t y_dtype, int32_t M, int32_t N, int32_t K, void* stream) {
+    const bool wide = y_dtype == SD_F32 || (act & SD_WHOLE_SUMS);
+    act &= ~SD_WHOLE_SUMS;
     const int rc = linear8_check("linear_fp8_fwd", x, x_scales, x_lds, W, w_scales, w_lds, act, M, N, N, K);
     if (rc) return rc;
     SD_REQUIRE(y_dtype == SD_BF16 || y_dtype == SD_F32, SD_EINVAL, "linear_fp8_fwd: y_dtype=%d", y_dtype);
@@ -124,10 +130,10 @@ extern "C" int sd_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int6
     P.y_f32 = y_dtype == SD_F32;
     hipStream_t s = static_cast<hipStream_t>(stream);
     bool taken;
-    const int few = launch_few8<false>(P, taken, s);
+    const int few = launch_few8<false>(P, wide, taken, s);
     if (taken) return few;
     float us;
-    if (P.y_f32)
+    if (wide)
         switch (cols_choose(WIDE8, M, N, K, us)) {
         case 0: return launch_cols<COLS_FP8_WIDE, 128, 256, 2, 4, 3, false, false>(P, s);
         case 1: return launch_cols<COLS_FP8_WIDE, 128, 192, 4, 2, 3, false, false>(P, s);
@@ -154,6 +160,8 @@ extern "C" size_t sd_gated_linear_fp8_workspace_bytes(int32_t M, int32_t N, int3
 
 extern "C" int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales, int64_t x_lds, const uint8_t* W, const uint8_t* w_scales, int64_t w_lds, const uint16_t* bias, int32_t act,
                                        void* y, int32_t y_dtype, uint8_t* y_scales, int64_t y_lds, int32_t M, int32_t N, int32_t K, void* ws, size_t ws_bytes, void* stream) {
+    const bool whole = (act & SD_WHOLE_SUMS) != 0;
+    act &= ~SD_WHOLE_SUMS;
     int rc = linear8_check("gated_linear_fp8_fwd", x, x_scales, x_lds, W, w_scales, w_lds, act, M, N, 2ll * N, K);
     if (rc) return rc;
     SD_REQUIRE(y_dtype == SD_BF16 || y_dtype == SD_F32 || y_dtype == SD_FP8, SD_EINVAL, "gated_linear_fp8_fwd: y_dtype=%d", y_dtype);
@@ -178,6 +186,12 @@ extern "C" int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales
         // Up to 64 rows, where weights are all that counts, widened operands cost nothing (us, 32 x 256 widened / 64 x 256: one row 5120 x 1280 11.4 / 11.8, 10240 x 2560 21.1 / 21.4, 1280 x 2560 15.7 / 15.1)
         if (gated8_one_widened(M, N)) return launch_cols<COLS_FP8_WIDE, 32, 256, 1, 2, 3, true, true, 2>(P, s);
         float us;
+        if (whole)
+            switch (cols_choose(GATED_WIDE8_TO_8, M, 2ll * N, K, us)) {
+            case 0: return launch_cols<COLS_FP8_WIDE, 128, 256, 4, 2, 3, true, true>(P, s);
+            case 1: return launch_cols<COLS_FP8_WIDE, 64, 256, 2, 2, 3, true, true, 2>(P, s);
+            default: return launch_cols<COLS_FP8_WIDE, 32, 256, 1, 2, 3, true, true, 2>(P, s);
+            }
         switch (cols_choose(GATED8_TO_8, M, 2ll * N, K, us)) {
         case 0: return launch_cols<COLS_FP8, 256, 256, 4, 2, 2, true, true>(P, s);
         case 1: return launch_cols<COLS_FP8, 128, 256, 4, 2, 3, true, true>(P, s);
@@ -190,8 +204,9 @@ extern "C" int sd_gated_linear_fp8_fwd(const uint8_t* x, const uint8_t* x_scales
         P.y = ws;
         P.y_f32 = 1;
     }
-    rc = launch_few8<true>(P, taken, s);
+    const bool wide = y_dtype == SD_F32 || whole || (out8 && M <= 64);
+    rc = launch_few8<true>(P, y_dtype == SD_F32 || whole || out8, taken, s);
     // (to 8 bits widened up to 64 rows, as in one launch.  us, both launches, widened / not: one row 10240 x 5120 30.6 / 27.0, 5120 x 5120 19.9 / 18.7, 64 rows of them 36.1 / 36.2 and 22.3 / 21.5)
-    if (!taken) rc = launch_gated8(P, y_dtype == SD_F32 || (out8 && M <= 64), s);
+    if (!taken) rc = launch_gated8(P, wide, s);
     return rc || !out8 ? rc : launch_quantize(ws, true, static_cast<uint8_t*>(y), y_scales, y_lds, M, N, s);
 }

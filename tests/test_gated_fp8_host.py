@@ -277,3 +277,18 @@ def test_one_launch_or_two_by_what_is_launched(B, M, N, K, first):
     with B.dry_run() as names:
         assert gat8(L, M=M, N=N, K=K, xl=ld, yl=ld, wl=ld, ws=PE if need else None, n=need) == 0
     assert (names[0].startswith(first) and names[1] == "quantize") if first else (len(names) == 1 and "to 8 bits 32x256" in names[0])
+
+
+def test_whole_sums_are_widened(B):
+    """SD_WHOLE_SUMS beside any activation: widened operands at every size and type of y, in the workspace that the query asks for"""
+    import random
+    L, rng, ld = B.lib(), random.Random(5), 1 << 20
+    for f, yt in ((lin8, 0), (lin8, 1), (gat8, 0), (gat8, 1), (gat8, 2)):
+        assert f(L, act=B.SD_WHOLE_SUMS + 5) == EINVAL and f(L, act=2 * B.SD_WHOLE_SUMS) == EINVAL and f(L, act=B.SD_WHOLE_SUMS - 1) == EINVAL and f(L, act=-1) == EINVAL
+        for i in range(200):
+            M, N, K = int(2 ** rng.uniform(0, 14)), 16 * int(2 ** rng.uniform(0, 8)), 16 * int(2 ** rng.uniform(0, 9))
+            kw = dict(yl=ld, ys=PD, ws=PE, n=L.sd_gated_linear_fp8_workspace_bytes(M, N, K)) if f is gat8 else {}
+            with B.dry_run() as names:
+                assert f(L, M=M, N=N, K=K, xl=ld, wl=ld, yt=yt, act=B.SD_WHOLE_SUMS + i % 5, **kw) == 0
+            assert "wide" in names[0] or "few rows" in names[0]
+            assert names[1:] == (["quantize"] if kw.get("n") and yt == 2 else [])

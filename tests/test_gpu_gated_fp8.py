@@ -1000,3 +1000,67 @@ def test_gated_fp8_of_few_rows_in_two_launches_keeps_all_of_a_sum(B, M, N, K):
     first = lambda r: B.Fp8Rows(r.q[:, :128], r.scales[:1])
     ref, slack = gated_ref(*product(first(x), first(W), None, True), 0)
     within_fp8(y, ref, slack)
+
+
+def drops_low_bits(B, g, M, N, K):
+    """Rows whose sums of products hold two of 2^14 that cancel, and beside them, in the same eights, smaller ones, of which the scaled MFMA drops up to 2 each"""
+    a, w = randn(g, M, K, scale=2.8), randn(g, N, K, scale=2.8)
+    a[:, 0], a[:, 8], w[:, 0], w[:, 8] = 128.0, -128.0, 128.0, 128.0
+    return B.quantize_fp8(a), B.quantize_fp8(w)
+
+
+@pytest.mark.parametrize("M,N,K", [(65, 65, 64), (300, 515, 80), (700, 333, 128), (2100, 640, 64), (8200, 1040, 80)])
+def test_linear_fp8_whole_sums(B, M, N, K):
+    import torch
+    g = gen(M + N)
+    x, W = drops_low_bits(B, g, M, N, K)
+    bias, res = randn(g, N, scale=0.5).bfloat16(), randn(g, M, N, dtype=torch.bfloat16)
+    z, ez = product(x, W, bias, True)
+    y = B.linear_fp8_fwd(x, W, bias, residual=res, whole_sums=True)
+    within(y, z + res.double(), ez + 2 * U * (z + res.double()).abs())
+    assert torch.equal(y, B.linear_fp8_fwd(x, W, bias, residual=res, whole_sums=True))
+    # y in fp32 is summed whole whether it is asked for or not
+    assert torch.equal(B.linear_fp8_fwd(x, W, bias, 3, out_dtype=torch.float32, whole_sums=True), B.linear_fp8_fwd(x, W, bias, 3, out_dtype=torch.float32))
+
+
+WHOLE_KERNELS = [(65, 144, 64, "gemm cols 8 bits wide gated to 8 bits 32x256/4 waves/3 stages guard"), (300, 1296, 128, "gemm cols 8 bits wide gated to 8 bits 32x256/4 waves/3 stages"),
+                 (1500, 2560, 128, "gemm cols 8 bits wide gated to 8 bits 128x256/8 waves/3 stages"), (8200, 1040, 80, "gemm cols 8 bits wide gated to 8 bits 128x256/8 waves/3 stages guard"),
+                 (500, 2064, 128, "gemm cols 8 bits wide gated to 8 bits 64x256/8 waves/3 stages"), (500, 2064, 112, "gemm cols 8 bits wide gated to 8 bits 64x256/8 waves/3 stages guard"), (64, 32896, 128, "gemm cols 8 bits wide gated to 8 bits 64x256/8 waves/3 stages")]
+
+
+@pytest.mark.parametrize("M,N,K,kernel", WHOLE_KERNELS)
+def test_gated_fp8_whole_sums(B, M, N, K, kernel):
+    import torch
+    g = gen(M + N)
+    x, W = drops_low_bits(B, g, M, 2 * N, K)
+    bias = randn(g, 2 * N, scale=0.5).bfloat16()
+    for act in (0, 4):
+        ref, slack = gated_ref(*product(x, W, bias, True), act)
+        with B.dry_run() as names:
+            B.gated_linear_fp8_fwd(x, W, bias, act, out_dtype=torch.float8_e4m3fn, whole_sums=True)
+        assert names == [kernel]
+        within_fp8(B.gated_linear_fp8_fwd(x, W, bias, act, out_dtype=torch.float8_e4m3fn, whole_sums=True), ref, slack)
+        within(B.gated_linear_fp8_fwd(x, W, bias, act, whole_sums=True), ref, slack)
+        within(B.gated_linear_fp8_fwd(x, W, bias, act, out_dtype=torch.float32, whole_sums=True), ref, slack)
+
+
+@pytest.mark.parametrize("M,N,K", [(130, 640, 4112), (300, 1296, 5120)])
+def test_gated_fp8_whole_sums_in_two_launches(B, M, N, K):
+    import torch
+    g = gen(M)
+    x, W = rows8(B, g, M, K), rows8(B, g, 2 * N, K, 1.3 / math.sqrt(K), 0.3)
+    y = B.gated_linear_fp8_fwd(x, W, None, 3, out_dtype=torch.float8_e4m3fn, whole_sums=True)
+    want = B.quantize_fp8(B.gated_linear_fp8_fwd(x, W, None, 3, out_dtype=torch.float32))
+    assert torch.equal(y.q.view(torch.uint8), want.q.view(torch.uint8)) and torch.equal(y.scales.contiguous().view(torch.uint8), want.scales.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("M,N,K", [(1500, 2560, 1296), (500, 2064, 272), (300, 1296, 640)])
+def test_gated_fp8_whole_sums_of_usual_rows(B, M, N, K):
+    """Steps, stages and scales of the kernels that only whole sums take"""
+    import torch
+    g = gen(K)
+    x, W = rows8(B, g, M, K), rows8(B, g, 2 * N, K, 1.3 / math.sqrt(K), 0.3)
+    bias = randn(g, 2 * N, scale=0.5).bfloat16()
+    for act in (1, 3):
+        ref, slack = gated_ref(*product(x, W, bias, True), act)
+        within_fp8(B.gated_linear_fp8_fwd(x, W, bias, act, out_dtype=torch.float8_e4m3fn, whole_sums=True), ref, slack)
