@@ -324,6 +324,8 @@ int sd_layernorm_bwd(const void* dy, int32_t y_dtype, const void* x, int32_t x_d
  * an element stands for q 2^(s - 127).  s is the least with amax <= 448 * 2^(s - 127), amax the largest magnitude
  * of the block's finite elements, and at least 1; q is the element times 2^(127 - s), which is exact, rounded to nearest, ties to
  * even.  A NaN or an infinity becomes NaN, and its block's other elements are as they would be without it.
+ * Products take any rows of that form, whatever their scales: s = 255 makes its block NaN, and elements of 2^128 and more may count as infinities
+ * (s up to 246 makes none; quantize_fp8 makes 2^128 of numbers from 1.9375 * 2^127 on).
  * The scales of a matrix of M rows of K elements lie block by block: s of row m and block b is scales[b * lds + m], lds a
  * multiple of 4, at least M (device, (ceil(K / 128) - 1) * lds + M rounded up to a multiple of 4 bytes; of what lies behind a block's M
  * at most three bytes are read, whose values do not matter, and nothing is written).  Rows are K bytes, K a multiple of 16 below 2^22; M below 2^27.
@@ -433,9 +435,9 @@ int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, cons
 
 /* ---- linear_fp8_fwd / gated_linear_fp8_fwd -----------------------------------------------
  * The linear and the gated linear layer of rows in 8 bits (above), for serving: products of e4m3 values with both
- * blocks' scales.  With y in fp32, or where SD_WHOLE_SUMS is added to act, they are those of bf16, which holds every element, summed
- * in fp32.  Else the matrix core may add eight neighbouring products at a time, of which it drops what is below 2^-13 of the largest,
- * and those sums in fp32: 1.5e-5 of a sum of random terms, for which y in bf16 or 8 bits may be its neighbour.  Whether it does depends
+ * blocks' scales.  With y in fp32, or where SD_WHOLE_SUMS is added to act, they are those of bf16, which holds every element (those below
+ * 2^-126 as multiples of 2^-133), summed in fp32.  Else the matrix core may add eight neighbouring products at a time, of which it
+ * drops what is below 2^-13 of the largest, and those sums in fp32: 1.5e-5 of a sum of random terms, for which y in bf16 or 8 bits may be its neighbour.  Whether it does depends
  * on the sizes (for few rows mostly not), so a row alone and among others may differ in that.  Whole sums of many rows take up to twice
  * as long.
  *   y = act(x W^T + bias) + residual;       gated: y = (x Wv^T + bv) act(x Wg^T + bg)

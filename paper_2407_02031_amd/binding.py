@@ -568,7 +568,8 @@ def linear_bwd(dy: torch.Tensor, x: torch.Tensor, W: torch.Tensor, z=None, act: 
 
 class Fp8Rows(NamedTuple):
     """Rows in 8 bits: values q [M, K] (torch.float8_e4m3fn) and scales [ceil(K / 128), M] (torch.float8_e8m0fnu), one for every 128 elements of a row.  Element
-    [m, k] stands for q[m, k] * scales[k // 128, m].  The scales of a block are dense, and blocks a multiple of 4 apart (so a view [:, :M], where M is none)."""
+    [m, k] stands for q[m, k] * scales[k // 128, m].  The scales of a block are dense, and blocks a multiple of 4 apart (so a view [:, :M], where M is none).  Elements of
+    2^128 and more may count as infinities, and those below 2^-126 as the nearest multiple of 2^-133."""
     q: torch.Tensor
     scales: torch.Tensor
 

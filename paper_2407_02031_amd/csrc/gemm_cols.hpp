@@ -54,7 +54,8 @@ __device__ __forceinline__ void dma4(const void* gptr, uint32_t lds_base) {
 // What the operands are, and how they are multiplied.  The scaled MFMA takes 128 of 8 bits in the time of 64 of bf16, but it adds products eight at a time, and of those eight it keeps what is worth 2^-13 of
 // the largest and more (measured: with one of 2^16, another of 2^2 is gone; in another eight, and of the sums of eights, nothing is): off by 1.5e-5 of a sum of random terms, where
 // 8 bits were off by 2^-5 in each.  That is far below the rounding of y to bf16 or to 8 bits, but not of y in fp32: there, where the caller asks for whole sums, and where the rows are few
-// and the operands' bytes all that counts, they are widened to bf16, exactly and with their scales, and multiplied as those.
+// and the operands' bytes all that counts, they are widened to bf16, with their scales and exactly (elements from 2^-126 to below 2^128;
+// smaller ones to multiples of 2^-133, larger ones to infinities, which the scaled MFMA would multiply), and multiplied as those.
 enum ColsMode { COLS_BF16, COLS_FP8, COLS_FP8_WIDE };
 
 // Eight e4m3 elements times 2^(s - 127), s a byte, which is what the conversion looks at of an fp32 scale

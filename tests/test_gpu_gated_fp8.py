@@ -1064,3 +1064,137 @@ def test_gated_fp8_whole_sums_of_usual_rows(B, M, N, K):
     for act in (1, 3):
         ref, slack = gated_ref(*product(x, W, bias, True), act)
         within_fp8(B.gated_linear_fp8_fwd(x, W, bias, act, out_dtype=torch.float8_e4m3fn, whole_sums=True), ref, slack)
+
+
+# ---- scales, NaN and the largest values in every kernel ------------------------------------------------------------------------
+def with_rows(r, bytes_, q=None):
+    """Rows in 8 bits with other scale bytes (and values)"""
+    import torch
+    M = r.q.shape[0]
+    return B_rows(r.q if q is None else q, torch.nn.functional.pad(bytes_.to(torch.uint8), (0, -M % 4)).view(torch.float8_e8m0fnu)[:, :M])
+
+
+def B_rows(q, s):
+    from paper_2407_02031_amd import binding
+    return binding.Fp8Rows(q, s)
+
+
+def bytes_of(r):
+    import torch
+    return r.scales.contiguous().view(torch.uint8).int()
+
+
+def spoiled(r, at):
+    """A NaN among the scales of row at[0], and one among the values of row at[1]; +-448 everywhere in row at[2].  The rows that are NaN for it."""
+    import torch
+    s, q, bad = bytes_of(r), r.q.view(torch.uint8).clone(), torch.zeros(r.q.shape[0], dtype=torch.bool, device="cuda")
+    K = q.shape[1]
+    if len(at) > 0:
+        s[-1, at[0]], bad[at[0]] = 255, True
+    if len(at) > 1:
+        q[at[1], K // 2], bad[at[1]] = 0x7f, True
+    if len(at) > 2:
+        q[at[2]] = 0x7e + 128 * (torch.arange(K, device="cuda") % 3 == 0).to(torch.uint8)
+    return with_rows(r, s, q.view(torch.float8_e4m3fn)), bad
+
+
+def at_the_end(r, at, high, shift):
+    """Rows `at` with scale byte 254 and values +-1, or byte 0 and their values; the others' scales by 2^shift"""
+    import torch
+    s, q = (bytes_of(r) + shift).clamp(1, 250), r.q.view(torch.uint8).clone()
+    for i in at:
+        s[:, i] = 254 if high else 0
+        if high:
+            q[i] = 0x38 + (q[i] & 128)
+    return with_rows(r, s, q.view(torch.float8_e4m3fn))
+
+
+def check_ends(B, M, N, K, yt, gated, **kw):
+    import torch
+    g = gen(M + N + K + 1)
+    x, W = rows8(B, g, M, K, 1.0, 2.0), rows8(B, g, 2 * N if gated else N, K, 1.3 / math.sqrt(K), 2.0)
+    R = W.q.shape[0]
+    some = lambda n: [i for i in sorted({n // 3, n // 2 + 1, n - 1, n // 5}) if 0 < i < n][:3]      # (row 0 is left alone)
+
+    def check(x, W, bx, bw, lost=None):
+        if gated:
+            y = B.gated_linear_fp8_fwd(x, W, None, 0, out_dtype=yt, **kw)
+            bw = bw[:N] | bw[N:]
+        else:
+            y = B.linear_fp8_fwd(x, W, out_dtype=yt, **kw)
+        bad = bx[:, None] | bw[None, :]
+        clean = lambda r: B_rows(torch.where(r.q.double().isnan(), 0.0, r.q.float()).to(torch.float8_e4m3fn), torch.where(r.scales.double().isnan(), 1.0, r.scales.float()).to(torch.float8_e8m0fnu))
+        z, ez = product(clean(x), clean(W), None, yt == torch.float32 or kw.get("whole_sums", False))
+        if lost is not None:
+            ez = ez + lost
+        ref, slack = gated_ref(z, ez, 0) if gated else (z, ez)
+        over = ref.abs() + slack >= 2.0 ** 127        # (a product of value and gate near 2^128 and beyond: infinite, or its neighbour)
+        assert int(over.sum()) <= 1e-4 * over.numel()
+        if yt == torch.float8_e4m3fn:
+            bad = bad | over
+            assert torch.equal(y.q.double().isnan() | over, bad)
+            ref, slack = torch.where(bad, 0.0, ref), torch.where(bad, 0.0, slack)
+            within_fp8(B_rows(torch.where(bad, 0.0, y.q.float()).to(torch.float8_e4m3fn), y.scales), ref, slack)
+        else:
+            assert torch.equal(y.isnan(), bad)
+            bad = bad | over
+            within(torch.where(bad, 0.0, y), torch.where(bad, 0.0, ref), torch.where(bad, 0.0, slack))
+    nx, nw = torch.zeros(M, dtype=torch.bool, device="cuda"), torch.zeros(R, dtype=torch.bool, device="cuda")
+    check(*(p for a in zip(spoiled(x, some(M)), spoiled(W, some(R))) for p in a))
+    for mine, other, first in ((x, W, True), (W, x, False)):
+        at = some(mine.q.shape[0])
+        for high, up, down in ((True, 50, -80), (False, -60, 100)):
+            a, b = at_the_end(mine, at, high, up), at_the_end(other, [], False, down)
+            # elements below 2^-126, of which bf16 holds multiples of 2^-133: off by 2^-134 at most
+            lost = 2.0 ** -134 * values(b).abs().sum(1)
+            if first:
+                check(a, b, nx, nw, lost[None, :])
+            else:
+                check(b, a, nx, nw, lost[:, None])
+
+
+@pytest.mark.parametrize("yt,M,N,K,kernel", LIN8_KERNELS + [("bfloat16", 700, 700, 256, "gemm cols 8 bits 64x64/4 waves/4 stages"), ("bfloat16", 2100, 640, 272, "gemm cols 8 bits 64x128/4 waves/3 stages guard")])
+def test_linear_fp8_ends_in_every_kernel(B, yt, M, N, K, kernel):
+    """NaN scales and values stay in their rows and columns; +-448 throughout; scale bytes 254 and 0; scales far apart in both operands"""
+    import torch
+    with B.dry_run() as names:
+        B.linear_fp8_fwd(*(B.Fp8Rows(torch.empty(n, K, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((K + 127) // 128, (n + 3) // 4 * 4, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)[:, :n]) for n in (M, N)),
+                         out_dtype=getattr(torch, yt))
+    assert names == [kernel]
+    check_ends(B, M, N, K, getattr(torch, yt), False)
+
+
+@pytest.mark.parametrize("yt,M,N,K", [k[:4] for k in GATED8_KERNELS] + [("float8_e4m3fn", 130, 640, 4112)])
+def test_gated_fp8_ends_in_every_kernel(B, yt, M, N, K):
+    import torch
+    check_ends(B, M, N, K, getattr(torch, yt), True)
+
+
+@pytest.mark.parametrize("M,N,K", [k[:3] for k in WHOLE_KERNELS] + [(700, 336, 640)])
+def test_whole_sums_ends_in_every_kernel(B, M, N, K):
+    import torch
+    check_ends(B, M, N, K, torch.float8_e4m3fn, True, whole_sums=True)
+    check_ends(B, M, N, K, torch.bfloat16, True, whole_sums=True)
+    check_ends(B, M, N, K, torch.bfloat16, False, whole_sums=True)
+
+
+@pytest.mark.parametrize("M,N,kernel", [(256, 32, "few rows 8 bits 16x16"), (2100, 640, "gemm cols 8 bits wide 64x128/8 waves/3 stages")])
+def test_widened_elements_are_those_of_bf16(B, M, N, kernel):
+    """One element a product, of every scale byte up to 246: exact from 2^-126 on, the nearest multiple of 2^-133 below"""
+    import torch
+    K = 128
+    q = torch.tensor([1, 2, 3, 7, 8, 9, 15, 16, 31, 48, 55, 56, 63, 64, 88, 112, 126, 0x81, 0x87, 0xb8, 0xfe], dtype=torch.uint8, device="cuda")[torch.arange(K, device="cuda") % 21].expand(M, K).contiguous()
+    s = (torch.arange(M, device="cuda") % 247)[None]
+    x = with_rows(B_rows(q.view(torch.float8_e4m3fn), None), s)
+    w = torch.zeros(N, K, dtype=torch.uint8, device="cuda")
+    w[torch.arange(N), torch.arange(N) % K] = 0x38
+    held = (q.view(torch.float8_e4m3fn).double() * power(s[0] - 127)[:, None]).bfloat16().double()[:, torch.arange(N) % K]
+    for t in (127 - 100, 127, 127 + 100):
+        W = with_rows(B_rows(w.view(torch.float8_e4m3fn), None), torch.full((1, N), t, device="cuda"))
+        with B.dry_run() as names:
+            B.linear_fp8_fwd(x, W, out_dtype=torch.float32)
+        assert names == [kernel]
+        want = (held * 2.0 ** (t - 127)).float()
+        y = B.linear_fp8_fwd(x, W, out_dtype=torch.float32)
+        keep = (want.abs() >= 2.0 ** -126) & want.isfinite() | (want == 0)          # (results of less are the matrix core's to round)
+        assert torch.equal(y[keep], want[keep]) and bool((y[~want.isfinite()].isinf()).all())
