@@ -437,9 +437,9 @@ int sd_gated_linear_bwd(const void* dy, int32_t y_dtype, const uint16_t* x, cons
  * The linear and the gated linear layer of rows in 8 bits (above), for serving: products of e4m3 values with both
  * blocks' scales.  With y in fp32, or where SD_WHOLE_SUMS is added to act, they are those of bf16, which holds every element (those below
  * 2^-126 as multiples of 2^-133), summed in fp32.  Else the matrix core may add eight neighbouring products at a time, of which it
- * drops what is below 2^-13 of the largest, and those sums in fp32: 1.5e-5 of a sum of random terms, for which y in bf16 or 8 bits may be its neighbour.  Whether it does depends
- * on the sizes (for few rows mostly not), so a row alone and among others may differ in that.  Whole sums of many rows take up to twice
- * as long.
+ * drops what is below 2^-13 of the largest, and those sums in fp32: 1.5e-5 of a sum of random terms, for which y in bf16 or 8 bits may be
+ * its neighbour.  Whether it does depends on the sizes (for few rows mostly not), so a row alone and among others may differ in that.
+ * Whole sums of many rows take up to twice as long.
  *   y = act(x W^T + bias) + residual;       gated: y = (x Wv^T + bv) act(x Wg^T + bg)
  *   x          device [M, K] in 8 bits with x_scales, x_lds;  W device [N, K], gated [2 N, K] (Wv first), with w_scales, w_lds
  *   bias       device [N] or [2 N] bf16, or NULL;  residual device [M, N] of y_dtype, or NULL; may alias y

@@ -1198,3 +1198,69 @@ def test_widened_elements_are_those_of_bf16(B, M, N, kernel):
         y = B.linear_fp8_fwd(x, W, out_dtype=torch.float32)
         keep = (want.abs() >= 2.0 ** -126) & want.isfinite() | (want == 0)          # (results of less are the matrix core's to round)
         assert torch.equal(y[keep], want[keep]) and bool((y[~want.isfinite()].isinf()).all())
+
+
+# ---- NaN and infinities on the way into 8 bits -----------------------------------------------------------------------------------
+def same_but_nan(got, clean, bad):
+    """Rows in 8 bits that are NaN in columns `bad` and, scales included, those of `clean` elsewhere"""
+    import torch
+    assert torch.equal(got.scales.contiguous().view(torch.uint8), clean.scales.contiguous().view(torch.uint8))
+    assert got.q[:, bad].double().isnan().all()
+    assert torch.equal(got.q[:, ~bad].contiguous().view(torch.uint8), clean.q[:, ~bad].contiguous().view(torch.uint8)) and not clean.q.double().isnan().any()
+
+
+@pytest.mark.parametrize("M,N,K,whole,kernel", [
+    (5, 528, 256, False, "wide gated to 8 bits 32x256"), (100, 528, 256, False, "gated to 8 bits 64x256"), (9309, 528, 144, False, "gated to 8 bits 256x256"), (4200, 528, 256, False, "gated to 8 bits 128x256"), (8200, 1040, 144, False, "gated to 8 bits 256x256"),
+    (300, 528, 144, True, "wide gated to 8 bits 32x256"), (1900, 528, 144, True, "wide gated to 8 bits 64x256"), (3800, 528, 256, True, "wide gated to 8 bits 128x256"), (130, 528, 4112, False, "quantize"), (5, 528, 5120, False, "quantize")])
+def test_gated_fp8_bias_that_is_not_finite(B, M, N, K, whole, kernel):
+    """Columns whose bias, the value's or the gate's, is NaN or infinite, in either half of a block, some of a block and all of it: NaN, and the others' bytes and scales are those of a call where these columns are zero"""
+    import torch
+    g = gen(M)
+    columns = [0, 5, 62, 64, 101, 127] + [128 + 17] + [256 + 70] + list(range(384, 512)) + [N - 1, N - 16]
+    bad = torch.zeros(N, dtype=torch.bool, device="cuda")
+    bad[columns] = True
+    w = randn(g, 2 * N, K, scale=1.3 / math.sqrt(K))
+    w[:N][bad] = 0
+    x, W, bias = B.quantize_fp8(randn(g, M, K)), B.quantize_fp8(w), randn(g, 2 * N, scale=0.5).bfloat16()
+    bias[:N][bad] = 0
+    run = lambda b, act: B.gated_linear_fp8_fwd(x, W, b, act, out_dtype=torch.float8_e4m3fn, whole_sums=whole)
+    with B.dry_run() as names:
+        run(bias, 0)
+    assert kernel in names[-1]
+    for act in (0, 3, 1):
+        clean = run(bias, act)
+        for values_of, gate_of in (((math.inf,), ()), ((-math.inf,), ()), ((math.nan,), ()), ((), (math.nan,)), ((), (math.inf,)), ((math.nan, math.inf, -math.inf), (math.nan, math.inf))):
+            b = bias.clone()
+            for i, c in enumerate(columns):
+                if values_of and (i % 2 == 0 or not gate_of):
+                    b[c] = values_of[i % len(values_of)]
+                else:
+                    b[N + c] = gate_of[i % len(gate_of)]
+            same_but_nan(run(b, act), clean, bad)
+
+
+@pytest.mark.parametrize("C", [16, 64, 128, 320, 512, 768, 1280, 2048, 4096, 8192, 16384])
+def test_rmsnorm_to_8_bits_of_what_is_not_finite(B, C):
+    """A weight that is NaN or infinite: its column is NaN, and the others' bytes and scales are those of a weight of zero there; a row that holds a NaN is NaN, with the least scale"""
+    import torch
+    for xt, rt in (("bfloat16", "float32"), ("float32", None)):
+        for M in (1, 37):
+            x, r, ga, g = rms_inputs(M, C, xt, rt, C + M)
+            columns = sorted({0, 3, min(C - 1, 70), C // 2 + 1, C - 1} | (set(range(128, 256)) if C > 256 else set()))
+            bad = torch.zeros(C, dtype=torch.bool, device="cuda")
+            bad[columns] = True
+            run = lambda w, x=x: (lambda o: o[0] if r is not None else o)(B.rmsnorm_fwd(x, w, residual=r, out_dtype=torch.float8_e4m3fn))
+            zero = ga.clone()
+            zero[bad] = 0
+            clean = run(zero)
+            for what in ((math.inf,), (math.nan,), (-math.inf, math.nan, math.inf)):
+                w = zero.clone()
+                for i, c in enumerate(columns):
+                    w[c] = what[i % len(what)]
+                same_but_nan(run(w), clean, bad)
+            spoiled_x = x.clone()
+            spoiled_x[M // 2, C // 3] = math.nan
+            got, whole = run(ga, spoiled_x), run(ga)
+            rows = torch.arange(M, device="cuda") != M // 2
+            assert got.q[M // 2].double().isnan().all() and (got.scales.contiguous().view(torch.uint8)[:, M // 2] == 1).all()
+            assert torch.equal(got.q.view(torch.uint8)[rows], whole.q.view(torch.uint8)[rows])
