@@ -14,6 +14,7 @@
 //     long reductions (gated in bf16, 512 x 640 x 2560 14.4 -> 12.9 with 64 x 64, 1024 x 1280 x 5120 65 -> 53 with 128 x 128).
 #pragma once
 #include "gemm_dma.hpp"
+#include "cols_index.hpp"
 #include "fp8.hpp"
 
 namespace sd {
@@ -35,15 +36,9 @@ struct ColsProblem {
     int32_t tiles_m, tiles_n;
 };
 
-// Which row of 16 B rows is row i of block b: every B-th
-template <int B>
-__device__ __forceinline__ constexpr int spread(int b, int i) { return b / B * (16 * B) + B * i + b % B; }
-
-template <bool FP8, int BM, int BN>
-constexpr int cols_scale_words() { return FP8 ? ((BM + BN + 255) / 256) * 64 : 0; }      // of a stage
 template <bool FP8, int BM, int BN, int WGN, int STAGES, bool OUT8>
 constexpr int cols_lds_chunks() {
-    const int ring = STAGES * ((BM + BN) * 8 + cols_scale_words<FP8, BM, BN>() / 4);
+    const int ring = STAGES * ColsTileIndex<FP8, BM, BN, 1, 1, 1, STAGES, false, OUT8>::STAGE;
     return ring + BN / 4 + (OUT8 ? WGN * BM / 4 : 0);
 }
 
@@ -96,18 +91,11 @@ __device__ __forceinline__ void each(F f) {
 template <int MODE, int BM, int BN, int WGM, int WGN, int KS, int STAGES, bool GATED, bool OUT8, bool GUARD>
 __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, u32x4* const lds) {
     constexpr bool FP8 = MODE != COLS_BF16, WIDE = MODE == COLS_FP8_WIDE;
-    constexpr int NW = WGM * WGN * KS, WM = BM / WGM, WN = BN / WGN, MI = WM / 16, NI = WN / 16;
-    constexpr int ROWS8 = (BM + BN) / 8, LPT = (ROWS8 + NW - 1) / NW;      // loads of a step, and of a wavefront
-    constexpr bool EVEN = BM / 8 % NW == 0 && BN / 8 % NW == 0;            // (where not, some are made twice, and a wavefront's are of P or of Q as its number says)
+    using I = ColsTileIndex<FP8, BM, BN, WGM, WGN, KS, STAGES, GATED, OUT8>;
+    constexpr int NW = I::NW, WM = I::WM, WN = I::WN, MI = I::MI, NI = I::NI, LPT = I::LPT, STAGE = I::STAGE, PIECES = I::PIECES, NV = I::NV, BP = I::BP, BQ = I::BQ, BN_OUT = I::BN_OUT, WN_OUT = I::WN_OUT;
     constexpr int HC = 2 / KS;                         // chunks of a row's step that a lane works on
-    constexpr int SW = cols_scale_words<FP8, BM, BN>();
-    constexpr int STAGE = (BM + BN) * 8 + SW / 4;      // 16-byte chunks
-    constexpr int PIECES = SW / 64;
     constexpr int LOADS = LPT + (FP8 ? 1 : 0);
     constexpr int RING = NI >= 4 ? NI / 2 : NI;
-    constexpr int NV = GATED ? NI / 2 : NI;            // blocks of columns of the result
-    constexpr int BP = MI % 4 == 0 ? 4 : 2, BQ = OUT8 ? 4 : 2;
-    constexpr int BN_OUT = GATED ? BN / 2 : BN, WN_OUT = GATED ? WN / 2 : WN;
     static_assert(MI % BP == 0 && NV % BQ == 0 && NI % RING == 0 && (!WIDE || NI % 2 == 0) && STAGES >= 2 && STAGES <= 4, "tile");
     static_assert(KS == 1 || (KS == 2 && MODE != COLS_FP8 && MI % 2 == 0 && WGM * WGN * MI * NI * 64 <= STAGES * STAGE), "halves");
     static_assert(!FP8 || PIECES <= NW, "scales");
@@ -128,28 +116,21 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     const int half = KS == 2 ? wave / (WGM * WGN) : 0;
     const int wm = (KS == 2 ? wave % (WGM * WGN) : wave) / WGN * WM, wn = (wave % WGN) * WN, wn_out = (wave % WGN) * WN_OUT;
 
-    // ---- loads: load j of a wavefront fills rows 8 (j NW + wave) .. + 8 of a stage, lane l the chunk at position l % 8 of row l / 8.  They lie in one block, so what
-    // differs between value and gate is the wavefront's base.
+    // ---- loads (cols_index.hpp).  They lie in one block, so what differs between value and gate is the wavefront's base.
     uint32_t off[LPT];
     const uint8_t* base[LPT];
     const uint8_t* const pb = P.p + (int64_t)m0 * Kb;
     const uint8_t* const qb = P.q + (int64_t)n0 * Kb;
-    auto eight = [&](int j) { return EVEN ? j * NW + wave : min(j * NW + wave, ROWS8 - 1); };
-    auto chunk = [&](int j) { return swz<8>(eight(j) * 8 + (lane >> 3), lane & 7) * 16; };
+    auto chunk = [&](int j) { return I::chunk(I::eight(j, wave), lane); };
 #pragma unroll
     for (int j = 0; j < LPT; ++j) {
-        const int first = eight(j) * 8, row = first + (lane >> 3);
-        if (EVEN ? j < BM / 8 / NW : first < BM) {
-            const int w = first / WM, b = first % WM / 16;
-            const int r = min(m0 + w * WM + spread<BP>(b, row % 16), M - 1) - m0;
+        const int first = I::eight(j, wave) * 8, row = first + (lane >> 3);
+        if (I::of_p(j, first)) {
             base[j] = pb;
-            off[j] = (uint32_t)r * (uint32_t)Kb + chunk(j);
+            off[j] = (uint32_t)I::p_row(first, row, m0, M) * (uint32_t)Kb + chunk(j) * 16;
         } else {
-            const int w = (first - BM) / WN, b = (first - BM) % WN / 16;
-            const bool gate = GATED && b >= NV;
-            const int r = min(n0 + w * WN_OUT + spread<BQ>(gate ? b - NV : b, row % 16), N - 1) - n0;
-            base[j] = gate ? qb + (int64_t)N * Kb : qb;
-            off[j] = (uint32_t)r * (uint32_t)Kb + chunk(j);
+            base[j] = I::q_gate(first) ? qb + (int64_t)N * Kb : qb;
+            off[j] = (uint32_t)I::q_row(first, row, n0, N) * (uint32_t)Kb + chunk(j) * 16;
         }
     }
     // what the epilogue adds to columns: thread j has that of the tile's j-th (of the value's, then of the gate's)
@@ -158,16 +139,15 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
         const int j = GATED && tid >= BN_OUT ? tid - BN_OUT : tid;
         if (n0 + j < N) bias_raw = P.bias[n0 + j + (GATED && tid >= BN_OUT ? N : 0)];
     }
-    // scales: word a of a stage has those of rows 4 a .. 4 a + 3 of P's, then of Q's (values, gates); past the last row, the last word that there is
     const uint8_t* sp = nullptr;
     int64_t sp_step = 0;
     if constexpr (FP8) {
-        const int a = (wave % PIECES) * 64 + lane, j = a * 4 - BM;
-        if (j < 0 || j >= BN) {
-            sp = P.ps + min(m0 + (j < 0 ? a * 4 : 0), (M - 1) & ~3);
+        const int a = (wave % PIECES) * 64 + lane;
+        if (I::scale_of_p(a)) {
+            sp = P.ps + I::p_scale(a, m0, M);
             sp_step = P.ldps;
         } else {
-            sp = P.qs + min(n0 + (GATED && j >= BN_OUT ? N + j - BN_OUT : j), ((GATED ? 2 * N : N) - 1) & ~3);
+            sp = P.qs + I::q_scale(a, n0, N);
             sp_step = P.ldqs;
         }
     }
@@ -175,11 +155,11 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     const uint32_t scale_base = lds_base + (uint32_t)((BM + BN) * 128 + (PIECES ? wave % (PIECES ? PIECES : 1) : 0) * 256);
     // load j of step t; steps are loaded in order, each once
     auto load = [&](int j, int t, int stg, auto partial) {
-        const uint32_t to = lds_base + (uint32_t)stg * (STAGE * 16) + (uint32_t)eight(j) * 1024;
+        const uint32_t to = lds_base + (uint32_t)stg * (STAGE * 16) + (uint32_t)I::eight(j, wave) * 1024;
         const int kb = t * 128;
         if (decltype(partial)::value && kb + 128 > Kb) {
             const uint8_t* const src = base[j] + kb + off[j];
-            dma16(kb + (int)chunk(j) < Kb ? src : reinterpret_cast<const uint8_t*>(g_gemm_zeros), to);
+            dma16(I::there(kb, chunk(j), Kb) ? src : reinterpret_cast<const uint8_t*>(g_gemm_zeros), to);
         } else {
             dma16_so(base[j] + kb, off[j], to);
         }
@@ -198,29 +178,27 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     // ---- operands in registers: P's blocks, and a ring of Q's.  A lane has chunks quad and quad + 4 of a row, of halves the one or the other, of either operand: which k an MFMA's lane has does not matter, if it is the same ones.
     u32x4 pr[MI][HC], qr[RING][HC];
     uint32_t ps[FP8 ? MI / BP : 1], qs[FP8 ? NI / BQ : 1];     // scales of the step being multiplied
-    const int lsw = swz<8>(l16, 0);
     const u32x4* const frag = lds + l16 * 8;
-    auto part = [&](int h) { return ((KS == 2 ? half : h) * 4 + quad) ^ lsw; };
+    auto part = [&](int h) { return I::part(l16, (KS == 2 ? half : h) * 4 + quad); };
     auto fetch_p = [&](int st, int mi) {
 #pragma unroll
-        for (int h = 0; h < HC; ++h) pr[mi][h] = frag[st * STAGE + (wm + mi * 16) * 8 + part(h)];
+        for (int h = 0; h < HC; ++h) pr[mi][h] = frag[st * STAGE + I::p_block(wm, mi) + part(h)];
     };
     auto fetch_q = [&](int st, int ni) {
 #pragma unroll
-        for (int h = 0; h < HC; ++h) qr[ni % RING][h] = frag[st * STAGE + (BM + wn + ni * 16) * 8 + part(h)];
+        for (int h = 0; h < HC; ++h) qr[ni % RING][h] = frag[st * STAGE + I::q_block(wn, ni) + part(h)];
     };
     auto fetch_scales = [&](int st, auto& p, auto& q) {
         if constexpr (FP8) {
             const uint8_t* const sc = reinterpret_cast<const uint8_t*>(lds) + st * (STAGE * 16) + (BM + BN) * 128;
 #pragma unroll
             for (int i = 0; i < MI / BP; ++i) {
-                const uint8_t* const at = sc + wm + i * 16 * BP + BP * l16;
+                const uint8_t* const at = sc + I::p_scales_at(wm, i, l16);
                 p[i] = BP == 4 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
             }
 #pragma unroll
             for (int i = 0; i < NI / BQ; ++i) {
-                const bool gate = GATED && i >= NV / BQ;
-                const uint8_t* const at = sc + BM + wn_out + (gate ? BN_OUT : 0) + (gate ? i - NV / BQ : i) * 16 * BQ + BQ * l16;
+                const uint8_t* const at = sc + I::q_scales_at(wn_out, i, l16);
                 q[i] = BQ == 4 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at);
             }
         }
@@ -360,17 +338,17 @@ __device__ __forceinline__ void cols_tile(const ColsProblem& P, const int tile, 
     constexpr int ME = MI / KS;
     if constexpr (KS == 2) {
         __syncthreads();
-        f32x4* const swap = reinterpret_cast<f32x4*>(lds) + (wave % (WGM * WGN)) * (MI * NI * 64) + lane;
+        f32x4* const swap = reinterpret_cast<f32x4*>(lds) + I::meet(wave % (WGM * WGN), 0, 0, lane);
 #pragma unroll
-        for (int i = 0; i < ME * NI; ++i) swap[((1 - half) * ME * NI + i) * 64] = half ? acc[i / NI][i % NI] : acc[ME + i / NI][i % NI];
+        for (int i = 0; i < ME * NI; ++i) swap[I::meet(0, 1 - half, i, 0)] = half ? acc[i / NI][i % NI] : acc[ME + i / NI][i % NI];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < ME * NI; ++i) acc[i / NI][i % NI] = (half ? acc[ME + i / NI][i % NI] : acc[i / NI][i % NI]) + swap[(half * ME * NI + i) * 64];
+        for (int i = 0; i < ME * NI; ++i) acc[i / NI][i % NI] = (half ? acc[ME + i / NI][i % NI] : acc[i / NI][i % NI]) + swap[I::meet(0, half, i, 0)];
     }
     // ---- epilogue.  A lane has rows spread<BP>(mi, l16) of its wavefront's, and of each group of 16 BQ columns the 4 BQ from 4 BQ quad on.
     constexpr int W4 = BQ, NG = NV / BQ;               // pieces of four columns of a lane in a group; groups
-    auto column = [&](int g) { return n0 + wn_out + (g * 4 + quad) * 4 * W4; };
-    auto row_of = [&](int mi) { return wm + (KS == 2 ? spread<BP>(half * ME + mi, l16) : spread<BP>(mi, l16)); };
+    auto column = [&](int g) { return n0 + I::result_column(wn_out, g, quad); };
+    auto row_of = [&](int mi) { return I::result_row(wm, KS == 2 ? half * ME + mi : mi, l16); };
     // element x of piece c of group g, of the blocks from `first` on
     auto element = [&](int mi, int first, int g, int c, int x) -> float& { return reinterpret_cast<float(&)[4]>(acc[mi][first + g * BQ + (4 * c + x) % BQ])[(4 * c + x) / BQ]; };
     auto piece = [&](int mi, int first, int g, int c) {

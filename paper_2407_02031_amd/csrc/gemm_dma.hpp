@@ -2,16 +2,9 @@
 // workgroup finds its tile.
 #pragma once
 #include "common.hpp"
+#include "swizzle.hpp"
 
 namespace sd {
-
-// XOR swizzle of the 16-byte chunk index inside an LDS row of CPR chunks (8: 128-byte rows,
-// 4: 64-byte rows): any 16 consecutive rows put the same logical chunk in 16 distinct
-// 16-byte slots of a 256-byte bank window.
-template <int CPR>
-__device__ __forceinline__ int swz(int row, int chunk) {
-    return CPR == 8 ? (chunk ^ ((row >> 1) & 7)) : (chunk ^ ((row >> 2) & 3));
-}
 
 // GELU, exact (erf) form, with erf by Abramowitz & Stegun 7.1.26 (|error| <= 1.5e-7, far below
 // bf16 resolution): erf(|x|) = 1 - (a1 t + ... + a5 t^5) exp(-x^2), t = 1 / (1 + p |x|).
