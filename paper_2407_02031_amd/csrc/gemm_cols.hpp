@@ -510,7 +510,8 @@ __global__ __launch_bounds__(64 * WGM * WGN * KS, (cols_lds_chunks<MODE != COLS_
 
 // Few rows (one token's, a guidance pair's, a short text's).  A workgroup has 16 MB rows and 16 NB columns (of a gated product of value and gate each); its eight wavefronts take every eighth
 // step of 128 bytes and bring the rows of P and Q straight into the registers as MFMA operands, U steps at once, and meet in LDS when they are done.  Bound by Q, which comes in once per
-// 16 MB rows, and one trip to HBM.
+// 16 MB rows, and by trips to HBM one after the other: one for every eight U steps, and those of the epilogue's operands (a bias is widened where it is loaded, which waits for the steps before it; then the gate's, or
+// the residual, is asked for).
 constexpr int FEW_NW = 8;
 template <bool FP8, bool GATED, int MB, int NB, int U>
 __global__ __launch_bounds__(64 * FEW_NW) void few_rows_kernel(const ColsProblem P) {

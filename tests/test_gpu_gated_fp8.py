@@ -1264,3 +1264,21 @@ def test_rmsnorm_to_8_bits_of_what_is_not_finite(B, C):
             rows = torch.arange(M, device="cuda") != M // 2
             assert got.q[M // 2].double().isnan().all() and (got.scales.contiguous().view(torch.uint8)[:, M // 2] == 1).all()
             assert torch.equal(got.q.view(torch.uint8)[rows], whole.q.view(torch.uint8)[rows])
+
+
+@pytest.mark.parametrize("M,N,K", [(1003, 317, 648), (2048, 640, 320), (600, 2560, 1280)])
+@pytest.mark.parametrize("act", [1, 2, 3])
+def test_gated_bwd_loses_the_rounding_of_dz_alone(B, M, N, K, act):
+    """Against products of dz as bf16 holds it: what is left is the results' own rounding, sums in fp32, and dz that fp32 rounds to the other side of a tie (1e-6 of it off, steps of 2^-8 apart: one in a thousand, 2^-8 each)"""
+    import torch
+    x, W, _, g = lin_inputs(M, 2 * N, K, M + N)
+    dy, z = randn(g, M, N).bfloat16(), randn(g, M, 2 * N, scale=1.5).bfloat16()
+    zz = z.double().requires_grad_(True)
+    dz = torch.autograd.grad(zz[:, :N] * act64(zz[:, N:], act), zz, dy.double())[0]
+    held = dz.bfloat16().double()
+    off = lambda a, ref: float((a.double() - ref).norm() / ref.norm())
+    dx, dW, _ = B.gated_linear_bwd(dy, x, W, z, act, dw_dtype=torch.float32)
+    rx, rw = held @ W.double(), held.T.contiguous() @ x.double()
+    assert off(dW, rw) <= math.sqrt(1e-3) * 2.0 ** -8 and off(dx, rx) <= off(rx.bfloat16(), rx) + math.sqrt(1e-3) * 2.0 ** -8
+    # ... and dz's rounding, uniform in steps of 2^-8 to 2^-7 of it, is what it costs
+    assert 1e-3 < off(rw, dz.T.contiguous() @ x.double()) < 2.0 ** -9
