@@ -165,7 +165,7 @@ struct GatedDzCut {
     }
 };
 // The same of a gated layer: dy [M, N] and z = [v, g] [M, 2 N] in, dz = [dy act(g), dy v act'(g)] [M, Np] out, Np 2 N rounded up to a multiple of 8; its column sums are 2 N.  Where N is
-// no multiple of eight, accesses to the gate's half are aligned to an element alone.  Bound by HBM: 8192 x 5120 bf16 with SiLU 72 to 74 us (420 MB, 5.7 TB/s).  dz is rounded to bf16 as above.
+// no multiple of eight, accesses to the gate's half are aligned to an element alone.  Bound by HBM: 8192 x 5120 bf16 with SiLU 70 to 72 us (420 MB, 5.8 to 6.0 TB/s).  dz is rounded to bf16 as above.
 // PAST: a large z is read past the caches, which dz has to itself then (all of the backward pass, us, past / through: 8192 x 1280 to 5120 456 / 463, 8192 x 640 to 2560 151 / 157, 4096 x 1280 to 5120 231.7 / 233.4;
 // but 2048 135.5 / 134.8 and 2048 x 640 to 2560 50.6 / 49.4).
 template <class D, bool STORE, bool SUMS, bool PAST>

@@ -6,9 +6,9 @@
 // Bound by HBM: every element is read once and written once.  Rows lie in registers as layer norm's do (norm_rows.hpp), and the norm is of h as it is in fp32, before it is rounded
 // to its type.  A block of 128 elements lies in 32 neighbouring lanes (or in 16, twice), so a row in 8 bits takes no pass of its own and no LDS.
 //
-// Measured (kernels alone, cold; mean and least): 8192 x 1280 bf16 onto fp32, h and 8 bits out, 18.6 and 17.6 us (115 MB, 6.2 to 6.6 TB/s); backward fp32 with the stream's gradient and the weight's 28.9 and
-// 25.8 (147 MB) and 4.2 for the sums (in bf16 25.8 in the mean, 16.2 without the stream's gradient: each chunk of it is widened in a branch of its own, which waits for all loads before it asks for the next; gamma's
-// chunks likewise, ahead of the first row); 10240 x 1280 bf16 quantized 9.8 and 9.3 (39 MB); one row 3.3 and 2.3.  (Of the twelve backward kernels beyond C = 4096 with the weight's gradient six keep 12 to 40
+// Measured (kernels alone, cold; mean and least): 8192 x 1280 bf16 onto fp32, h and 8 bits out, 18.7 and 16.8 us (115 MB, 6.1 to 6.8 TB/s); backward fp32 with the stream's gradient and the weight's 28.3 and
+// 26.0 (147 MB) and 4.1 for the sums (in bf16 25.8 in the mean, 16.2 without the stream's gradient: each chunk of it is widened in a branch of its own, which waits for all loads before it asks for the next; gamma's
+// chunks likewise, ahead of the first row); 10240 x 1280 bf16 quantized 9.5 and 9.0 (39 MB); one row 3.5 and 2.3.  (Of the twelve backward kernels beyond C = 4096 with the weight's gradient six keep 12 to 40
 // bytes a lane in scratch.)
 #include "norm_rows.hpp"
 #include "fp8.hpp"
