@@ -370,7 +370,7 @@ def _on(x: torch.Tensor) -> int:
     dev = x.get_device()
     if dev < 0:
         raise ValueError(f"a tensor on {x.device}: not on a GPU")
-    if dev != torch._C._cuda_getDevice():      # (x is on one, so they are initialised: torch.cuda.current_device, which makes sure, takes twice as long)
+    if dev != torch.cuda.current_device():
         raise ValueError(f"a tensor on {x.device}, the current device is {torch.cuda.current_device()}")
     return dev
 

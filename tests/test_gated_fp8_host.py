@@ -292,3 +292,16 @@ def test_whole_sums_are_widened(B):
                 assert f(L, M=M, N=N, K=K, xl=ld, wl=ld, yt=yt, act=B.SD_WHOLE_SUMS + i % 5, **kw) == 0
             assert "wide" in names[0] or "few rows" in names[0]
             assert names[1:] == (["quantize"] if kw.get("n") and yt == 2 else [])
+
+
+def test_the_current_device_is_asked_for_by_its_public_name(B, monkeypatch):
+    import torch
+
+    class OnTheFirst:
+        device = "cuda:0"
+        get_device = staticmethod(lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert B._on(OnTheFirst) == 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="the current device is 1"):
+        B._on(OnTheFirst)
