@@ -1282,3 +1282,31 @@ def test_gated_bwd_loses_the_rounding_of_dz_alone(B, M, N, K, act):
     assert off(dW, rw) <= math.sqrt(1e-3) * 2.0 ** -8 and off(dx, rx) <= off(rx.bfloat16(), rx) + math.sqrt(1e-3) * 2.0 ** -8
     # ... and dz's rounding, uniform in steps of 2^-8 to 2^-7 of it, is what it costs
     assert 1e-3 < off(rw, dz.T.contiguous() @ x.double()) < 2.0 ** -9
+
+
+@pytest.mark.parametrize("M,N,K,kernel", [k[1:] for k in LIN8_KERNELS if k[0] == "float32"] + [(1000, 500, 144, "few rows 8 bits 64x32")])
+def test_linear_fp8_whole_sums_every_kernel(B, M, N, K, kernel):
+    """In bf16, with bias and residual, from the kernels that y in fp32 has"""
+    import torch
+    g = gen(M + K)
+    x, W = rows8(B, g, M, K), rows8(B, g, N, K, 1.3 / math.sqrt(K), 0.3)
+    bias, res = randn(g, N, scale=0.5).bfloat16(), randn(g, M, N).bfloat16()
+    with B.dry_run() as names:
+        B.linear_fp8_fwd(x, W, bias, 1, residual=res, whole_sums=True)
+    assert names == [kernel]
+    z, ez = product(x, W, bias, True)
+    for r in (res, None):
+        ref = act64(z, 3) + (r.double() if r is not None else 0)
+        within(B.linear_fp8_fwd(x, W, bias, 3, residual=r, whole_sums=True), ref, 1.13 * ez + 4e-7 * (1 + z.abs()) + 2 * U * ref.abs())
+
+
+@pytest.mark.parametrize("M,N,K,kernel", [k[1:] for k in GATED8_KERNELS if k[0] == "float32"])
+def test_gated_fp8_whole_sums_every_kernel(B, M, N, K, kernel):
+    import torch
+    g = gen(M + K)
+    x, W = rows8(B, g, M, K), rows8(B, g, 2 * N, K, 1.3 / math.sqrt(K), 0.3)
+    bias = randn(g, 2 * N, scale=0.5).bfloat16()
+    with B.dry_run() as names:
+        B.gated_linear_fp8_fwd(x, W, bias, 3, whole_sums=True)
+    assert names == [kernel]
+    within(B.gated_linear_fp8_fwd(x, W, bias, 3, whole_sums=True), *gated_ref(*product(x, W, bias, True), 3))
