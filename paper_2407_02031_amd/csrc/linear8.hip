@@ -68,8 +68,10 @@ static int launch_few8(const ColsProblem& P, bool wide, bool& taken, hipStream_t
     case FEW_32x32: return launch_few<true, GATED, 2, 2, GATED ? 2 : 3>(P, s);
     case FEW_64x32:
         if constexpr (!GATED) return launch_few<true, false, 4, 2, 2>(P, s);
-    default: return SD_OK;
+        break;
+    default: break;
     }
+    return SD_OK;
 }
 // y in 8 bits by way of fp32, in two launches: where a block's columns lie in several workgroups (few rows, smaller tiles), which a long reduction makes up for.  (us, one launch / two, of which the second
 // is 6, and what the rule adds for it, with its start, 9: 64 x 1280 x 5120 30.2 / 18, 256 of them 32.5 / 22; 64 x 5120 x 1280 11.6 / 13.)
